@@ -1,4 +1,4 @@
-"""Binding of libagattn.so: same names as include/ag.h, argument
+"""Binding of libagattn.so: same names as include/ag.h and its companions, argument
 marshalling only.  Every step of the path runs in the HIP kernels behind the
 C ABI; tensors are torch CUDA (ROCm) tensors used as device memory.
 
@@ -33,6 +33,9 @@ EXPORTS = [
     "ag_stream_create_cumask", "ag_stream_destroy", "ag_cumask_build", "ag_probe_placement", "ag_device_info",
     "ag_debug_validate", "ag_prof_enable", "ag_prof_collect", "ag_prof_disable", "ag_status_string",
     "ag_last_error", "ag_version",
+    # ag_q8.h
+    "ag_kv_append_q8", "ag_kv_read_q8", "ag_attn_prefill_q8", "ag_attn_resume_q8", "ag_attn_decode_q8_workspace_bytes",
+    "ag_attn_decode_q8",
     # ag_sched.h
     "ag_ctl_create", "ag_ctl_destroy", "ag_ctl_record_decode", "ag_ctl_tick", "ag_ctl_get", "ag_ctl_classify",
     "ag_partition_level_for", "ag_slots_create", "ag_slots_destroy", "ag_slots_count", "ag_slots_units",
@@ -78,6 +81,11 @@ class ag_kv_cache(C.Structure):
                 ("dtype", C.c_int32)]
 
 
+class ag_kv_cache_q8(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("exps", C.c_void_p), ("num_pages", C.c_int32),
+                ("page_size", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
 _lib = None
 
 
@@ -106,6 +114,14 @@ def lib():
     l.ag_attn_merged_workspace_bytes.restype = C.c_size_t
     l.ag_attn_merged.argtypes = [cp, vp, vp, i32p, i32, i32p, i32p, i32p, i32, i32, i32, i32, i32, C.c_float, vp,
                                  C.c_size_t, vp]
+    c8 = C.POINTER(ag_kv_cache_q8)
+    l.ag_kv_append_q8.argtypes = [c8, vp, vp, i32p, i32, i32p, i32p, i32p, i32, i32, vp]
+    l.ag_kv_read_q8.argtypes = [c8, vp, vp, i32p, i32, i32p, i32p, i32p, i32, i32, vp]
+    l.ag_attn_prefill_q8.argtypes = [c8, vp, vp, i32p, i32, i32p, i32p, i32, i32, i32, i32, C.c_float, vp]
+    l.ag_attn_resume_q8.argtypes = [c8, vp, vp, i32p, i32, i32p, i32p, i32p, i32, i32, i32, i32, i32, C.c_float, vp]
+    l.ag_attn_decode_q8_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    l.ag_attn_decode_q8_workspace_bytes.restype = C.c_size_t
+    l.ag_attn_decode_q8.argtypes = [c8, vp, vp, i32p, i32, i32p, i32, i32, i32, C.c_float, vp, C.c_size_t, vp]
     l.ag_stream_create_cumask.argtypes = [C.POINTER(vp), u32p, i32]
     l.ag_stream_destroy.argtypes = [vp]
     l.ag_cumask_build.argtypes = [u32p, i32, i32, i32, i32, i32]
@@ -144,7 +160,7 @@ def lib():
     l.ag_pager_page_state.argtypes = [vp, i32]
     l.ag_pager_get_stats.argtypes = [vp, C.POINTER(ag_pager_stats)]
     for name in EXPORTS:
-        if name not in ("ag_attn_decode_workspace_bytes", "ag_decode_step_workspace_bytes", "ag_attn_merged_workspace_bytes", "ag_status_string", "ag_last_error", "ag_version"):
+        if name not in ("ag_attn_decode_workspace_bytes", "ag_decode_step_workspace_bytes", "ag_attn_merged_workspace_bytes", "ag_attn_decode_q8_workspace_bytes", "ag_status_string", "ag_last_error", "ag_version"):
             getattr(l, name).restype = C.c_int
     l.ag_status_string.argtypes = [C.c_int]
     for name in ("ag_status_string", "ag_last_error", "ag_version"):
@@ -154,7 +170,8 @@ def lib():
 
 
 _native = None
-_CALLS = ("kv_append", "attn_prefill", "attn_resume", "attn_decode", "attn_decode_static", "decode_step", "attn_merged")
+_CALLS = ("kv_append", "attn_prefill", "attn_resume", "attn_decode", "attn_decode_static", "decode_step", "attn_merged",
+          "kv_append_q8", "kv_read_q8", "attn_prefill_q8", "attn_resume_q8", "attn_decode_q8")
 
 
 class _NoCalls:
@@ -177,7 +194,7 @@ def _load_calls():
     here = f"torch {torch.__version__} python {sys.version_info[0]}.{sys.version_info[1]}"
     if getattr(m, "built_for", None) != here:                 # it reads torch's and Python's objects directly
         raise ImportError(f"{CALL_PATH} is built for {getattr(m, 'built_for', 'an unknown torch')}, this is {here}")
-    m.setup(KVCache, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+    m.setup(KVCache, KVCacheQ8, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
             *(C.cast(getattr(l, "ag_" + name), C.c_void_p).value for name in _CALLS))
     return m
 
@@ -367,6 +384,103 @@ def ag_attn_merged(cache: KVCache, q, out, block_tables, prefix_lens, new_lens, 
                                 _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0], total_new,
                                 max_new, max_ctx, num_q_heads, scale, _ptr(workspace),
                                 workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+class KVCacheQ8:
+    """Caller-owned pools of an 8-bit cache plus the geometry the library needs (mirrors ag_kv_cache_q8).  `dtype` is the type of
+    the activations.  `fill`: a byte for every slot of the pools and exponents (0x7F and 0xFF are NaN in the pools)."""
+
+    def __init__(self, num_pages: int, page_size: int, num_kv_heads: int, head_dim: int, dtype: int, device="cuda",
+                 fill: Optional[int] = None):
+        if head_dim <= 0 or head_dim % 16 or page_size <= 0 or page_size % 16:
+            raise ValueError("an 8-bit cache has a head_dim and a page_size that are multiples of 16")
+
+        def mk(*shape):
+            return torch.empty(shape, dtype=torch.uint8, device=device) if fill is None else \
+                torch.full(shape, fill, dtype=torch.uint8, device=device)
+        e4m3 = torch.float8_e4m3fn
+        self.k_pool = mk(num_pages, num_kv_heads, page_size // 4, head_dim // 16, 4, 16).view(e4m3)
+        self.v_pool = mk(num_pages, num_kv_heads, page_size // 16, head_dim, 16).view(e4m3)
+        self.exps = mk(num_pages, num_kv_heads, 2, page_size)
+        self.num_pages, self.page_size = num_pages, page_size
+        self.num_kv_heads, self.head_dim, self.dtype = num_kv_heads, head_dim, dtype
+
+    def c_struct(self) -> ag_kv_cache_q8:
+        return ag_kv_cache_q8(self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.exps.data_ptr(), self.num_pages, self.page_size,
+                              self.num_kv_heads, self.head_dim, self.dtype)
+
+    def k_pool_token_major(self) -> torch.Tensor:
+        """The key pool's bytes as [page][head][slot][d] (the library stores [slot / 4][d / 16][4][16])."""
+        return self.k_pool.view(torch.uint8).permute(0, 1, 2, 4, 3, 5).reshape(self.num_pages, self.num_kv_heads, self.page_size, self.head_dim)
+
+    def v_pool_token_major(self) -> torch.Tensor:
+        """The value pool's bytes as [page][head][slot][d] (the library stores [slot / 16][d][16])."""
+        return self.v_pool.view(torch.uint8).permute(0, 1, 2, 4, 3).reshape(self.num_pages, self.num_kv_heads, self.page_size, self.head_dim)
+
+    def exps_token_major(self):
+        """The exponent bytes of keys and of values, each [page][head][slot]."""
+        s = torch.arange(self.page_size, device=self.exps.device)
+        return self.exps[:, :, 0][..., (s & ~15) | ((s & 3) << 2) | ((s >> 2) & 3)], self.exps[:, :, 1]
+
+
+def ag_kv_append_q8(cache: KVCacheQ8, k_new, v_new, block_tables, prefix_lens, new_lens, cu_new, total_new: int, stream=None):
+    st = (_native or _calls()).kv_append_q8(cache, k_new, v_new, block_tables, prefix_lens, new_lens, cu_new, total_new, stream)
+    if st is not None:
+        return _check(st)
+    c = cache.c_struct()
+    _check(lib().ag_kv_append_q8(C.byref(c), _ptr(k_new), _ptr(v_new), _i32(block_tables), block_tables.shape[1],
+                                 _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0], total_new,
+                                 _stream(stream)))
+
+
+def ag_kv_read_q8(cache: KVCacheQ8, k_out, v_out, block_tables, prefix_lens, new_lens, cu_new, total_new: int, stream=None):
+    st = (_native or _calls()).kv_read_q8(cache, k_out, v_out, block_tables, prefix_lens, new_lens, cu_new, total_new, stream)
+    if st is not None:
+        return _check(st)
+    c = cache.c_struct()
+    _check(lib().ag_kv_read_q8(C.byref(c), _ptr(k_out), _ptr(v_out), _i32(block_tables), block_tables.shape[1],
+                               _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0], total_new,
+                               _stream(stream)))
+
+
+def ag_attn_prefill_q8(cache: KVCacheQ8, q, out, block_tables, new_lens, cu_new, total_new: int, max_new: int,
+                       num_q_heads: int, scale: float, stream=None):
+    st = (_native or _calls()).attn_prefill_q8(cache, q, out, block_tables, new_lens, cu_new, total_new, max_new, num_q_heads,
+                                              scale, stream)
+    if st is not None:
+        return _check(st)
+    c = cache.c_struct()
+    _check(lib().ag_attn_prefill_q8(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1],
+                                    _i32(new_lens), _i32(cu_new), new_lens.shape[0], total_new, max_new, num_q_heads,
+                                    scale, _stream(stream)))
+
+
+def ag_attn_resume_q8(cache: KVCacheQ8, q, out, block_tables, prefix_lens, new_lens, cu_new, total_new: int,
+                      max_new: int, max_ctx: int, num_q_heads: int, scale: float, stream=None):
+    st = (_native or _calls()).attn_resume_q8(cache, q, out, block_tables, prefix_lens, new_lens, cu_new, total_new, max_new,
+                                             max_ctx, num_q_heads, scale, stream)
+    if st is not None:
+        return _check(st)
+    c = cache.c_struct()
+    _check(lib().ag_attn_resume_q8(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1],
+                                   _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0], total_new,
+                                   max_new, max_ctx, num_q_heads, scale, _stream(stream)))
+
+
+def ag_attn_decode_q8_workspace_bytes(batch: int, num_q_heads: int, head_dim: int, max_ctx: int) -> int:
+    return int(lib().ag_attn_decode_q8_workspace_bytes(batch, num_q_heads, head_dim, max_ctx))
+
+
+def ag_attn_decode_q8(cache: KVCacheQ8, q, out, block_tables, ctx_lens, max_ctx: int, num_q_heads: int, scale: float,
+                      workspace: torch.Tensor, stream=None):
+    st = (_native or _calls()).attn_decode_q8(cache, q, out, block_tables, ctx_lens, max_ctx, num_q_heads, scale, workspace,
+                                             stream)
+    if st is not None:
+        return _check(st)
+    c = cache.c_struct()
+    _check(lib().ag_attn_decode_q8(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1],
+                                   _i32(ctx_lens), ctx_lens.shape[0], max_ctx, num_q_heads, scale, _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def ag_cumask_build(total_cus: int, n_xcd: int, first_cu_per_xcd: int, cus_per_xcd: int) -> list:

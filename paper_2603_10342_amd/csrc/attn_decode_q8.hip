@@ -1,0 +1,396 @@
+// Decode over the 8-bit paged KV cache: one query per session, any group size, head_dim a multiple of 16 up to 256.
+//
+// Bound by HBM: 2 Hkv (D + 1) bytes a cached token, read once for all query heads of a KV head.  The schedule is that of the other
+// caches' decode: the batch's (session, KV head, block of 16 query heads) pairs are laid end to end in steps - here of 64 tokens, the
+// same bytes as 32 of bf16 - and dealt to the workgroups in equal shares (find_share); a share's part of a pair is a segment, whose
+// steps the four waves take in contiguous quarters; the segments' (m, l, O) meet in a merge kernel in their order.
+//
+// A wave's step is four 16-token groups, whatever pages they lie in:
+//   scores  S^T[token][head]: 16x16x32 bf16 products, rows = 4 slots of each of the 4 groups (product j takes slots 4 j .. 4 j + 3),
+//           so that lane group c ends up with all 16 slots of group c - which is what a 16-byte load of the value pool holds
+//           of a channel.  The key pool stores four slots of a 16-channel chunk in a run: a load reads 256 contiguous bytes of every group.
+//   values  O^T[channel][head] += V^T . P^T, the weights of a lane's 16 slots against 16-byte pieces, slots 0..7 and 8..15.
+// Keys and values become bf16 on the way into the products, exactly, two numbers an instruction; a key's power of two goes in
+// with that instruction, a value's is multiplied into its weight.
+// bf16 activations: weights are rounded to bf16 for the value product, as over bf16 caches (half a step of 2^-8, independent for
+// every key, beside the output's own rounding); fp32: queries and weights as three bf16 terms, 24 bits.
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "attn_split_common.h"
+#include "bf16_terms.h"
+#include "q8_internal.h"
+
+namespace ag {
+namespace q8 {
+namespace {
+
+using splitk::find_share;
+using splitk::Share;
+
+constexpr int kTok = 64;                // tokens of a step
+constexpr int kCols = 16;               // query heads of a pair, at most
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ int steps_of(int ctx) { return splitk::steps_of<kTok>(ctx); }
+__host__ __device__ inline int blocks_of(int G) { return (G + kCols - 1) / kCols; }
+
+// A number of the activations' type as kTerms bf16 terms: operands of the products
+template <typename A>
+constexpr int terms_of() { return sizeof(A) == 4 ? 3 : 1; }
+
+__device__ __forceinline__ void to_terms(const __bf16* p, bf16x8 (&t)[1]) { t[0] = *reinterpret_cast<const bf16x8*>(p); }
+__device__ __forceinline__ void to_terms(const float* p, bf16x8 (&t)[3])
+{
+    const Terms x = split8(*reinterpret_cast<const Four*>(p), *reinterpret_cast<const Four*>(p + 4));
+    t[0] = __builtin_bit_cast(bf16x8, x.h);
+    t[1] = __builtin_bit_cast(bf16x8, x.m);
+    t[2] = __builtin_bit_cast(bf16x8, x.l);
+}
+__device__ __forceinline__ void to_terms(const float (&w)[8], bf16x8 (&t)[1])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[0][i] = (__bf16)w[i];
+}
+__device__ __forceinline__ void to_terms(const float (&w)[8], bf16x8 (&t)[3])
+{
+    Terms x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.set_pair(i, w[2 * i], w[2 * i + 1]);
+    t[0] = __builtin_bit_cast(bf16x8, x.h);
+    t[1] = __builtin_bit_cast(bf16x8, x.m);
+    t[2] = __builtin_bit_cast(bf16x8, x.l);
+}
+// acc += a . (sum of b's terms), smallest terms first
+template <int kTerms>
+__device__ __forceinline__ f32x4 product(const bf16x8& a, const bf16x8 (&b)[kTerms], f32x4 acc)
+{
+#pragma unroll
+    for (int t = kTerms - 1; t >= 0; --t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[t], acc, 0, 0, 0);
+    return acc;
+}
+
+__device__ __forceinline__ u32x4 stream16(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+
+// One wave's part of a segment, steps u0 .. u0 + n - 1 of (session s, KV head g, heads h0 .. h0 + nh - 1 of its group): running maximum,
+// this lane's share of the sum, and O^T.  o[mb][i]: channel 16 mb + 4 c + i of head r, lane = 16 c + r.
+template <typename A, int DT, bool kExact>
+__device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0, int nh, int ctx, int u0, int n, int lane,
+                                             float& m, float& lsum, f32x4 (&o)[DT / 16])
+{
+    constexpr int kTerms = terms_of<A>(), kH = DT / 64, kV = DT / 16;          // 64-channel blocks of the keys, 16-channel blocks of the values
+    const AttnArgs& a = x.a;
+    const int hkv = a.c.hkv, D = kExact ? DT : a.c.d, ps = a.c.ps, chunks = D >> 4;
+    const int r = lane & 15, c = lane >> 4;
+    const float unit = a.scale * kLog2e;
+    m = -INFINITY;
+    lsum = 0.f;
+#pragma unroll
+    for (int mb = 0; mb < kV; ++mb) o[mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (n <= 0) return;
+
+    // the queries as B operands: column = head r, k = channels (4 h + c) * 16 + 8 half .. + 7; zero beyond the heads and channels
+    bf16x8 q[kH][2][kTerms];
+    {
+        const A* row = (const A*)a.q + ((int64_t)s * a.hq + (int64_t)g * (a.hq / hkv) + h0 + min(r, nh - 1)) * D;
+#pragma unroll
+        for (int h = 0; h < kH; ++h)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int chunk = kExact ? 4 * h + c : min(4 * h + c, chunks - 1);
+                to_terms(row + chunk * 16 + half * 8, q[h][half]);
+                if (r >= nh || (!kExact && 4 * h + c >= chunks)) {
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) q[h][half][t] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                }
+            }
+    }
+
+    const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
+    const int64_t block = (int64_t)D * ps;                       // bytes of one (page, head)
+    const uint8_t* const kpool = (const uint8_t*)a.c.k;
+    const uint8_t* const vpool = (const uint8_t*)a.c.v;
+    // page ids by scalar loads: the index is uniform and the table read-only for the kernel's lifetime
+    typedef const __attribute__((address_space(4))) int32_t* cptr_t;
+    const cptr_t bt = (cptr_t)(uintptr_t)(a.bt + (int64_t)s * a.max_pages);
+    struct Pages { int k, v; };                                  // of this lane's group of the keys, and of the values
+    auto pages_of = [&](int st) {
+        Pages p = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int id = bt[min(4 * (u0 + st) + i, last_grp) >> gshift];
+            p.k |= id & ((r >> 2) == i ? -1 : 0);
+            p.v |= id & (c == i ? -1 : 0);
+        }
+        return p;
+    };
+
+    u32x4 k[4][kH], v[kV], ve;
+    uint32_t ke;
+    auto load_k = [&](int st, Pages p) {
+        const int gi = min(4 * (u0 + st) + (r >> 2), last_grp) & gmask;
+        const int64_t at = (int64_t)p.k * hkv + g;
+        const uint8_t* kp = kpool + at * block + gi * 16 * D + (r & 3) * 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int h = 0; h < kH; ++h) {
+                const int chunk = kExact ? 4 * h + c : min(4 * h + c, chunks - 1);       // (beyond: times zeros of the query)
+                k[j][h] = stream16(kp + (j * chunks + chunk) * 64);
+            }
+        ke = *reinterpret_cast<const uint32_t*>(x.exps + at * (2 * ps) + gi * 16 + (r & 3) * 4);
+    };
+    auto load_v = [&](int st, Pages p) {
+        const int gi = min(4 * (u0 + st) + c, last_grp) & gmask;
+        const int64_t at = (int64_t)p.v * hkv + g;
+        const uint8_t* vp = vpool + at * block + gi * 16 * D;
+#pragma unroll
+        for (int mb = 0; mb < kV; ++mb) v[mb] = stream16(vp + (kExact ? mb * 16 + r : min(mb * 16 + r, D - 1)) * 16);
+        ve = *reinterpret_cast<const u32x4*>(x.exps + at * (2 * ps) + ps + gi * 16);
+    };
+
+    Pages pg = pages_of(0);
+    load_k(0, pg);
+    load_v(0, pg);
+    pg = pages_of(1);
+    __builtin_amdgcn_sched_barrier(0);
+
+    // One step; unless it is the wave's last, the next step's keys are requested as soon as the scores have taken this one's, and
+    // its values as soon as the value product has: half a step of every wave is always in flight in the registers of one.
+    // Only a wave's last step can reach behind the context.
+    auto step = [&](int st, auto last_c) {
+        constexpr bool kLast = decltype(last_c)::value;
+        f32x4 sc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const float scale = power((ke >> (8 * j)) & 0xFFu);
+#pragma unroll
+            for (int h = 0; h < kH; ++h) {
+                sc[j] = product(widen8(k[j][h][0], k[j][h][1], scale), q[h][0], sc[j]);
+                sc[j] = product(widen8(k[j][h][2], k[j][h][3], scale), q[h][1], sc[j]);
+            }
+        }
+        if constexpr (!kLast) {
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(st + 1, pg);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // sc[j][i]: slot 4 j + i of group c
+        const int keep = ctx - ((u0 + st) * kTok + c * 16);      // slot e exists iff e < keep
+        float xs[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) xs[e] = !kLast || e < keep ? sc[e >> 2][e & 3] * unit : -INFINITY;
+        float mx = xs[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, xs[e]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m, mx);
+        const float m_ref = m_new == -INFINITY ? 0.f : m_new;    // (scores that are all -inf or NaN)
+        const float alpha = __builtin_amdgcn_exp2f(m - m_ref);
+        float psum = 0.f;
+        bf16x8 w[2][kTerms];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int e = half * 8 + i;
+                p[i] = __builtin_amdgcn_exp2f(xs[e] - m_ref);
+                psum += p[i];
+                p[i] = !kLast || e < keep ? p[i] * power_of(ve, e) : 0.f;      // (a stale power may be an infinity)
+            }
+            to_terms(p, w[half]);
+        }
+        lsum = lsum * alpha + psum;
+        m = m_new;
+        if constexpr (kLast) {                                   // slots behind the last token may hold anything, NaN included
+#pragma unroll
+            for (int mb = 0; mb < kV; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[mb][i] = keep_bytes(v[mb][i], keep - 4 * i);
+        }
+#pragma unroll
+        for (int mb = 0; mb < kV; ++mb) {
+            o[mb] *= alpha;
+            o[mb] = product(widen8(v[mb][0], v[mb][1], 1.f), w[0], o[mb]);
+            o[mb] = product(widen8(v[mb][2], v[mb][3], 1.f), w[1], o[mb]);
+        }
+        if constexpr (!kLast) {
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(st + 1, pg);
+            pg = pages_of(st + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+#pragma unroll 1
+    for (int st = 0; st + 1 < n; ++st) step(st, std::false_type{});
+    step(n - 1, std::true_type{});
+}
+
+// LDS of a workgroup: per wave and head O, then m and l
+constexpr int kWaves = 4;
+inline size_t lds_of(int nh, int d) { return (size_t)kWaves * nh * (d + 2) * sizeof(float); }
+
+template <typename A, int DT, bool kExact>
+__global__ __launch_bounds__(64 * kWaves, DT > 128 || sizeof(A) == 4 ? 1 : 2) void decode_q8_split_kernel(Args x, int32_t* __restrict__ hdr, float* __restrict__ ws_o,
+                                                                                                          float* __restrict__ ws_ml, int pmax)
+{
+    extern __shared__ __attribute__((aligned(16))) float s_o[];           // [wave][head][D], then m and l [wave][head]
+    const AttnArgs& a = x.a;
+    const int B = a.batch, hkv = a.c.hkv, hq = a.hq, G = hq / hkv, D = kExact ? DT : a.c.d;
+    const int nb = blocks_of(G), pairs = hkv * nb, rows = min(G, kCols);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wg = blockIdx.x;
+    float* const s_m = s_o + kWaves * rows * D;
+    float* const s_l = s_m + kWaves * rows;
+
+    Share sh;
+    if (!find_share<true, kTok>(a.ctx_lens, B, pairs, hdr, sh)) return;
+    const int q = sh.q, f1 = sh.f1;
+    int s = sh.s, base = sh.base, ctx = sh.ctx, n = steps_of(ctx);
+    int pair = (sh.f0 - base) / n;
+    int u = (sh.f0 - base) - pair * n;
+    for (int f = sh.f0; f < f1 && s < B;) {               // one segment per pass; every value here is uniform
+        const int k = min(n - u, f1 - f);                 // steps of this segment
+        if (k <= 0) break;                                // (only if the lengths changed under the kernel: never spin)
+        const int per = (k + kWaves - 1) / kWaves;
+        const int g = pair / nb, h0 = (pair - g * nb) * kCols, nh = min(G - h0, kCols);
+        float m, lsum;
+        f32x4 o[DT / 16];
+        attend_steps<A, DT, kExact>(x, s, g, h0, nh, ctx, u + w * per, max(0, min(per, k - w * per)), lane, m, lsum, o);
+        lsum += __shfl_xor(lsum, 16);
+        lsum += __shfl_xor(lsum, 32);
+        const int r = lane & 15, c = lane >> 4;
+        if (r < nh) {
+#pragma unroll
+            for (int mb = 0; mb < DT / 16; ++mb)
+                if (kExact || mb * 16 < D) *reinterpret_cast<f32x4*>(s_o + (w * rows + r) * D + mb * 16 + c * 4) = o[mb];
+            if (c == 0) { s_m[w * rows + r] = m; s_l[w * rows + r] = lsum; }
+        }
+        __syncthreads();
+        // the pair starts at flat step base + pair n; its segments are numbered from the workgroup holding that step
+        const int piece = wg - (base + pair * n) / q;
+        if (piece < pmax) {
+            for (int idx = tid; idx < nh * (D / 4); idx += 64 * kWaves) {      // four channels a thread
+                const int head = idx / (D / 4), d = (idx - head * (D / 4)) * 4;
+                float ms = s_m[head];
+#pragma unroll
+                for (int ww = 1; ww < kWaves; ++ww) ms = fmaxf(ms, s_m[ww * rows + head]);
+                const float ref = ms == -INFINITY ? 0.f : ms;
+                float l = 0.f;
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ww = 0; ww < kWaves; ++ww) {
+                    const float fw = __builtin_amdgcn_exp2f(s_m[ww * rows + head] - ref);     // a wave without steps has m = -inf -> 0
+                    const f32x4 y = *reinterpret_cast<const f32x4*>(s_o + (ww * rows + head) * D + d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[e] += fw * y[e];
+                    l += fw * s_l[ww * rows + head];
+                }
+                const int64_t slot = ((int64_t)s * hq + (int64_t)g * G + h0 + head) * pmax + piece;
+                *reinterpret_cast<f32x4*>(ws_o + slot * D + d) = acc;
+                if (d == 0) { ws_ml[slot * 2] = ms; ws_ml[slot * 2 + 1] = l; }
+            }
+        }
+        __syncthreads();                                  // s_o is rewritten by the next segment
+        f += k;
+        u += k;
+        if (u == n) {                                     // on to the next pair
+            u = 0;
+            if (++pair == pairs) {
+                pair = 0;
+                base += pairs * n;
+                do {
+                    ++s;
+                    ctx = s < B ? a.ctx_lens[s] : 0;
+                    n = steps_of(ctx);
+                } while (s < B && n == 0);
+            }
+        }
+    }
+}
+
+// D / 4 lanes per (session, query head), `rows` of them a workgroup
+template <typename A>
+__global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int32_t* __restrict__ hdr, const float* __restrict__ ws_o,
+                                                              const float* __restrict__ ws_ml, int pmax, int rows)
+{
+    const AttnArgs& a = x.a;
+    const int D = a.c.d, G = a.hq / a.c.hkv, nb = blocks_of(G);
+    const int mine = threadIdx.x / (D / 4);
+    const int64_t row = (int64_t)blockIdx.x * rows + mine;             // s * hq + h
+    if (mine >= rows || row >= (int64_t)a.batch * a.hq) return;
+    const int s = (int)(row / a.hq), h = (int)(row - (int64_t)s * a.hq), d = (threadIdx.x - mine * (D / 4)) * 4;
+    const int ctx = a.ctx_lens[s];
+    A* out = (A*)a.out + row * D;
+    if (ctx <= 0) {
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        splitk::store_quad(out + d, zero);
+        return;
+    }
+    const int g = h / G, pair = g * nb + (h - g * G) / kCols;
+    const int q = max(1, hdr[0]), n = steps_of(ctx);
+    const int first = a.c.hkv * nb * hdr[1 + s] + pair * n;            // the pair's first flat step
+    const int pieces = min(pmax, (first + n - 1) / q - first / q + 1);
+    splitk::merge_quad<A>(ws_o, ws_ml, row * pmax, pieces, d, D, out);
+}
+
+template <typename A, int DT, bool kExact>
+ag_status launch(const Args& x, int32_t* hdr, float* ws_o, float* ws_ml, int pmax, int grid, hipStream_t st)
+{
+    const int rows = std::min(x.a.hq / x.a.c.hkv, kCols);
+    const size_t lds = lds_of(rows, x.a.c.d);
+    if (lds > 64 * 1024) {
+        static std::atomic<uint64_t> told{0};
+        ag_status e = allow_dynamic_lds((const void*)decode_q8_split_kernel<A, DT, kExact>, (int)lds_of(kCols, DT), told);
+        if (e) return e;
+    }
+    hipLaunchKernelGGL((decode_q8_split_kernel<A, DT, kExact>), dim3(grid), dim3(64 * kWaves), lds, st, x, hdr, ws_o, ws_ml, pmax);
+    return hip_check(hipGetLastError(), "decode split launch");
+}
+
+template <typename A>
+ag_status launch_typed(const Args& x, int32_t* hdr, float* ws_o, float* ws_ml, int pmax, int grid, hipStream_t st)
+{
+    const int d = x.a.c.d;
+    ag_status e = AG_OK;
+    if (grid > 0)
+        e = d == 64 ? launch<A, 64, true>(x, hdr, ws_o, ws_ml, pmax, grid, st) : d < 64 ? launch<A, 64, false>(x, hdr, ws_o, ws_ml, pmax, grid, st)
+          : d == 128 ? launch<A, 128, true>(x, hdr, ws_o, ws_ml, pmax, grid, st) : d < 128 ? launch<A, 128, false>(x, hdr, ws_o, ws_ml, pmax, grid, st)
+          : d == 256 ? launch<A, 256, true>(x, hdr, ws_o, ws_ml, pmax, grid, st) : launch<A, 256, false>(x, hdr, ws_o, ws_ml, pmax, grid, st);
+    if (e) return e;
+    const int rows = 256 / (d / 4);
+    hipLaunchKernelGGL(decode_q8_merge_kernel<A>, dim3((unsigned)(((int64_t)x.a.batch * x.a.hq + rows - 1) / rows)), dim3(256), 0, st, x, hdr, ws_o, ws_ml, pmax, rows);
+    return hip_check(hipGetLastError(), "decode merge launch");
+}
+
+}  // namespace
+
+size_t decode_workspace(int batch, int hq, int d, int max_ctx)
+{
+    return splitk::header_ints(batch) * sizeof(int32_t) + (size_t)batch * hq * splitk::pieces_max<kTok>(max_ctx) * (size_t)(d + 2) * sizeof(float);
+}
+
+ag_status launch_decode(const Args& x, void* ws, hipStream_t st)
+{
+    const AttnArgs& a = x.a;
+    const int pmax = splitk::pieces_max<kTok>(a.max_ctx);
+    int32_t* hdr = (int32_t*)ws;
+    float* ws_o = (float*)(hdr + splitk::header_ints(a.batch));
+    float* ws_ml = ws_o + (size_t)a.batch * a.hq * pmax * a.c.d;
+    // Upper bound of the step count from the host-known bounds: a share is at most kMaxSteps steps even if every session is max_ctx long.
+    const int64_t f_max = (int64_t)a.c.hkv * blocks_of(a.hq / a.c.hkv) * a.batch * ((a.max_ctx + (kTok - 1)) / kTok);
+    if (f_max > (1 << 30)) { set_error("decode batch of %lld steps of %d tokens is beyond one launch", (long long)f_max, kTok); return AG_ERR_INVALID_ARG; }
+    const int grid = a.max_ctx > 0 ? share_workgroups(f_max, st) : 0;
+    prof_before(st);
+    ag_status e = a.c.dtype == AG_BF16 ? launch_typed<__bf16>(x, hdr, ws_o, ws_ml, pmax, grid, st) : launch_typed<float>(x, hdr, ws_o, ws_ml, pmax, grid, st);
+    prof_after(st);
+    return e;
+}
+
+}  // namespace q8
+}  // namespace ag

@@ -158,10 +158,13 @@ constexpr int kMinSplit = 256;
 constexpr int kMinSteps = kMinSplit / 32;      // a workgroup's share is at least this many steps (256 tokens)
 constexpr int kMaxSteps = 128;                 // and at most this many (share_workgroups() sizes the grid for it)
 
-__device__ __forceinline__ int steps_of(int ctx) { return ctx > 0 ? (ctx + 31) >> 5 : 0; }
+// (kTok: the 8-bit cache's steps are of 64 tokens, as many bytes)
+template <int kTok = 32>
+__device__ __forceinline__ int steps_of(int ctx) { return ctx > 0 ? (int)((unsigned)(ctx + (kTok - 1)) / kTok) : 0; }
 
 // Segments a pair of n steps starting at flat step a may be cut into when shares are q >= kMinSteps steps.
-inline int pieces_max(int max_ctx) { return (((max_ctx + 31) / 32) - 1) / kMinSteps + 2; }
+template <int kTok = 32>
+inline int pieces_max(int max_ctx) { return (((max_ctx + (kTok - 1)) / kTok) - 1) / kMinSteps + 2; }
 // Workspace: header [q, then the exclusive step count before each session], partials O, partials (m, l).
 inline size_t header_ints(int batch) { return ((size_t)batch + 1 + 3) & ~(size_t)3; }
 
@@ -174,15 +177,15 @@ struct Share {
 // Finds this workgroup's share from the lengths (`heads` pairs per session); false if it has none.  Every wave scans the
 // lengths for itself, 64 sessions at a time: one memory round trip and no barrier for up to 64 sessions.
 // With kPublish workgroup 0 also writes the plan for the merge kernel: hdr[0] = q, hdr[1 + s] = steps before session s.
-template <bool kPublish>
+template <bool kPublish, int kTok = 32>
 __device__ __forceinline__ bool find_share(const int32_t* __restrict__ ctx_lens, int B, int heads, int32_t* __restrict__ hdr,
                                            Share& sh)
 {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wg = blockIdx.x, W = gridDim.x;
     int len = lane < B ? ctx_lens[lane] : 0;
-    int total = steps_of(len);
-    for (int s = lane + 64; s < B; s += 64) total += steps_of(ctx_lens[s]);
+    int total = steps_of<kTok>(len);
+    for (int s = lane + 64; s < B; s += 64) total += steps_of<kTok>(ctx_lens[s]);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
     const int F = heads * __builtin_amdgcn_readfirstlane(total);
@@ -198,7 +201,7 @@ __device__ __forceinline__ bool find_share(const int32_t* __restrict__ ctx_lens,
     int carry = 0;                      // steps of the sessions before this pass of 64
     for (int s0 = 0; s0 < B; s0 += 64) {
         if (s0 > 0) len = s0 + lane < B ? ctx_lens[s0 + lane] : 0;
-        const int n = steps_of(len);
+        const int n = steps_of<kTok>(len);
         int incl = n;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {

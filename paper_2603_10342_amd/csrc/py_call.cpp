@@ -9,8 +9,10 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "ag.h"
+#include "ag_q8.h"
 
 namespace {
 
@@ -22,12 +24,18 @@ struct Entries {
     decltype(&ag_attn_decode_static) attn_decode_static;
     decltype(&ag_decode_step) decode_step;
     decltype(&ag_attn_merged) attn_merged;
+    decltype(&ag_kv_append_q8) kv_append_q8;
+    decltype(&ag_kv_read_q8) kv_read_q8;
+    decltype(&ag_attn_prefill_q8) attn_prefill_q8;
+    decltype(&ag_attn_resume_q8) attn_resume_q8;
+    decltype(&ag_attn_decode_q8) attn_decode_q8;
 };
 Entries entries;
 PyObject* cache_type;           // binding.KVCache
+PyObject* cache_q8_type;        // binding.KVCacheQ8
 PyObject* get_device;           // torch._C._cuda_getDevice
 PyObject* get_raw_stream;       // torch._C._cuda_getCurrentRawStream
-PyObject *n_k_pool, *n_v_pool, *n_num_pages, *n_page_size, *n_num_kv_heads, *n_head_dim, *n_dtype, *n_cuda_stream;
+PyObject *n_k_pool, *n_v_pool, *n_exps, *n_num_pages, *n_page_size, *n_num_kv_heads, *n_head_dim, *n_dtype, *n_cuda_stream;
 
 // Reads arguments; `plain` becomes false at the first that is not for this path, and the rest is not looked at.
 struct Reader {
@@ -76,9 +84,19 @@ struct Reader {
         if (!plain || !PyFloat_CheckExact(o)) { plain = false; return 0.f; }
         return (float)PyFloat_AS_DOUBLE(o);
     }
-    void cache(PyObject* o, ag_kv_cache& c)
+    void cache(PyObject* o, ag_kv_cache& c) { pools(o, cache_type, c); }
+    void cache(PyObject* o, ag_kv_cache_q8& c)
     {
-        if (!plain || (PyObject*)Py_TYPE(o) != cache_type) { plain = false; return; }
+        pools(o, cache_q8_type, c);
+        PyObject* v = plain ? PyObject_GetAttr(o, n_exps) : nullptr;
+        if (!v) { PyErr_Clear(); plain = false; return; }
+        if (const at::Tensor* t = tensor(v)) c.exps = t->data_ptr();
+        Py_DECREF(v);
+    }
+    template <class Cache>
+    void pools(PyObject* o, PyObject* type, Cache& c)
+    {
+        if (!plain || (PyObject*)Py_TYPE(o) != type) { plain = false; return; }
         auto get = [&](PyObject* name, auto use) {
             PyObject* v = plain ? PyObject_GetAttr(o, name) : nullptr;
             if (!v) { PyErr_Clear(); plain = false; return; }
@@ -139,26 +157,29 @@ PyObject* finish(const Reader& r, Call call)
     return PyLong_FromLong(st);
 }
 
-PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n)
+// append and read-back: which entry point, over which cache
+template <class Cache, auto kEntry>
+PyObject* kv_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     return guarded(n, 9, [&] {
         Reader r;
-        ag_kv_cache c;
+        Cache c;
         const at::Tensor *bt, *lens;
         r.cache(a[0], c);
-        const void *k = r.device(a[1]), *v = r.device(a[2]);
+        void *k = r.device(a[1]), *v = r.device(a[2]);
         const int32_t *b = r.ints(a[3], &bt), *prefix = r.ints(a[4]), *len = r.ints(a[5], &lens), *cu = r.ints(a[6]);
         const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), total = r.number(a[7]);
         void* s = r.stream(a[8]);
-        return finish(r, [&] { return entries.kv_append(&c, k, v, b, pages, prefix, len, cu, batch, total, s); });
+        return finish(r, [&] { return (entries.*kEntry)(&c, k, v, b, pages, prefix, len, cu, batch, total, s); });
     });
 }
 
+template <class Cache, auto kEntry>
 PyObject* attn_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     return guarded(n, 11, [&] {
         Reader r;
-        ag_kv_cache c;
+        Cache c;
         const at::Tensor *bt, *lens;
         r.cache(a[0], c);
         void *q = r.device(a[1]), *out = r.device(a[2]);
@@ -166,17 +187,18 @@ PyObject* attn_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)
         const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), total = r.number(a[6]), max_new = r.number(a[7]), hq = r.number(a[8]);
         const float scale = r.real(a[9]);
         void* s = r.stream(a[10]);
-        return finish(r, [&] { return entries.attn_prefill(&c, q, out, b, pages, len, cu, batch, total, max_new, hq, scale, s); });
+        return finish(r, [&] { return (entries.*kEntry)(&c, q, out, b, pages, len, cu, batch, total, max_new, hq, scale, s); });
     });
 }
 
 // resume prefill, and the merged batch, which takes a workspace as well
-template <bool kMerged>
+template <class Cache, auto kEntry>
 PyObject* attn_resume(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
+    constexpr bool kMerged = std::is_same_v<decltype(kEntry), decltype(&Entries::attn_merged)>;
     return guarded(n, kMerged ? 14 : 13, [&] {
         Reader r;
-        ag_kv_cache c;
+        Cache c;
         const at::Tensor *bt, *lens, *ws = nullptr;
         r.cache(a[0], c);
         void *q = r.device(a[1]), *out = r.device(a[2]);
@@ -188,19 +210,20 @@ PyObject* attn_resume(PyObject*, PyObject* const* a, Py_ssize_t n)
         const size_t bytes = ws && r.plain ? (size_t)ws->numel() * ws->element_size() : 0;
         void* s = r.stream(a[n - 1]);
         return finish(r, [&] {
-            return kMerged ? entries.attn_merged(&c, q, out, b, pages, prefix, len, cu, batch, total, max_new, max_ctx, hq, scale, w, bytes, s)
-                           : entries.attn_resume(&c, q, out, b, pages, prefix, len, cu, batch, total, max_new, max_ctx, hq, scale, s);
+            if constexpr (kMerged) return (entries.*kEntry)(&c, q, out, b, pages, prefix, len, cu, batch, total, max_new, max_ctx, hq, scale, w, bytes, s);
+            else return (entries.*kEntry)(&c, q, out, b, pages, prefix, len, cu, batch, total, max_new, max_ctx, hq, scale, s);
         });
     });
 }
 
 // decode with the caller's workspace or the library's own
-template <bool kStatic>
+template <class Cache, auto kEntry>
 PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
+    constexpr bool kStatic = std::is_same_v<decltype(kEntry), decltype(&Entries::attn_decode_static)>;
     return guarded(n, kStatic ? 9 : 10, [&] {
         Reader r;
-        ag_kv_cache c;
+        Cache c;
         const at::Tensor *bt, *lens, *ws = nullptr;
         r.cache(a[0], c);
         void *q = r.device(a[1]), *out = r.device(a[2]);
@@ -211,8 +234,8 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n)
         const size_t bytes = ws && r.plain ? (size_t)ws->numel() * ws->element_size() : 0;
         void* s = r.stream(a[n - 1]);
         return finish(r, [&] {
-            return kStatic ? entries.attn_decode_static(&c, q, out, b, pages, ctx, batch, max_ctx, hq, scale, s)
-                           : entries.attn_decode(&c, q, out, b, pages, ctx, batch, max_ctx, hq, scale, w, bytes, s);
+            if constexpr (kStatic) return (entries.*kEntry)(&c, q, out, b, pages, ctx, batch, max_ctx, hq, scale, s);
+            else return (entries.*kEntry)(&c, q, out, b, pages, ctx, batch, max_ctx, hq, scale, w, bytes, s);
         });
     });
 }
@@ -235,31 +258,39 @@ PyObject* decode_step(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
-// setup(KVCache, _cuda_getDevice, _cuda_getCurrentRawStream, addresses of the entry points in the order of Entries)
+// setup(KVCache, KVCacheQ8, _cuda_getDevice, _cuda_getCurrentRawStream, addresses of the entry points in the order of Entries)
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     void** at = reinterpret_cast<void**>(&entries);
     constexpr Py_ssize_t kEntries = sizeof(Entries) / sizeof(void*);
-    if (n != 3 + kEntries) { PyErr_SetString(PyExc_TypeError, "setup: wrong number of arguments"); return nullptr; }
+    if (n != 4 + kEntries) { PyErr_SetString(PyExc_TypeError, "setup: wrong number of arguments"); return nullptr; }
     for (Py_ssize_t i = 0; i < kEntries; ++i) {
-        at[i] = PyLong_AsVoidPtr(a[3 + i]);
+        at[i] = PyLong_AsVoidPtr(a[4 + i]);
         if (PyErr_Occurred()) return nullptr;
     }
     Py_INCREF(a[0]);
     Py_INCREF(a[1]);
     Py_INCREF(a[2]);
+    Py_INCREF(a[3]);
     cache_type = a[0];
-    get_device = a[1];
-    get_raw_stream = a[2];
+    cache_q8_type = a[1];
+    get_device = a[2];
+    get_raw_stream = a[3];
     Py_RETURN_NONE;
 }
 
 #define AG_METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(+fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    AG_METHOD("setup", setup), AG_METHOD("kv_append", kv_append), AG_METHOD("attn_prefill", attn_prefill),
-    AG_METHOD("attn_resume", attn_resume<false>), AG_METHOD("attn_merged", attn_resume<true>),
-    AG_METHOD("attn_decode", attn_decode<false>), AG_METHOD("attn_decode_static", attn_decode<true>),
-    AG_METHOD("decode_step", decode_step), {nullptr, nullptr, 0, nullptr}};
+    AG_METHOD("setup", setup), AG_METHOD("kv_append", (kv_rows<ag_kv_cache, &Entries::kv_append>)),
+    AG_METHOD("attn_prefill", (attn_prefill<ag_kv_cache, &Entries::attn_prefill>)),
+    AG_METHOD("attn_resume", (attn_resume<ag_kv_cache, &Entries::attn_resume>)), AG_METHOD("attn_merged", (attn_resume<ag_kv_cache, &Entries::attn_merged>)),
+    AG_METHOD("attn_decode", (attn_decode<ag_kv_cache, &Entries::attn_decode>)),
+    AG_METHOD("attn_decode_static", (attn_decode<ag_kv_cache, &Entries::attn_decode_static>)),
+    AG_METHOD("decode_step", decode_step),
+    AG_METHOD("kv_append_q8", (kv_rows<ag_kv_cache_q8, &Entries::kv_append_q8>)), AG_METHOD("kv_read_q8", (kv_rows<ag_kv_cache_q8, &Entries::kv_read_q8>)),
+    AG_METHOD("attn_prefill_q8", (attn_prefill<ag_kv_cache_q8, &Entries::attn_prefill_q8>)),
+    AG_METHOD("attn_resume_q8", (attn_resume<ag_kv_cache_q8, &Entries::attn_resume_q8>)),
+    AG_METHOD("attn_decode_q8", (attn_decode<ag_kv_cache_q8, &Entries::attn_decode_q8>)), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "agcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -267,7 +298,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "agcall", nullptr, -1, methods, nul
 PyMODINIT_FUNC PyInit_agcall()
 {
     struct { PyObject** at; const char* name; } names[] = {
-        {&n_k_pool, "k_pool"}, {&n_v_pool, "v_pool"}, {&n_num_pages, "num_pages"}, {&n_page_size, "page_size"},
+        {&n_k_pool, "k_pool"}, {&n_v_pool, "v_pool"}, {&n_exps, "exps"}, {&n_num_pages, "num_pages"}, {&n_page_size, "page_size"},
         {&n_num_kv_heads, "num_kv_heads"}, {&n_head_dim, "head_dim"}, {&n_dtype, "dtype"}, {&n_cuda_stream, "cuda_stream"}};
     for (auto& x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.name))) return nullptr;

@@ -1,0 +1,91 @@
+// Internal declarations of the 8-bit cache (include/ag_q8.h): the host's view of it, the launchers, and the device's way between
+// e4m3 numbers and the types that arithmetic runs in.
+#pragma once
+
+#include "ag_internal.h"
+#include "ag_q8.h"
+
+namespace ag {
+namespace q8 {
+
+// An attention problem over an 8-bit cache: a.c holds the pools and the geometry, with the activations' type as its dtype.
+struct Args {
+    AttnArgs a;
+    const uint8_t* exps;
+};
+
+ag_status launch_append(const CacheView& c, uint8_t* exps, const void* k_new, const void* v_new, const int32_t* bt, int max_pages,
+                        const int32_t* prefix_lens, const int32_t* new_lens, const int32_t* cu_new, int batch, int total_new, hipStream_t st);
+ag_status launch_read(const CacheView& c, const uint8_t* exps, void* k_out, void* v_out, const int32_t* bt, int max_pages,
+                      const int32_t* prefix_lens, const int32_t* new_lens, const int32_t* cu_new, int batch, int total_new, hipStream_t st);
+size_t    decode_workspace(int batch, int hq, int d, int max_ctx);
+ag_status launch_decode(const Args& x, void* ws, hipStream_t st);
+ag_status launch_prefill(const Args& x, hipStream_t st);
+
+// Where a key's exponent byte stands in its group of 16 slots: the four that a lane of the score product needs are one word.
+__host__ __device__ inline int key_place(int slot) { return (slot & 3) * 4 + ((slot >> 2) & 3); }
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kExpLo = -110 + 127, kExpHi = 119 + 127;          // of the stored bytes
+
+// 2^(byte - 127)
+__device__ __forceinline__ float power(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+// Byte i of four words, as a power; a byte that is nobody's may be any, 255 (an infinity) included.
+__device__ __forceinline__ float power_of(const u32x4& bytes, int i) { return power((bytes[i >> 2] >> (8 * (i & 3))) & 0xFFu); }
+
+// |x| in bits, 0 for what is not finite: sizes compare as integers
+__device__ __forceinline__ uint32_t size_of(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu;
+    return u < 0x7F800000u ? u : 0u;
+}
+// The byte of a row whose largest size has these bits: 448 is 1.75 * 2^8, so a mantissa above 0.75 takes the next power.
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t most)
+{
+    return (uint32_t)min(max((int)((most + 0x1FFFFFu) >> 23) - 8, kExpLo), kExpHi);
+}
+// Four numbers as e4m3 under the row's power.  Only the largest power leaves numbers past 448 (they are cut to it); infinities become NaN.
+__device__ __forceinline__ uint32_t quantise4(float a, float b, float c, float d, uint32_t byte)
+{
+    const float inv = power(254 - byte);
+    float y[4] = {a * inv, b * inv, c * inv, d * inv};
+    if (byte == (uint32_t)kExpHi) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? fminf(fmaxf(y[i], -448.f), 448.f) : y[i];
+    }
+    uint32_t w = 0;
+    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], (int)w, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], (int)w, true);
+}
+
+// Eight e4m3 numbers times a power of two as bf16: exact, four instructions (as fast as an addition: 4 cycles a wave).
+__device__ __forceinline__ bf16x8 widen8(uint32_t w0, uint32_t w1, float scale)
+{
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true));
+    return __builtin_bit_cast(bf16x8, r);
+}
+// Two numbers of a word, each times a power of its own, as bf16: exact
+template <bool kHigh>
+__device__ __forceinline__ uint32_t widen_pair(uint32_t w, float s0, float s1)
+{
+    const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, kHigh);
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(x[0] * s0), (__bf16)(x[1] * s1)});
+}
+
+// Keeps the first `keep` bytes of a word (any `keep`), zeroes the others.
+__device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int keep)
+{
+    return keep >= 4 ? w : keep <= 0 ? 0u : w & ((1u << (8 * keep)) - 1u);
+}
+
+}  // namespace q8
+}  // namespace ag
