@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libagattn.so")
 CALL = os.path.join(HERE, "agcall.so")
 SOURCES = ["ag_api.hip", "kv_append.hip", "attn_general.hip", "attn_decode_mfma.hip", "attn_decode_any.hip", "attn_prefill_mfma.hip", "attn_prefill_any.hip", "attn_prefill_split.hip", "attn_prefill_f32.hip",
            "attn_merged_mfma.hip",
-           "ag_q8.hip", "kv_q8.hip", "attn_decode_q8.hip", "attn_prefill_q8.hip",
+           "ag_q8.hip", "kv_q8.hip", "attn_decode_q8.hip", "attn_prefill_q8.hip", "attn_split_q8.hip",
            "ag_sched.hip", "ag_pager.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-strict-aliasing", "-fvisibility=hidden",

@@ -19,7 +19,6 @@
 #include <type_traits>
 
 #include "attn_split_common.h"
-#include "bf16_terms.h"
 #include "q8_internal.h"
 
 namespace ag {
@@ -36,32 +35,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ int steps_of(int ctx) { return splitk::steps_of<kTok>(ctx); }
 __host__ __device__ inline int blocks_of(int G) { return (G + kCols - 1) / kCols; }
 
-// A number of the activations' type as kTerms bf16 terms: operands of the products
-template <typename A>
-constexpr int terms_of() { return sizeof(A) == 4 ? 3 : 1; }
-
-__device__ __forceinline__ void to_terms(const __bf16* p, bf16x8 (&t)[1]) { t[0] = *reinterpret_cast<const bf16x8*>(p); }
-__device__ __forceinline__ void to_terms(const float* p, bf16x8 (&t)[3])
-{
-    const Terms x = split8(*reinterpret_cast<const Four*>(p), *reinterpret_cast<const Four*>(p + 4));
-    t[0] = __builtin_bit_cast(bf16x8, x.h);
-    t[1] = __builtin_bit_cast(bf16x8, x.m);
-    t[2] = __builtin_bit_cast(bf16x8, x.l);
-}
-__device__ __forceinline__ void to_terms(const float (&w)[8], bf16x8 (&t)[1])
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t[0][i] = (__bf16)w[i];
-}
-__device__ __forceinline__ void to_terms(const float (&w)[8], bf16x8 (&t)[3])
-{
-    Terms x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.set_pair(i, w[2 * i], w[2 * i + 1]);
-    t[0] = __builtin_bit_cast(bf16x8, x.h);
-    t[1] = __builtin_bit_cast(bf16x8, x.m);
-    t[2] = __builtin_bit_cast(bf16x8, x.l);
-}
 // acc += a . (sum of b's terms), smallest terms first
 template <int kTerms>
 __device__ __forceinline__ f32x4 product(const bf16x8& a, const bf16x8 (&b)[kTerms], f32x4 acc)
@@ -70,8 +43,6 @@ __device__ __forceinline__ f32x4 product(const bf16x8& a, const bf16x8 (&b)[kTer
     for (int t = kTerms - 1; t >= 0; --t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[t], acc, 0, 0, 0);
     return acc;
 }
-
-__device__ __forceinline__ u32x4 stream16(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
 
 // One wave's part of a segment, steps u0 .. u0 + n - 1 of (session s, KV head g, heads h0 .. h0 + nh - 1 of its group): running maximum,
 // this lane's share of the sum, and O^T.  o[mb][i]: channel 16 mb + 4 c + i of head r, lane = 16 c + r.
@@ -100,10 +71,7 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
             for (int half = 0; half < 2; ++half) {
                 const int chunk = kExact ? 4 * h + c : min(4 * h + c, chunks - 1);
                 to_terms(row + chunk * 16 + half * 8, q[h][half]);
-                if (r >= nh || (!kExact && 4 * h + c >= chunks)) {
-#pragma unroll
-                    for (int t = 0; t < kTerms; ++t) q[h][half][t] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-                }
+                if (r >= nh || (!kExact && 4 * h + c >= chunks)) no_terms(q[h][half]);
             }
     }
 

@@ -7,8 +7,10 @@
 // its bytes go through registers, one tile ahead, and are written as bf16 numbers, their powers of two multiplied in (exactly).
 // Done once a workgroup that is an eighth (NW = 8) of what a conversion behind LDS would cost each wave, and the products run as
 // they do over a bf16 cache.  A wave brings one 16-token group of the tile (or half of one): one page id, 16 exponent bytes.
-//   iteration t: K(t + 1) and V(t) from registers into LDS; K(t + 2) and V(t + 1) requested; S(t) = K(t) Q^T; P(t) side by side with
-//   O += V(t - 1) P(t - 1); barrier.
+//   iteration t: K(t + 2) and V(t + 1) requested into registers; S(t) = K(t) Q^T, and between its products K(t + 1) and V(t), which are
+//   in registers, converted and written to LDS; P(t) side by side with O += V(t - 1) P(t - 1); barrier.
+// The conversions - 40 vector instructions a wave and tile at NW = 8 and 128 channels, beside 100 of the softmax - so run while the vector units
+// have nothing else; ahead of the products eight prompts of 4096 tokens took 1222 us, so 1134 (970 TFLOP/s; over a bf16 cache 1120).
 // bf16 activations: weights rounded to bf16 for the value product; fp32: queries and weights as three bf16 terms.
 #include <algorithm>
 #include <atomic>
@@ -26,23 +28,13 @@ using tile32::Weights;
 using tile32::f32x16;
 using tile32::tile_bytes;
 
-template <typename A>
-constexpr int terms_of() { return sizeof(A) == 4 ? 3 : 1; }
 // two key and two value tiles
 constexpr int lds_bytes(int dt) { return 4 * tile_bytes(dt); }
 
-__device__ __forceinline__ void query_terms(const __bf16* p, bf16x8 (&t)[1]) { t[0] = *reinterpret_cast<const bf16x8*>(p); }
-__device__ __forceinline__ void query_terms(const float* p, bf16x8 (&t)[3])
-{
-    const Terms x = split8(*reinterpret_cast<const Four*>(p), *reinterpret_cast<const Four*>(p + 4));
-    t[0] = __builtin_bit_cast(bf16x8, x.h);
-    t[1] = __builtin_bit_cast(bf16x8, x.m);
-    t[2] = __builtin_bit_cast(bf16x8, x.l);
-}
-
-// S^T tile = K tile . Q^T with queries in terms, smallest first (one term: tile32::qk_tile)
-template <int DT, int kTerms>
-__device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q)[DT / 16][kTerms], f32x16 (&sc)[2])
+// S^T tile = K tile . Q^T with queries in terms, smallest first.  Vector units have nothing to do meanwhile: between(i) of DT / 8
+// runs behind product i.
+template <int DT, int kTerms, class Between>
+__device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q)[DT / 16][kTerms], f32x16 (&sc)[2], Between between)
 {
     constexpr int kAhead = tile32::kOperandsAhead, kN = DT / 8;
     bf16x8 opnd[kAhead + 1];
@@ -56,6 +48,7 @@ __device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q
 #pragma unroll
         for (int t = kTerms - 1; t >= 0; --t)
             sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opnd[i % (kAhead + 1)], q[i >> 1][t], i < 2 && t == kTerms - 1 ? zero : sc[i & 1], 0, 0, 0);
+        between(i);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -116,84 +109,75 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
     const int64_t row = ((int64_t)row0 + token) * hq + (int64_t)g * G + head;
 
     // ---- tile requests: this wave's group of the tile, 16 keys; pieces [chunk][key] of the keys, [channel] of the values ----
-    typedef const __attribute__((address_space(4))) int32_t* cptr_t;
-    const cptr_t bt = (cptr_t)(uintptr_t)(a.bt + (int64_t)s * a.max_pages);
     const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
     const int64_t block = (int64_t)D * ps;                                    // bytes of one (page, head)
     const int my_grp = w / kWavesPerGroup, piece0 = (w % kWavesPerGroup) * kPer * 64 + lane;
     const int key = lane & 15;                                                // of the group, in every piece of a lane
     const uint8_t* const kpool = (const uint8_t*)a.c.k;
     const uint8_t* const vpool = (const uint8_t*)a.c.v;
-    u32x4 kr[kPer], vr[kPer], ve = {0, 0, 0, 0};
-    uint32_t ke = 0;
-    auto page_of = [&](int t) { return bt[min(t * 4 + my_grp, last_grp) >> gshift]; };
-    auto request_k = [&](int t, int page) {
+    // Page ids of 64 groups, 16 tiles, a lane each, and of the next 64: everything that is in flight in the loop is a vector load, as a
+    // scalar one shares its counter with the LDS operands and turns every wait for one of them into a wait for all.
+    auto ids_of = [&](int win) { return a.bt[(int64_t)s * a.max_pages + (min(win * 64 + lane, last_grp) >> gshift)]; };
+    int ids = ids_of(0), next_ids = ids_of(1);
+    struct Raw { u32x4 k[kPer], v[kPer]; uint32_t ke, ve; };                  // ke: this lane's key's byte; ve: word lane & 3 of the values' 16
+    // (uniform bases and 32-bit offsets of the lanes, the same for every tile: four 64-bit addresses kept in registers made the loop spill)
+    const uint32_t k_off = (uint32_t)((key >> 2) * chunks * 64 + (key & 3) * 16 + (piece0 >> 4) * 64), v_off = (uint32_t)(piece0 * 16);
+    const uint32_t ke_off = (uint32_t)key_place(key), ve_off = (uint32_t)(ps + (lane & 3) * 4);
+    auto request_k = [&](int t, int page, Raw& x8) {
         const int gi = min(t * 4 + my_grp, last_grp) & gmask;
         const int64_t at = (int64_t)page * hkv + g;
-        const uint8_t* kp = kpool + at * block + gi * 16 * D + (key >> 2) * chunks * 64 + (key & 3) * 16;
+        const uint8_t* kp = kpool + at * block + gi * 16 * D;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int chunk = (piece0 + i * 64) >> 4;
-            kr[i] = u32x4{0, 0, 0, 0};
-            if (kExact || chunk < chunks) kr[i] = *reinterpret_cast<const u32x4*>(kp + chunk * 64);
+            x8.k[i] = u32x4{0, 0, 0, 0};
+            if (kExact || (piece0 >> 4) + i * 4 < chunks) x8.k[i] = *reinterpret_cast<const u32x4*>(kp + (k_off + i * 256));
         }
-        ke = x.exps[at * (2 * ps) + gi * 16 + key_place(key)];
+        x8.ke = (x.exps + at * (2 * ps) + gi * 16)[ke_off];
     };
-    auto request_v = [&](int t, int page) {
+    auto request_v = [&](int t, int page, Raw& x8) {
         const int gi = min(t * 4 + my_grp, last_grp) & gmask;
         const int64_t at = (int64_t)page * hkv + g;
         const uint8_t* vp = vpool + at * block + gi * 16 * D;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int ch = piece0 + i * 64;
-            vr[i] = u32x4{0, 0, 0, 0};
-            if (kExact || ch < D) vr[i] = *reinterpret_cast<const u32x4*>(vp + ch * 16);
+            x8.v[i] = u32x4{0, 0, 0, 0};
+            if (kExact || piece0 + i * 64 < D) x8.v[i] = *reinterpret_cast<const u32x4*>(vp + (v_off + i * 1024));
         }
-        ve = *reinterpret_cast<const u32x4*>(x.exps + at * (2 * ps) + ps + gi * 16);
+        x8.ve = *reinterpret_cast<const uint32_t*>(x.exps + at * (2 * ps) + gi * 16 + ve_off);
     };
-    // into LDS as bf16: K [chunk of 8 channels][64 keys], V [chunk of 8 keys][channel], 16-byte pieces
-    auto put_k = [&](int t) {
-        unsigned char* dst = lds + (t & 1) * kTile + (my_grp * 16 + key) * 16;
-        const float scale = power(ke);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int chunk = (piece0 + i * 64) >> 4;
-            *reinterpret_cast<bf16x8*>(dst + chunk * 2048) = widen8(kr[i][0], kr[i][1], scale);
-            *reinterpret_cast<bf16x8*>(dst + chunk * 2048 + 1024) = widen8(kr[i][2], kr[i][3], scale);
-        }
-    };
-    auto put_v = [&](int t) {
-        unsigned char* dst = lds + (2 + (t & 1)) * kTile + my_grp * (DT * 32);
+    // Into LDS as bf16: K [chunk of 8 channels][64 keys], V [chunk of 8 keys][channel], 16-byte pieces, in kUnits steps of about four
+    // instructions: of every piece the two halves of its keys, then the eight pairs of its values.
+    constexpr int kUnits = 10 * kPer;
+    unsigned char* const k_put = lds + (my_grp * 16 + key) * 16;
+    unsigned char* const v_put = lds + 2 * kTile + my_grp * (DT * 32);
+    struct Put { float e[16]; u32x4 y; };                                     // the values' powers, a piece in the making
+    auto begin_put = [&](int t, Raw& x8, Put& p) {
         const int keep = ctx - (t * BN + my_grp * 16);       // slots behind the last token may hold anything, NaN included: zeros
-        float e[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] = power_of(ve, i);
         if (keep < 16) {                                     // uniform
-#pragma unroll
-            for (int i = 0; i < 16; ++i) e[i] = i < keep ? e[i] : 0.f;
+            asm volatile("");                                // (a branch, not a select for every word)
+            x8.ve = keep_bytes(x8.ve, keep - 4 * (lane & 3));            // (a byte of zero is a power of zero: a stale one may be an infinity)
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) vr[i][k] = keep_bytes(vr[i][k], keep - 4 * k);
+                for (int k = 0; k < 4; ++k) x8.v[i][k] = keep_bytes(x8.v[i][k], keep - 4 * k);
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int ch = piece0 + i * 64;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {           // slots half * 4 + {0..3} and 8 + half * 4 + {0..3}
-                u32x4 y;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int o = half * 4 + k * 8;
-                    y[2 * k] = widen_pair<false>(vr[i][half + 2 * k], e[o], e[o + 1]);
-                    y[2 * k + 1] = widen_pair<true>(vr[i][half + 2 * k], e[o + 2], e[o + 3]);
-                }
-                *reinterpret_cast<u32x4*>(dst + half * (DT * 16) + ch * 16) = y;
-            }
+        for (int i = 0; i < 16; ++i) p.e[i] = power(((uint32_t)__builtin_amdgcn_readlane((int)x8.ve, i >> 2) >> (8 * (i & 3))) & 0xFFu);
+    };
+    auto put_unit = [&](int unit, int t, const Raw& x8, Put& p) {             // keys of tile t + 1, values of tile t
+        const int i = unit / 10, u = unit % 10;
+        if (u < 2) {
+            const int chunk = (piece0 + i * 64) >> 4;
+            *reinterpret_cast<bf16x8*>(k_put + ((t + 1) & 1) * kTile + chunk * 2048 + u * 1024) = widen8(x8.k[i][2 * u], x8.k[i][2 * u + 1], power(x8.ke));
+        } else {                                             // half: slots half * 4 + {0..3} and 8 + half * 4 + {0..3}
+            const int half = (u - 2) >> 2, pair = (u - 2) & 3, word = half + (pair & 2), o = word * 4 + (pair & 1) * 2;
+            p.y[pair] = pair & 1 ? widen_pair<true>(x8.v[i][word], p.e[o], p.e[o + 1]) : widen_pair<false>(x8.v[i][word], p.e[o], p.e[o + 1]);
+            if (pair == 3) *reinterpret_cast<u32x4*>(v_put + (t & 1) * kTile + half * (DT * 16) + (piece0 + i * 64) * 16) = p.y;
         }
     };
 
-    request_k(0, page_of(0));
+    Raw ra, rb;
+    request_k(0, __builtin_amdgcn_readlane(ids, my_grp), rb);
 
     // ---- Q^T as B operand: column n, k-step ks covers channels ks * 16 + hi * 8 .. + 7 ----
     bf16x8 qf[DT / 16][kTerms];
@@ -201,12 +185,8 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
         const A* qp = (const A*)a.q + row * D + hi * 8;
 #pragma unroll
         for (int ks = 0; ks < DT / 16; ++ks) {
-            if (kExact || ks < chunks) {
-                query_terms(qp + ks * 16, qf[ks]);
-            } else {
-#pragma unroll
-                for (int t = 0; t < kTerms; ++t) qf[ks][t] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-            }
+            if (kExact || ks < chunks) to_terms(qp + ks * 16, qf[ks]);
+            else no_terms(qf[ks]);
         }
     }
     const float sl2 = a.scale * tile32::kLog2e;
@@ -217,27 +197,44 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[mb][i] = 0.f;
 
-    put_k(0);
-    request_v(0, page_of(0));
-    request_k(min(1, n_tiles - 1), page_of(min(1, n_tiles - 1)));
+    // what iteration 0 finds: K(0) in LDS, K(1) and V(0) on their way; tile t's page is that of K(t) now and of V(t) an iteration later
+    int page = __builtin_amdgcn_readlane(ids, my_grp);
+    request_v(0, page, ra);
+    page = __builtin_amdgcn_readlane(ids, min(4, 4 * (n_tiles - 1)) + my_grp);
+    request_k(min(1, n_tiles - 1), page, ra);
+    {
+        Put none;
+#pragma unroll
+        for (int unit = 0; unit < kUnits; ++unit)
+            if (unit % 10 < 2) put_unit(unit, -1, rb, none);
+    }
     __syncthreads();
 
     const unsigned char* const k_lane = lds + n * 16 + hi * 1024;
     const unsigned char* const v_lane = lds + 2 * kTile + n * 16 + hi * (DT * 16);
-    f32x16 sc[2];
     Weights<kLo> pa, pb;
     // Requests past the last tile repeat it; what they bring is written to a place that nobody reads.
-    auto iter = [&](int t, Weights<kLo>& p_prev, Weights<kLo>& p_cur) {
-        put_k(t + 1);
-        put_v(t);
-        const int tk = min(t + 2, n_tiles - 1), tv = min(t + 1, n_tiles - 1);
-        request_k(tk, page_of(tk));
-        request_v(tv, page_of(tv));
+    auto iter = [&](int t, Weights<kLo>& p_prev, Weights<kLo>& p_cur, Raw& now, Raw& next) {
+        const int tk = min(t + 2, n_tiles - 1);
+        request_v(min(t + 1, n_tiles - 1), page, next);
+        if (((t + 2) & 15) == 0) {                                            // K(t + 2) is the next window's first
+            ids = next_ids;
+            next_ids = ids_of(((t + 2) >> 4) + 1);
+        }
+        if (t + 2 < n_tiles) page = __builtin_amdgcn_readlane(ids, (tk & 15) * 4 + my_grp);
+        request_k(tk, page, next);
         const bool do_sm = t < wave_tiles, do_pv = t >= 1 && t - 1 < wave_tiles;
         const unsigned char* kb = k_lane + (t & 1) * kTile;
         const unsigned char* vb = v_lane + ((t + 1) & 1) * kTile;             // V(t - 1)
+        Put put;
+        f32x16 sc[2];
+        begin_put(t, now, put);
         if (do_sm) {
-            scores<DT, kTerms>(kb, qf, sc);
+            constexpr int kSteps = DT / 8;
+            scores<DT, kTerms>(kb, qf, sc, [&](int i) {
+#pragma unroll
+                for (int unit = i * kUnits / kSteps; unit < (i + 1) * kUnits / kSteps; ++unit) put_unit(unit, t, now, put);
+            });
             if (t >= first_masked) {                                          // the tile straddles this wave's diagonal
                 const int kbase = t * BN + hi * 4;
 #pragma unroll
@@ -248,6 +245,11 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
                         sc[b][i] = at <= qpos ? sc[b][i] : -INFINITY;
                     }
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) asm volatile("" : "+v"(now.k[i]), "+v"(now.v[i]));      // (else this is done ahead of the branch, for both sides)
+#pragma unroll
+            for (int unit = 0; unit < kUnits; ++unit) put_unit(unit, t, now, put);
         }
         if constexpr (DT > 128) softmax_after_value_product<DT, kLo>(do_sm, do_pv, vb, sc, sl2, m, lsum, p_prev, p_cur, o);
         else tile32::softmax_and_value_product<DT, kLo>(do_sm, do_pv, vb, sc, sl2, m, lsum, p_prev, p_cur, o);
@@ -255,8 +257,8 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
     };
 #pragma unroll 1
     for (int t = 0; t <= n_tiles; t += 2) {
-        iter(t, pb, pa);
-        if (t + 1 <= n_tiles) iter(t + 1, pa, pb);
+        iter(t, pb, pa, ra, rb);
+        if (t + 1 <= n_tiles) iter(t + 1, pa, pb, rb, ra);
     }
 
     // o[mb][q4 * 4 + e] is O^T[channel mb * 32 + q4 * 8 + hi * 4 + e][column n]
@@ -307,10 +309,38 @@ ag_status launch(const Args& x, hipStream_t st)
     return hip_check(hipGetLastError(), "prefill launch");
 }
 
+// Few rows on long contexts: the keys of 32 columns dealt to the waves of a workgroup (attn_split_q8.hip) instead of whole tiles, each a chain
+// of all of them.  Both chains grow with the context, that of tiles 3.5 times as fast (fp32: 4.2); a launch is as long as a chain, or as
+// many as a CU's workgroups come to.  Graph replay, 32 / 8 heads x 128 unless said otherwise, tiles -> split, us (workgroups of 32 columns): one chunk on
+// 6007 tokens of 50 rows (56) 128 -> 34.5, 211 (216) 133 -> 40, 600 (600) 142 -> 106, 1000 (1000) 150 -> 152; on 2000 of 211 51 -> 18.6, 1000 72 -> 75;
+// 16 of 30 on 600 (512) 20.9 -> 17.7; 8 of 50..300 on 2000..4000 (1328) 105 -> 124, x 256 on 500..1000 91 -> 101, x 64 74 -> 73; 4 prompts of 100 (416)
+// 9.8 -> 9.7, 16 of 50 (896) 9.3 -> 17.4, one of 1000 (1000) 29 -> 31; fp32: 211 on 6007 235 -> 79, x 64 6 of 20..300 on 100..2000 (784) 55 -> 45, 8 prompts of 300..1500
+// (8000) 266 -> 373.
+bool split_preferred(const AttnArgs& a, hipStream_t st)
+{
+    const bool wide = a.c.d > 128 || a.c.dtype == AG_F32;
+    const double cus = stream_cus(st), heads = a.c.hkv, ctx = a.max_ctx;
+    const double chains = std::max(1.0, heads * (double)tiles_bound(a, 32) / (cus * (a.c.d <= 64 && !wide ? 2 : 1)));       // workgroups of eight waves, or four of up to 512 registers
+    const double tiles = std::max(1.0, heads * (double)tiles_bound(a, 128) / (cus * (wide ? 1 : 2)));
+    return chains * (1200 + ctx) < tiles * (600 + ctx) * (a.c.dtype == AG_F32 ? 4.2 : 3.5);
+}
+
+// 256 columns a workgroup, bf16 x 128: a tile is brought in for twice the columns, but a launch ends on longer chains.  Where the context is
+// long, and there are workgroups for two a CU, or one and chunks that are alike beside their contexts.  Graph replay, 128 -> 256 columns, us (of the larger a
+// CU): eight prompts of 4096 (16) 1203 -> 1134, 32 chunks of 128..1024 on 2048..8192 (9.5) 1931 -> 1874, of 100..200 on 2000..4000 (2.6) 294 -> 281, two
+// of 1000 on 2000 (1) 101 -> 93; but one prompt of 2048 (1) 58 -> 64, eight of 512 (2) 43 -> 48, 64 of 600 (19) 353 -> 380, 16 of 1500 (12) 383 -> 389, one chunk of 1000
+// on 6007 (0.5) 150 -> 189.
+bool wide_workgroups(const AttnArgs& a, hipStream_t st)
+{
+    const int64_t cus = stream_cus(st), large = a.c.hkv * tiles_bound(a, 256), ctx = a.max_ctx;
+    return ctx > 1536 && (large >= 2 * cus || (large >= cus && ctx >= 2 * (int64_t)a.max_new));
+}
+
 template <typename A>
 ag_status launch_typed(const Args& x, hipStream_t st)
 {
     const int d = x.a.c.d;
+    if (sizeof(A) == 2 && d == 128 && wide_workgroups(x.a, st)) return launch<__bf16, 8, 128, true>(x, st);
     return d == 64 ? launch<A, 4, 64, true>(x, st) : d < 64 ? launch<A, 4, 64, false>(x, st)
          : d == 128 ? launch<A, 4, 128, true>(x, st) : d < 128 ? launch<A, 4, 128, false>(x, st)
          : d == 256 ? launch<A, 4, 256, true>(x, st) : launch<A, 4, 256, false>(x, st);
@@ -320,6 +350,7 @@ ag_status launch_typed(const Args& x, hipStream_t st)
 
 ag_status launch_prefill(const Args& x, hipStream_t st)
 {
+    if (split_preferred(x.a, st)) return launch_prefill_split(x, st);
     return x.a.c.dtype == AG_BF16 ? launch_typed<__bf16>(x, st) : launch_typed<float>(x, st);
 }
 

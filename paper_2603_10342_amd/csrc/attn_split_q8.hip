@@ -1,0 +1,288 @@
+// Prefill of few rows over the 8-bit paged KV cache: the keys of 32 columns - (token, query head of the group) pairs of one (session, KV
+// head) - are dealt to the waves of one workgroup, whose sums meet in LDS.
+//
+// A chunk of a few hundred rows on a long context makes few workgroups of whole tiles, each a chain of as many key tiles as the context has
+// (attn_prefill_q8.hip).  Here a chain is a W-th of that.  No wave shares a tile with another, so nothing goes through LDS: keys
+// and values come from the pools straight into the operands of 32x32x16 bf16 products, converted in registers.  A step of a wave is 32
+// keys, two 16-token groups:
+//   scores  S^T[key][column]: row n is slot 4 (n / 8) + n % 4 of group (n / 4) % 2, so that a lane ends up with the 16 slots of group
+//           hi = lane / 32, which are the 16 bytes that a load of the value pool holds of a channel; a key's power goes in with the conversion
+//   values  O^T[channel][column] += V^T . P^T: slots 0..7 and 8..15 of the lane's group; a value's power is multiplied into its weight
+// The next step's keys are requested when the scores have taken this one's, its values when the value product has.
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "q8_internal.h"
+#include "tile_list.h"
+
+namespace ag {
+namespace q8 {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kTok = 32;                // keys of a step
+constexpr int kCols = 32;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.0f;          // a reference maximum may be outgrown by 2^8 before O is rescaled
+
+template <int kTerms>
+__device__ __forceinline__ f32x16 product(const bf16x8& a, const bf16x8 (&b)[kTerms], f32x16 acc)
+{
+#pragma unroll
+    for (int t = kTerms - 1; t >= 0; --t) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[t], acc, 0, 0, 0);
+    return acc;
+}
+
+// Waves of a workgroup: eight, two a SIMD, where queries, O and a step's operands fit 256 registers.
+template <typename A>
+constexpr int waves_of(int dt) { return dt > 128 || (dt > 64 && sizeof(A) == 4) ? 4 : 8; }
+// per wave O, and m and l per column
+constexpr int lds_bytes(int waves, int dt) { return waves * (kCols * dt * 4 + 2 * kCols * 4); }
+
+template <typename A, int DT, bool kExact>
+__global__ __launch_bounds__(64 * waves_of<A>(DT), waves_of<A>(DT) / 4) void prefill_q8_split_kernel(Args x, Deal deal)
+{
+    constexpr int W = waves_of<A>(DT), kTerms = terms_of<A>(), kK = DT / 32, kV = DT / 32;      // 16-byte loads of a lane for a step's keys, and for its values
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const AttnArgs& a = x.a;
+    const int hkv = a.c.hkv, hq = a.hq, G = hq / hkv, D = kExact ? DT : a.c.d, ps = a.c.ps, chunks = D >> 4;
+    int g, j;
+    if (!place_of(deal, hkv, g, j)) return;
+    int s = -1, qt = 0, N = 0, P = 0, row0 = 0;
+    find_tile<kCols>(a, j, G, s, qt, N, P, row0);
+    if (s < 0) return;                              // beyond the batch's tiles
+    const int ctx = P + N;
+    const int col0 = qt * kCols, cols = min(N * G - col0, kCols);
+    const Columns columns(col0, G);
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hi = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = min(n, cols - 1);                                         // columns beyond the tile repeat the last one
+    const int token = columns.token(col), head = columns.head(col, token), qpos = P + token;
+    const int64_t row = ((int64_t)row0 + token) * hq + (int64_t)g * G + head;
+    const int steps = (P + columns.token(cols - 1)) / kTok + 1;               // of the workgroup
+    const int per = (steps + W - 1) / W, u0 = w * per, my_n = max(0, min(per, steps - u0));
+    const int first_masked = (P + columns.token(0) + 1) / kTok;               // first step holding a key that the first column may not see
+
+    float m = -INFINITY, lsum = 0.f;
+    f32x16 o[kV];
+#pragma unroll
+    for (int mb = 0; mb < kV; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[mb][i] = 0.f;
+
+    if (my_n > 0) {
+        typedef const __attribute__((address_space(4))) int32_t* cptr_t;
+        const cptr_t bt = (cptr_t)(uintptr_t)(a.bt + (int64_t)s * a.max_pages);
+        const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
+        const int64_t block = (int64_t)D * ps;                                // bytes of one (page, head)
+        const uint8_t* const kpool = (const uint8_t*)a.c.k;
+        const uint8_t* const vpool = (const uint8_t*)a.c.v;
+        const int kg = (n >> 2) & 1;                                          // this lane's group of the keys
+        struct Pages { int a, b; };
+        auto pages_of = [&](int st) {
+            const int grp = 2 * (u0 + st);
+            return Pages{bt[min(grp, last_grp) >> gshift], bt[min(grp + 1, last_grp) >> gshift]};
+        };
+        // columns' queries as B operands: k-step (i, half) covers channels (2 i + hi) * 16 + half * 8 .. + 7
+        bf16x8 q[kK][2][kTerms];
+        {
+            const A* qp = (const A*)a.q + row * D;
+#pragma unroll
+            for (int i = 0; i < kK; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int chunk = 2 * i + hi;
+                    if (kExact || chunk < chunks) to_terms(qp + chunk * 16 + half * 8, q[i][half]);
+                    else no_terms(q[i][half]);
+                }
+        }
+        u32x4 k[kK], v[kV], ve;
+        uint32_t ke;
+        const uint32_t k_off = (uint32_t)((n >> 3) * chunks * 64 + (n & 3) * 16), ke_off = (uint32_t)((n & 3) * 4 + (n >> 3));
+        auto load_k = [&](int st, Pages p) {
+            const int gi = min(2 * (u0 + st) + kg, last_grp) & gmask;
+            const int64_t at = (int64_t)(kg ? p.b : p.a) * hkv + g;
+            const uint8_t* kp = kpool + at * block + gi * 16 * D + k_off;
+#pragma unroll
+            for (int i = 0; i < kK; ++i) {
+                const int chunk = kExact ? 2 * i + hi : min(2 * i + hi, chunks - 1);     // (beyond: times zeros of the query)
+                k[i] = *reinterpret_cast<const u32x4*>(kp + chunk * 64);
+            }
+            ke = (x.exps + at * (2 * ps) + gi * 16)[ke_off];
+        };
+        auto load_v = [&](int st, Pages p) {
+            const int gi = min(2 * (u0 + st) + hi, last_grp) & gmask;
+            const int64_t at = (int64_t)(hi ? p.b : p.a) * hkv + g;
+            const uint8_t* vp = vpool + at * block + gi * 16 * D;
+#pragma unroll
+            for (int mb = 0; mb < kV; ++mb) v[mb] = *reinterpret_cast<const u32x4*>(vp + (kExact ? mb * 32 + n : min(mb * 32 + n, D - 1)) * 16);
+            ve = *reinterpret_cast<const u32x4*>(x.exps + at * (2 * ps) + ps + gi * 16);
+        };
+        const float sl2 = a.scale * kLog2e;
+        Pages pg = pages_of(0);
+        load_k(0, pg);
+        load_v(0, pg);
+        pg = pages_of(1);
+        __builtin_amdgcn_sched_barrier(0);
+        // (past the wave's last step the requests run on: clamped to the context, never used)
+#pragma unroll 1
+        for (int st = 0; st < my_n; ++st) {
+            f32x16 sc;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+            const float scale = power(ke);
+#pragma unroll
+            for (int i = 0; i < kK; ++i) {
+                sc = product(widen8(k[i][0], k[i][1], scale), q[i][0], sc);
+                sc = product(widen8(k[i][2], k[i][3], scale), q[i][1], sc);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(st + 1, pg);
+            __builtin_amdgcn_sched_barrier(0);
+            // sc[i]: slot i of group hi
+            const int tok0 = (u0 + st) * kTok + hi * 16;
+            if (u0 + st >= first_masked) {
+                asm volatile("");                            // (a branch)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[i] = tok0 + i <= qpos ? sc[i] : -INFINITY;
+                // slots behind the last token may hold anything, NaN included: zeros, under powers of zero
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ve[i] = keep_bytes(ve[i], ctx - tok0 - 4 * i);
+#pragma unroll
+                for (int mb = 0; mb < kV; ++mb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[mb][i] = keep_bytes(v[mb][i], ctx - tok0 - 4 * i);
+            }
+            float mx = sc[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+            mx *= sl2;                                       // scale > 0: max and scaling commute
+            // m is shared by the two lanes of a column: if either lane's own maximum outgrew it, combine them
+            if (__builtin_amdgcn_ballot_w64(mx > m + kSlack) != 0) {
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float m_new = fmaxf(m, mx);
+                const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+                lsum *= alpha;
+#pragma unroll
+                for (int mb = 0; mb < kV; ++mb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[mb][i] *= alpha;
+                m = m_new;
+            }
+            const float m_ref = m == -INFINITY ? 0.f : m;
+            float psum = 0.f;
+            bf16x8 wt[2][kTerms];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(fmaf(sc[half * 8 + i], sl2, -m_ref));
+                    psum += p[i];
+                    p[i] *= power_of(ve, half * 8 + i);
+                }
+                to_terms(p, wt[half]);
+            }
+            lsum += psum;
+#pragma unroll
+            for (int mb = 0; mb < kV; ++mb) {
+                o[mb] = product(widen8(v[mb][0], v[mb][1], 1.f), wt[0], o[mb]);
+                o[mb] = product(widen8(v[mb][2], v[mb][3], 1.f), wt[1], o[mb]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(st + 1, pg);
+            pg = pages_of(st + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    lsum += __shfl_xor(lsum, 32);
+
+    // the waves' sums, lane by lane: O as quads of channels [wave][quad][lane], then m and l [wave][column]
+    f32x4* const part = reinterpret_cast<f32x4*>(lds);
+    float* const s_m = reinterpret_cast<float*>(lds + W * kCols * DT * 4);
+    float* const s_l = s_m + W * kCols;
+    constexpr int kQuads = DT / 8;
+#pragma unroll
+    for (int i = 0; i < kQuads; ++i) {
+        const int b = (i & 3) * 4;
+        part[(w * kQuads + i) * 64 + lane] = f32x4{o[i >> 2][b], o[i >> 2][b + 1], o[i >> 2][b + 2], o[i >> 2][b + 3]};
+    }
+    if (hi == 0) { s_m[w * kCols + n] = m; s_l[w * kCols + n] = lsum; }
+    __syncthreads();
+    float f[W], top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) top = fmaxf(top, s_m[i * kCols + n]);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        f[i] = __builtin_amdgcn_exp2f(s_m[i * kCols + n] - ref);              // a wave that saw no key has m = -inf -> 0
+        l += f[i] * s_l[i * kCols + n];
+    }
+    const float inv = 1.0f / l;
+    if (n >= cols) return;
+    A* const out = (A*)a.out + row * D;
+    typedef A quad __attribute__((ext_vector_type(4)));
+    for (int i = w; i < kQuads; i += W) {                                     // O^T[channel 8 i + 4 hi + e][column n]
+        const int d = i * 8 + hi * 4;
+        if (!kExact && d >= D) break;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ww = 0; ww < W; ++ww) {
+            const f32x4 y = part[(ww * kQuads + i) * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += f[ww] * y[e];
+        }
+        quad y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (A)(acc[e] * inv);
+        *reinterpret_cast<quad*>(out + d) = y;
+    }
+}
+
+int64_t tiles_bound(const AttnArgs& a)
+{
+    const int64_t G = a.hq / a.c.hkv;
+    return std::min<int64_t>((int64_t)a.total_rows * G / kCols + a.batch, (int64_t)a.batch * ((a.max_new * G + kCols - 1) / kCols));
+}
+
+template <typename A, int DT, bool kExact>
+ag_status launch(const Args& x, hipStream_t st)
+{
+    constexpr int W = waves_of<A>(DT), lds = lds_bytes(W, DT);
+    if constexpr (lds > 64 * 1024) {
+        static std::atomic<uint64_t> told{0};
+        ag_status e = allow_dynamic_lds((const void*)prefill_q8_split_kernel<A, DT, kExact>, lds, told);
+        if (e) return e;
+    }
+    const AttnArgs& a = x.a;
+    if (a.c.hkv * tiles_bound(a) + kDealtPast > 0x7fffffff || (int64_t)a.total_rows * (a.hq / a.c.hkv) > 0x7fffffff) {
+        set_error("too many rows for one launch");
+        return AG_ERR_INVALID_ARG;
+    }
+    const Deal deal = deal_of(a, tiles_bound(a), std::max(1, stream_cus(st) / 8));
+    prof_before(st);
+    hipLaunchKernelGGL((prefill_q8_split_kernel<A, DT, kExact>), dim3((unsigned)workgroups_of(deal)), dim3(64 * W), lds, st, x, deal);
+    prof_after(st);
+    return hip_check(hipGetLastError(), "prefill launch");
+}
+
+template <typename A>
+ag_status launch_typed(const Args& x, hipStream_t st)
+{
+    const int d = x.a.c.d;
+    return d == 64 ? launch<A, 64, true>(x, st) : d < 64 ? launch<A, 64, false>(x, st)
+         : d == 128 ? launch<A, 128, true>(x, st) : d < 128 ? launch<A, 128, false>(x, st)
+         : d == 256 ? launch<A, 256, true>(x, st) : launch<A, 256, false>(x, st);
+}
+
+}  // namespace
+
+ag_status launch_prefill_split(const Args& x, hipStream_t st)
+{
+    return x.a.c.dtype == AG_BF16 ? launch_typed<__bf16>(x, st) : launch_typed<float>(x, st);
+}
+
+}  // namespace q8
+}  // namespace ag

@@ -4,6 +4,7 @@
 
 #include "ag_internal.h"
 #include "ag_q8.h"
+#include "bf16_terms.h"
 
 namespace ag {
 namespace q8 {
@@ -21,6 +22,8 @@ ag_status launch_read(const CacheView& c, const uint8_t* exps, void* k_out, void
 size_t    decode_workspace(int batch, int hq, int d, int max_ctx);
 ag_status launch_decode(const Args& x, void* ws, hipStream_t st);
 ag_status launch_prefill(const Args& x, hipStream_t st);
+// few rows: the keys of 32 columns dealt to the waves of one workgroup
+ag_status launch_prefill_split(const Args& x, hipStream_t st);
 
 // Where a key's exponent byte stands in its group of 16 slots: the four that a lane of the score product needs are one word.
 __host__ __device__ inline int key_place(int slot) { return (slot & 3) * 4 + ((slot >> 2) & 3); }
@@ -86,6 +89,39 @@ __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int keep)
 {
     return keep >= 4 ? w : keep <= 0 ? 0u : w & ((1u << (8 * keep)) - 1u);
 }
+
+// Numbers of the activations' type, or their arithmetic's, as bf16 terms: operands of the products.  One term rounds.
+template <typename A>
+constexpr int terms_of() { return sizeof(A) == 4 ? 3 : 1; }
+__device__ __forceinline__ void as_terms(const Terms& x, bf16x8 (&t)[3])
+{
+    t[0] = __builtin_bit_cast(bf16x8, x.h);
+    t[1] = __builtin_bit_cast(bf16x8, x.m);
+    t[2] = __builtin_bit_cast(bf16x8, x.l);
+}
+__device__ __forceinline__ void to_terms(const __bf16* p, bf16x8 (&t)[1]) { t[0] = *reinterpret_cast<const bf16x8*>(p); }
+__device__ __forceinline__ void to_terms(const float* p, bf16x8 (&t)[3]) { as_terms(split8(*reinterpret_cast<const Four*>(p), *reinterpret_cast<const Four*>(p + 4)), t); }
+__device__ __forceinline__ void to_terms(const float (&w)[8], bf16x8 (&t)[1])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[0][i] = (__bf16)w[i];
+}
+__device__ __forceinline__ void to_terms(const float (&w)[8], bf16x8 (&t)[3])
+{
+    Terms x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.set_pair(i, w[2 * i], w[2 * i + 1]);
+    as_terms(x, t);
+}
+template <int kTerms>
+__device__ __forceinline__ void no_terms(bf16x8 (&t)[kTerms])
+{
+#pragma unroll
+    for (int i = 0; i < kTerms; ++i) t[i] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+}
+
+// K and V are read once by a decode step: the streaming hint
+__device__ __forceinline__ u32x4 stream16(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
 
 }  // namespace q8
 }  // namespace ag

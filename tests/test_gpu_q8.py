@@ -17,6 +17,7 @@ import torch
 import q8_oracle as Q
 from gpu_helpers import i32
 from paper_2603_10342_amd import binding as B
+from test_q8_dispatch import TILED
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -117,7 +118,7 @@ def decode(side, q, hq, scale, ctx=None, max_ctx=None, ws_fill=float("nan"), str
     return out
 
 
-def resume(side, q, new, hq, scale, cold=False, bound=None):
+def resume(side, q, new, hq, scale, cold=False, bound=None, stream=None):
     """The last new[s] tokens of every session attend."""
     new = np.asarray(new)
     t = int(new.sum())
@@ -125,11 +126,13 @@ def resume(side, q, new, hq, scale, cold=False, bound=None):
     qd = side.dev(np.concatenate([q, np.zeros(((bound or t) - t,) + q.shape[1:])]))
     lens, cu = i32(new), i32(np.concatenate([[0], np.cumsum(new)]))
     prefix, ctx = side.lens() - new, side.lens()
+    prefix_dev = i32(prefix)
+    torch.cuda.synchronize()
     if cold:
         assert not prefix.any()
-        B.ag_attn_prefill_q8(side.cache, qd, out, side.bt_dev, lens, cu, bound or t, int(new.max()), hq, scale)
+        B.ag_attn_prefill_q8(side.cache, qd, out, side.bt_dev, lens, cu, bound or t, int(new.max()), hq, scale, stream)
     else:
-        B.ag_attn_resume_q8(side.cache, qd, out, side.bt_dev, i32(prefix), lens, cu, bound or t, int(new.max()), int(ctx.max()), hq, scale)
+        B.ag_attn_resume_q8(side.cache, qd, out, side.bt_dev, prefix_dev, lens, cu, bound or t, int(new.max()), int(ctx.max()), hq, scale, stream)
     torch.cuda.synchronize()
     assert bool((out[t:] == 5.0).all()), "rows of nobody"
     return out[:t]
@@ -276,6 +279,33 @@ def test_prefill_and_resume(dtype, d, page, lens):
         assert torch.equal(cold.view(torch.uint8), out.view(torch.uint8))
 
 
+@pytest.fixture(scope="module")
+def few_cus():
+    """A stream of eight CUs, on which small batches are many workgroups."""
+    stream = B.ag_stream_create_cumask(B.ag_cumask_build(256, 8, 0, 1))
+    yield stream
+    torch.cuda.synchronize()
+    B.ag_stream_destroy(stream)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", GEOMETRIES)
+@pytest.mark.parametrize("lens", list(TILED))
+def test_whole_tiles(few_cus, dtype, d, page, lens):
+    prefix, new = (np.array(x) for x in TILED[lens])
+    hq, hkv = 16, 2
+    side = Side(dtype, d, page, hkv, prefix + new, seed=d)
+    if prefix.any():
+        side.append(prefix)
+    side.append(new)
+    q = side.draw(int(new.sum()), hq, d)
+    out = resume(side, q, new, hq, d ** -0.5, bound=int(new.sum()) + 2, stream=few_cus)
+    check_resume(side, q, out, new, d ** -0.5, (lens, d, page))
+    if not prefix.any():
+        cold = resume(side, q, new, hq, d ** -0.5, cold=True, stream=few_cus)
+        assert torch.equal(cold.view(torch.uint8), out.view(torch.uint8))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv,prefix,new", [(32, 8, [300, 900], [300, 41]), (24, 1, [50], [90]), (1, 1, [2000], [5]), (8, 2, [0] * 70, list(range(70))),
                                                (16, 1, [1500, 0, 20], [260, 515, 1])])
@@ -290,7 +320,7 @@ def test_resume_groups_and_batches(dtype, hq, hkv, prefix, new):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_sharp_scores_and_rising_ones(dtype):
+def test_sharp_scores_and_rising_ones(few_cus, dtype):
     """Logits of standard deviation 20: nearly one key a row; and keys whose scores rise along the context, so that every tile moves the maximum."""
     d, hkv, hq = 128, 2, 8
     new = [190]
@@ -302,23 +332,24 @@ def test_sharp_scores_and_rising_ones(dtype):
     q = side.draw(190, hq, d)
     q[::2] = np.abs(q[::2])                                       # (against the ramp: up to 8 * 128 * 0.8 * scale = 70)
     scale = 0.09 * 2
-    out = resume(side, q, new, hq, scale)
-    got = out.double().cpu().numpy()
-    check(dtype, got, q, side.k[0], side.v[0], 300, scale, "resume")
+    for stream in (None, few_cus):
+        got = resume(side, q, new, hq, scale, stream=stream).double().cpu().numpy()
+        check(dtype, got, q, side.k[0], side.v[0], 300, scale, "resume")
     check(dtype, decode(side, q[-1:], hq, scale).double().cpu().numpy(), q[-1:], side.k[0], side.v[0], 489, scale, "decode")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_nan_and_infinities_stay_with_the_rows_that_see_them(dtype):
+def test_nan_and_infinities_stay_with_the_rows_that_see_them(few_cus, dtype):
     """A NaN key reaches the rows at and behind it; a session beside it, and decode before it, do not notice."""
     side = Side(dtype, 64, 16, 1, [80, 80])
     k, v = side.draw(160, 1, 64), side.draw(160, 1, 64)
     k[40, 0, 3] = np.inf
     side.append([80, 80], k=k, v=v)
     q = side.draw(160, 2, 64)
-    out = resume(side, q, [80, 80], 2, 0.125).double().cpu().numpy()
-    assert np.isnan(out[40:80]).all() and np.isfinite(out[:40]).all() and np.isfinite(out[80:]).all()
-    check(dtype, out[80:], q[80:], side.k[1], side.v[1], 0, 0.125)
+    for stream in (None, few_cus):
+        out = resume(side, q, [80, 80], 2, 0.125, stream=stream).double().cpu().numpy()
+        assert np.isnan(out[40:80]).all() and np.isfinite(out[:40]).all() and np.isfinite(out[80:]).all()
+        check(dtype, out[80:], q[80:], side.k[1], side.v[1], 0, 0.125)
     got = decode(side, q[:2], 2, 0.125, ctx=[40, 80]).double().cpu().numpy()
     check(dtype, got[:1], q[:1], side.k[0][:40], side.v[0][:40], 39, 0.125)
     check(dtype, got[1:], q[1:2], side.k[1], side.v[1], 79, 0.125)

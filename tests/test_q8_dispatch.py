@@ -1,0 +1,54 @@
+"""Which kernel a call over an 8-bit cache takes, at batches where both sides of a line were measured and differ (the figures stand at
+the lines in the sources), and on which the GPU tests rely: seen on the CPU, through a HIP runtime that logs launches."""
+import pytest
+
+from q8_launches import launched
+
+
+@pytest.fixture(scope="module")
+def tmp(tmp_path_factory):
+    return tmp_path_factory.mktemp("launches")
+
+
+def kernels(tmp, *calls):
+    return [[l.split(" ")[0].replace("q8::", "") for l in r] for r in launched(calls, tmp)]
+
+
+SPLIT, TILES, WIDE = "prefill_q8_split_kernel<", "prefill_q8_kernel<__bf16,4", "prefill_q8_kernel<__bf16,8,128,true>"
+
+
+@pytest.mark.parametrize("want,batches", [
+    (SPLIT, [dict(batch=1, prefix=6007, new=211), dict(batch=1, prefix=6007, new=600), dict(batch=1, prefix=2000, new=211), dict(batch=16, prefix=600, new=30),
+             dict(batch=1, prefix=6007, new=211, dtype="f32"), dict(batch=6, total=784, max_new=300, max_ctx=2300, d=64, page=32, dtype="f32"),
+             dict(batch=4, prefix=2000, new=16, hq=24, hkv=1)]),
+    (TILES, [dict(batch=1, prefix=2000, new=1000), dict(batch=16, new=50), dict(batch=1, new=1000), dict(batch=8, new=512), dict(batch=64, new=600), dict(batch=1, new=2048)]),
+    (WIDE, [dict(batch=8, new=4096), dict(batch=2, prefix=2000, new=1000), dict(batch=32, prefix=3000, new=200)]),
+    ("prefill_q8_kernel<float,4,128,true>", [dict(batch=8, new=1500, dtype="f32")]),
+])
+def test_prefill(tmp, want, batches):
+    for b, k in zip(batches, kernels(tmp, *(dict(call="resume", **b) for b in batches))):
+        assert len(k) == 1 and k[0].startswith(want), (b, k)
+
+
+# sessions of the GPU tests of whole tiles, on streams of eight CUs: prefix, new
+TILED = {"ragged": ([130, 0, 64, 700, 33], [70, 90, 0, 130, 1]), "prompts": ([0, 0, 0], [200, 333, 64]), "long": ([1700, 1500], [300, 120])}
+
+
+def tiled(name, **more):
+    prefix, new = TILED[name]
+    return dict(call="resume", batch=len(new), total=sum(new), max_new=max(new), max_ctx=max(p + n for p, n in zip(prefix, new)), cus=8, **more)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(128, 16), (128, 64), (64, 32), (256, 16), (48, 128), (96, 32), (208, 256)])
+def test_tiles_of_the_gpu_tests(tmp, dtype, d, page):
+    for name, k in zip(TILED, kernels(tmp, *(tiled(name, dtype=dtype, d=d, page=page, hq=16, hkv=2) for name in TILED))):
+        assert k[0].startswith("prefill_q8_kernel<"), (name, k)
+        if dtype == "bf16" and d == 128 and name == "long":
+            assert k[0] == WIDE, k
+
+
+def test_rows_past_a_launch_are_refused(tmp):
+    call = dict(call="resume", batch=1 << 20, total=0x7fffffff, max_new=2048, max_ctx=2048, hq=8, hkv=1)
+    (k,) = launched([call], tmp)
+    assert k[0].startswith("refused -1"), k
