@@ -5,6 +5,8 @@
 // same bytes as 32 of bf16 - and dealt to the workgroups in equal shares (find_share); a share's part of a pair is a segment, whose
 // steps the four waves take in contiguous quarters; the segments' (m, l, O) meet in a merge kernel in their order.
 //
+// A batch of few, short contexts takes one workgroup a pair instead, which writes its result itself.
+//
 // A wave's step is four 16-token groups, whatever pages they lie in:
 //   scores  S^T[token][head]: 16x16x32 bf16 products, rows = 4 slots of each of the 4 groups (product j takes slots 4 j .. 4 j + 3),
 //           so that lane group c ends up with all 16 slots of group c - which is what a 16-byte load of the value pool holds
@@ -12,6 +14,8 @@
 //   values  O^T[channel][head] += V^T . P^T, the weights of a lane's 16 slots against 16-byte pieces, slots 0..7 and 8..15.
 // Keys and values become bf16 on the way into the products, exactly, two numbers an instruction; a key's power of two goes in
 // with that instruction, a value's is multiplied into its weight.
+// Two workgroups a CU; three (168 registers, of which 29 are spilled, or the same 198 dealt finer) take 64.3 to 81 us where two take 64 (64 sessions of
+// 1024..4096 tokens, 32 / 8 heads x 128, 352 MB: 5.9 TB/s in the split kernel, 4.7 us of merge).  Pages of 64 or 256 instead of 16 change 1 %.
 // bf16 activations: weights are rounded to bf16 for the value product, as over bf16 caches (half a step of 2^-8, independent for
 // every key, beside the output's own rounding); fp32: queries and weights as three bf16 terms, 24 bits.
 #include <algorithm>
@@ -44,11 +48,41 @@ __device__ __forceinline__ f32x4 product(const bf16x8& a, const bf16x8 (&b)[kTer
     return acc;
 }
 
+// fp32 queries are three operands for each of a bf16 one and stand in LDS, as the lanes take them: [block][half][term][lane].  In registers they
+// leave one wave a SIMD (16 sessions of 1024..4096 tokens, 32 / 8 heads x 128, 32.0 -> 25.4 us).
+template <typename A>
+constexpr bool queries_in_lds() { return sizeof(A) == 4; }
+template <typename A>
+constexpr int query_bytes(int dt) { return queries_in_lds<A>() ? dt / 64 * 2 * terms_of<A>() * 1024 : 0; }
+
+// The queries of heads h0 .. h0 + nh - 1 of (session s, KV head g) as B operands: column = head r, k = channels (4 h + c) * 16 + 8 half .. + 7,
+// lane = 16 c + r; zero beyond the heads and channels.
+template <typename A, int DT, bool kExact>
+__device__ __forceinline__ void query(const AttnArgs& a, int s, int g, int h0, int nh, int lane, int h, int half, bf16x8 (&q)[terms_of<A>()])
+{
+    const int r = lane & 15, c = lane >> 4, D = kExact ? DT : a.c.d, chunks = D >> 4;
+    const A* row = (const A*)a.q + ((int64_t)s * a.hq + (int64_t)g * (a.hq / a.c.hkv) + h0 + min(r, nh - 1)) * D;
+    to_terms(row + (kExact ? 4 * h + c : min(4 * h + c, chunks - 1)) * 16 + half * 8, q);
+    if (r >= nh || (!kExact && 4 * h + c >= chunks)) no_terms(q);
+}
+template <typename A, int DT, bool kExact, int kWaves>
+__device__ __forceinline__ void queries_to_lds(const AttnArgs& a, int s, int g, int h0, int nh, unsigned char* s_q)
+{
+    constexpr int kTerms = terms_of<A>();
+    const int lane = threadIdx.x & 63;
+    for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < DT / 32; i += kWaves) {
+        bf16x8 q[kTerms];
+        query<A, DT, kExact>(a, s, g, h0, nh, lane, i >> 1, i & 1, q);
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) *reinterpret_cast<bf16x8*>(s_q + (i * kTerms + t) * 1024 + lane * 16) = q[t];
+    }
+}
+
 // One wave's part of a segment, steps u0 .. u0 + n - 1 of (session s, KV head g, heads h0 .. h0 + nh - 1 of its group): running maximum,
 // this lane's share of the sum, and O^T.  o[mb][i]: channel 16 mb + 4 c + i of head r, lane = 16 c + r.
 template <typename A, int DT, bool kExact>
 __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0, int nh, int ctx, int u0, int n, int lane,
-                                             float& m, float& lsum, f32x4 (&o)[DT / 16])
+                                             const unsigned char* s_q, float& m, float& lsum, f32x4 (&o)[DT / 16])
 {
     constexpr int kTerms = terms_of<A>(), kH = DT / 64, kV = DT / 16;          // 64-channel blocks of the keys, 16-channel blocks of the values
     const AttnArgs& a = x.a;
@@ -61,18 +95,12 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
     for (int mb = 0; mb < kV; ++mb) o[mb] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (n <= 0) return;
 
-    // the queries as B operands: column = head r, k = channels (4 h + c) * 16 + 8 half .. + 7; zero beyond the heads and channels
-    bf16x8 q[kH][2][kTerms];
-    {
-        const A* row = (const A*)a.q + ((int64_t)s * a.hq + (int64_t)g * (a.hq / hkv) + h0 + min(r, nh - 1)) * D;
+    bf16x8 q[queries_in_lds<A>() ? 1 : kH][2][kTerms];
+    if constexpr (!queries_in_lds<A>()) {
 #pragma unroll
         for (int h = 0; h < kH; ++h)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int chunk = kExact ? 4 * h + c : min(4 * h + c, chunks - 1);
-                to_terms(row + chunk * 16 + half * 8, q[h][half]);
-                if (r >= nh || (!kExact && 4 * h + c >= chunks)) no_terms(q[h][half]);
-            }
+            for (int half = 0; half < 2; ++half) query<A, DT, kExact>(a, s, g, h0, nh, lane, h, half, q[h][half]);
     }
 
     const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
@@ -131,15 +159,20 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
         constexpr bool kLast = decltype(last_c)::value;
         f32x4 sc[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const float scale = power((ke >> (8 * j)) & 0xFFu);
+        for (int j = 0; j < 4; ++j) sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int h = 0; h < kH; ++h) {
-                sc[j] = product(widen8(k[j][h][0], k[j][h][1], scale), q[h][0], sc[j]);
-                sc[j] = product(widen8(k[j][h][2], k[j][h][3], scale), q[h][1], sc[j]);
+        for (int h = 0; h < kH; ++h)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                bf16x8(&qh)[kTerms] = q[queries_in_lds<A>() ? 0 : h][half];
+                if constexpr (queries_in_lds<A>()) {
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) qh[t] = *reinterpret_cast<const bf16x8*>(s_q + ((h * 2 + half) * kTerms + t) * 1024 + lane * 16);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    sc[j] = product(widen8(k[j][h][2 * half], k[j][h][2 * half + 1], power((ke >> (8 * j)) & 0xFFu)), qh, sc[j]);
             }
-        }
         if constexpr (!kLast) {
             __builtin_amdgcn_sched_barrier(0);
             load_k(st + 1, pg);
@@ -173,6 +206,11 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
             to_terms(p, w[half]);
         }
         lsum = lsum * alpha + psum;
+        if (__builtin_amdgcn_ballot_w64(m_new > m) != 0) {       // (uniform: most steps move no head's maximum)
+            asm volatile("");
+#pragma unroll
+            for (int mb = 0; mb < kV; ++mb) o[mb] *= alpha;
+        }
         m = m_new;
         if constexpr (kLast) {                                   // slots behind the last token may hold anything, NaN included
 #pragma unroll
@@ -182,7 +220,6 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
         }
 #pragma unroll
         for (int mb = 0; mb < kV; ++mb) {
-            o[mb] *= alpha;
             o[mb] = product(widen8(v[mb][0], v[mb][1], 1.f), w[0], o[mb]);
             o[mb] = product(widen8(v[mb][2], v[mb][3], 1.f), w[1], o[mb]);
         }
@@ -200,21 +237,55 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
 
 // LDS of a workgroup: per wave and head O, then m and l
 constexpr int kWaves = 4;
-inline size_t lds_of(int nh, int d) { return (size_t)kWaves * nh * (d + 2) * sizeof(float); }
+inline size_t lds_of(int waves, int nh, int d) { return (size_t)waves * nh * (d + 2) * sizeof(float); }
+
+// A wave's results of a pair's nh heads into LDS (s_o: [wave][head][D], then m and l [wave][head], `rows` heads a wave) ...
+template <int DT, bool kExact, int W>
+__device__ __forceinline__ void results_to_lds(float* s_o, int w, int rows, int nh, int D, int lane, float m, float lsum, const f32x4 (&o)[DT / 16])
+{
+    const int r = lane & 15, c = lane >> 4;
+    float* const s_m = s_o + W * rows * D;
+    if (r < nh) {
+#pragma unroll
+        for (int mb = 0; mb < DT / 16; ++mb)
+            if (kExact || mb * 16 < D) *reinterpret_cast<f32x4*>(s_o + (w * rows + r) * D + mb * 16 + c * 4) = o[mb];
+        if (c == 0) { s_m[w * rows + r] = m; s_m[(W + w) * rows + r] = lsum; }
+    }
+}
+// ... and the waves' together, of four channels of a head.
+template <int W>
+__device__ __forceinline__ f32x4 combine(const float* s_o, int rows, int D, int head, int d, float& ms, float& l)
+{
+    const float* const s_m = s_o + W * rows * D;
+    ms = s_m[head];
+#pragma unroll
+    for (int ww = 1; ww < W; ++ww) ms = fmaxf(ms, s_m[ww * rows + head]);
+    const float ref = ms == -INFINITY ? 0.f : ms;
+    l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ww = 0; ww < W; ++ww) {
+        const float fw = __builtin_amdgcn_exp2f(s_m[ww * rows + head] - ref);         // a wave without steps has m = -inf -> 0
+        const f32x4 y = *reinterpret_cast<const f32x4*>(s_o + (ww * rows + head) * D + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += fw * y[e];
+        l += fw * s_m[(W + ww) * rows + head];
+    }
+    return acc;
+}
 
 template <typename A, int DT, bool kExact>
-__global__ __launch_bounds__(64 * kWaves, DT > 128 || sizeof(A) == 4 ? 1 : 2) void decode_q8_split_kernel(Args x, int32_t* __restrict__ hdr, float* __restrict__ ws_o,
+__global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split_kernel(Args x, int32_t* __restrict__ hdr, float* __restrict__ ws_o,
                                                                                                           float* __restrict__ ws_ml, int pmax)
 {
-    extern __shared__ __attribute__((aligned(16))) float s_o[];           // [wave][head][D], then m and l [wave][head]
+    extern __shared__ __attribute__((aligned(16))) unsigned char s_q[];   // queries, then the waves' results
+    float* const s_o = reinterpret_cast<float*>(s_q + query_bytes<A>(DT));            // [wave][head][D], then m and l [wave][head]
     const AttnArgs& a = x.a;
     const int B = a.batch, hkv = a.c.hkv, hq = a.hq, G = hq / hkv, D = kExact ? DT : a.c.d;
     const int nb = blocks_of(G), pairs = hkv * nb, rows = min(G, kCols);
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wg = blockIdx.x;
-    float* const s_m = s_o + kWaves * rows * D;
-    float* const s_l = s_m + kWaves * rows;
 
     Share sh;
     if (!find_share<true, kTok>(a.ctx_lens, B, pairs, hdr, sh)) return;
@@ -229,36 +300,22 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 || sizeof(A) == 4 ? 1 : 2) vo
         const int g = pair / nb, h0 = (pair - g * nb) * kCols, nh = min(G - h0, kCols);
         float m, lsum;
         f32x4 o[DT / 16];
-        attend_steps<A, DT, kExact>(x, s, g, h0, nh, ctx, u + w * per, max(0, min(per, k - w * per)), lane, m, lsum, o);
+        if constexpr (queries_in_lds<A>()) {
+            queries_to_lds<A, DT, kExact, kWaves>(a, s, g, h0, nh, s_q);
+            __syncthreads();
+        }
+        attend_steps<A, DT, kExact>(x, s, g, h0, nh, ctx, u + w * per, max(0, min(per, k - w * per)), lane, s_q, m, lsum, o);
         lsum += __shfl_xor(lsum, 16);
         lsum += __shfl_xor(lsum, 32);
-        const int r = lane & 15, c = lane >> 4;
-        if (r < nh) {
-#pragma unroll
-            for (int mb = 0; mb < DT / 16; ++mb)
-                if (kExact || mb * 16 < D) *reinterpret_cast<f32x4*>(s_o + (w * rows + r) * D + mb * 16 + c * 4) = o[mb];
-            if (c == 0) { s_m[w * rows + r] = m; s_l[w * rows + r] = lsum; }
-        }
+        results_to_lds<DT, kExact, kWaves>(s_o, w, rows, nh, D, lane, m, lsum, o);
         __syncthreads();
         // the pair starts at flat step base + pair n; its segments are numbered from the workgroup holding that step
         const int piece = wg - (base + pair * n) / q;
         if (piece < pmax) {
             for (int idx = tid; idx < nh * (D / 4); idx += 64 * kWaves) {      // four channels a thread
                 const int head = idx / (D / 4), d = (idx - head * (D / 4)) * 4;
-                float ms = s_m[head];
-#pragma unroll
-                for (int ww = 1; ww < kWaves; ++ww) ms = fmaxf(ms, s_m[ww * rows + head]);
-                const float ref = ms == -INFINITY ? 0.f : ms;
-                float l = 0.f;
-                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ww = 0; ww < kWaves; ++ww) {
-                    const float fw = __builtin_amdgcn_exp2f(s_m[ww * rows + head] - ref);     // a wave without steps has m = -inf -> 0
-                    const f32x4 y = *reinterpret_cast<const f32x4*>(s_o + (ww * rows + head) * D + d);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[e] += fw * y[e];
-                    l += fw * s_l[ww * rows + head];
-                }
+                float ms, l;
+                const f32x4 acc = combine<kWaves>(s_o, rows, D, head, d, ms, l);
                 const int64_t slot = ((int64_t)s * hq + (int64_t)g * G + h0 + head) * pmax + piece;
                 *reinterpret_cast<f32x4*>(ws_o + slot * D + d) = acc;
                 if (d == 0) { ws_ml[slot * 2] = ms; ws_ml[slot * 2 + 1] = l; }
@@ -282,18 +339,78 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 || sizeof(A) == 4 ? 1 : 2) vo
     }
 }
 
-// D / 4 lanes per (session, query head), `rows` of them a workgroup
+// A batch of few, short contexts: one workgroup a pair, which writes its result itself - no plan, no partials, no merge, whose dependent
+// round trips are most of a small step.  Eight waves, two a SIMD, where they fit its registers.
+constexpr int direct_waves(int dt) { return dt > 128 ? 4 : 8; }
+constexpr int kDirectMaxTokens = 16 << 10;
+
+template <typename A, int DT, bool kExact>
+__global__ __launch_bounds__(64 * direct_waves(DT), DT > 128 ? 1 : 2) void decode_q8_direct_kernel(Args x)
+{
+    constexpr int W = direct_waves(DT);
+    extern __shared__ __attribute__((aligned(16))) unsigned char s_q[];   // as in the split kernel
+    float* const s_o = reinterpret_cast<float*>(s_q + query_bytes<A>(DT));
+    const AttnArgs& a = x.a;
+    const int hkv = a.c.hkv, hq = a.hq, G = hq / hkv, D = kExact ? DT : a.c.d;
+    const int nb = blocks_of(G), pairs = hkv * nb, rows = min(G, kCols);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int s = blockIdx.x / pairs, pair = blockIdx.x - s * pairs, g = pair / nb, h0 = (pair - g * nb) * kCols, nh = min(G - h0, kCols);
+    const int ctx = min(a.ctx_lens[s], kDirectMaxTokens);
+    A* const out = (A*)a.out + ((int64_t)s * hq + (int64_t)g * G + h0) * D;
+    if (ctx <= 0) {                     // uniform over the workgroup
+        for (int idx = tid; idx < nh * D; idx += 64 * W) out[idx] = (A)0.0f;
+        return;
+    }
+    const int n = steps_of(ctx), per = (n + W - 1) / W;
+    float m, lsum;
+    f32x4 o[DT / 16];
+    if constexpr (queries_in_lds<A>()) {
+        queries_to_lds<A, DT, kExact, W>(a, s, g, h0, nh, s_q);
+        __syncthreads();
+    }
+    attend_steps<A, DT, kExact>(x, s, g, h0, nh, ctx, w * per, max(0, min(per, n - w * per)), lane, s_q, m, lsum, o);
+    lsum += __shfl_xor(lsum, 16);
+    lsum += __shfl_xor(lsum, 32);
+    results_to_lds<DT, kExact, W>(s_o, w, rows, nh, D, lane, m, lsum, o);
+    __syncthreads();
+    for (int idx = tid; idx < nh * (D / 4); idx += 64 * W) {
+        const int head = idx / (D / 4), d = (idx - head * (D / 4)) * 4;
+        float ms, l;
+        const f32x4 acc = combine<W>(s_o, rows, D, head, d, ms, l);
+        const float y[4] = {acc[0] / l, acc[1] / l, acc[2] / l, acc[3] / l};
+        splitk::store_quad(out + head * D + d, y);
+    }
+}
+
+// D / 4 lanes per (session, query head), `rows` of them a workgroup.  The first kAtOnce partials, the plan and the context's length are fetched
+// together, before anything says how many there are: one memory round trip instead of three, of which this launch consists.
 template <typename A>
 __global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int32_t* __restrict__ hdr, const float* __restrict__ ws_o,
                                                               const float* __restrict__ ws_ml, int pmax, int rows)
 {
+    constexpr int kAtOnce = 4;
     const AttnArgs& a = x.a;
     const int D = a.c.d, G = a.hq / a.c.hkv, nb = blocks_of(G);
     const int mine = threadIdx.x / (D / 4);
     const int64_t row = (int64_t)blockIdx.x * rows + mine;             // s * hq + h
     if (mine >= rows || row >= (int64_t)a.batch * a.hq) return;
     const int s = (int)(row / a.hq), h = (int)(row - (int64_t)s * a.hq), d = (threadIdx.x - mine * (D / 4)) * 4;
-    const int ctx = a.ctx_lens[s];
+    const float* const po = ws_o + row * pmax * D + d;
+    const float* const pml = ws_ml + row * pmax * 2;
+    const int ctx = a.ctx_lens[s], share = hdr[0], before = hdr[1 + s];
+    float ml[kAtOnce][2];
+    f32x4 y[kAtOnce];
+    auto fetch = [&](int first) {                                      // (partials that were not written hold anything: not used)
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int64_t at = min(first + i, pmax - 1);
+            ml[i][0] = pml[at * 2];
+            ml[i][1] = pml[at * 2 + 1];
+            y[i] = *reinterpret_cast<const f32x4*>(po + at * D);
+        }
+    };
+    fetch(0);
     A* out = (A*)a.out + row * D;
     if (ctx <= 0) {
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
@@ -301,39 +418,84 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int3
         return;
     }
     const int g = h / G, pair = g * nb + (h - g * G) / kCols;
-    const int q = max(1, hdr[0]), n = steps_of(ctx);
-    const int first = a.c.hkv * nb * hdr[1 + s] + pair * n;            // the pair's first flat step
+    const int q = max(1, share), n = steps_of(ctx);
+    const int first = a.c.hkv * nb * before + pair * n;                // the pair's first flat step
     const int pieces = min(pmax, (first + n - 1) / q - first / q + 1);
-    splitk::merge_quad<A>(ws_o, ws_ml, row * pmax, pieces, d, D, out);
+    float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < pieces; i0 += kAtOnce) {                     // in their order
+        if (i0 > 0) fetch(i0);
+        float m_new = m;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (i0 + i >= pieces) ml[i][0] = -INFINITY;
+            m_new = fmaxf(m_new, ml[i][0]);
+        }
+        const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f(m - ref);
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] *= keep;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (i0 + i < pieces) {
+                const float f = __builtin_amdgcn_exp2f(ml[i][0] - ref);
+                l += f * ml[i][1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += f * y[i][e];
+            }
+        }
+        m = m_new;
+    }
+    const float r[4] = {acc[0] / l, acc[1] / l, acc[2] / l, acc[3] / l};
+    splitk::store_quad(out + d, r);
 }
 
+struct Partials { int32_t* hdr; float *o, *ml; int pmax; };
+
+// grid: workgroups of the split kernel, or 0 for one workgroup a pair
 template <typename A, int DT, bool kExact>
-ag_status launch(const Args& x, int32_t* hdr, float* ws_o, float* ws_ml, int pmax, int grid, hipStream_t st)
+ag_status launch(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
-    const int rows = std::min(x.a.hq / x.a.c.hkv, kCols);
-    const size_t lds = lds_of(rows, x.a.c.d);
+    const AttnArgs& a = x.a;
+    const int G = a.hq / a.c.hkv, rows = std::min(G, kCols), W = grid ? kWaves : direct_waves(DT);
+    const size_t lds = query_bytes<A>(DT) + lds_of(W, rows, a.c.d);
     if (lds > 64 * 1024) {
-        static std::atomic<uint64_t> told{0};
-        ag_status e = allow_dynamic_lds((const void*)decode_q8_split_kernel<A, DT, kExact>, (int)lds_of(kCols, DT), told);
+        static std::atomic<uint64_t> told[2] = {};
+        const void* kernel = grid ? (const void*)decode_q8_split_kernel<A, DT, kExact> : (const void*)decode_q8_direct_kernel<A, DT, kExact>;
+        ag_status e = allow_dynamic_lds(kernel, query_bytes<A>(DT) + (int)lds_of(W, kCols, DT), told[grid ? 0 : 1]);
         if (e) return e;
     }
-    hipLaunchKernelGGL((decode_q8_split_kernel<A, DT, kExact>), dim3(grid), dim3(64 * kWaves), lds, st, x, hdr, ws_o, ws_ml, pmax);
-    return hip_check(hipGetLastError(), "decode split launch");
+    if (grid) hipLaunchKernelGGL((decode_q8_split_kernel<A, DT, kExact>), dim3(grid), dim3(64 * kWaves), lds, st, x, p.hdr, p.o, p.ml, p.pmax);
+    else hipLaunchKernelGGL((decode_q8_direct_kernel<A, DT, kExact>), dim3(a.batch * a.c.hkv * blocks_of(G)), dim3(64 * direct_waves(DT)), lds, st, x);
+    return hip_check(hipGetLastError(), "decode launch");
 }
 
 template <typename A>
-ag_status launch_typed(const Args& x, int32_t* hdr, float* ws_o, float* ws_ml, int pmax, int grid, hipStream_t st)
+ag_status launch_typed(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
     const int d = x.a.c.d;
-    ag_status e = AG_OK;
-    if (grid > 0)
-        e = d == 64 ? launch<A, 64, true>(x, hdr, ws_o, ws_ml, pmax, grid, st) : d < 64 ? launch<A, 64, false>(x, hdr, ws_o, ws_ml, pmax, grid, st)
-          : d == 128 ? launch<A, 128, true>(x, hdr, ws_o, ws_ml, pmax, grid, st) : d < 128 ? launch<A, 128, false>(x, hdr, ws_o, ws_ml, pmax, grid, st)
-          : d == 256 ? launch<A, 256, true>(x, hdr, ws_o, ws_ml, pmax, grid, st) : launch<A, 256, false>(x, hdr, ws_o, ws_ml, pmax, grid, st);
-    if (e) return e;
-    const int rows = 256 / (d / 4);
-    hipLaunchKernelGGL(decode_q8_merge_kernel<A>, dim3((unsigned)(((int64_t)x.a.batch * x.a.hq + rows - 1) / rows)), dim3(256), 0, st, x, hdr, ws_o, ws_ml, pmax, rows);
+    return d == 64 ? launch<A, 64, true>(x, p, grid, st) : d < 64 ? launch<A, 64, false>(x, p, grid, st)
+         : d == 128 ? launch<A, 128, true>(x, p, grid, st) : d < 128 ? launch<A, 128, false>(x, p, grid, st)
+         : d == 256 ? launch<A, 256, true>(x, p, grid, st) : launch<A, 256, false>(x, p, grid, st);
+}
+
+template <typename A>
+ag_status launch_merge(const Args& x, const Partials& p, hipStream_t st)
+{
+    const int rows = 256 / (x.a.c.d / 4);
+    hipLaunchKernelGGL(decode_q8_merge_kernel<A>, dim3((unsigned)(((int64_t)x.a.batch * x.a.hq + rows - 1) / rows)), dim3(256), 0, st, x, p.hdr, p.o, p.ml, p.pmax, rows);
     return hip_check(hipGetLastError(), "decode merge launch");
+}
+
+// A workgroup alone takes 2 us for every 64 tokens of its eight waves, with fp32 queries 2.8, and the longest pair's is what a launch
+// takes (the host knows no other length); shares take about 10 whatever the context of few pairs, 12 to 16 beyond half of the CUs.  Graph
+// replay, shares -> one workgroup a pair, us (pairs at 256 CUs), 8 KV heads: bf16 x 128, 512 tokens (8) 9.5 -> 5.9, 1000 (8) 9.8 -> 8.2, 1000 (64) 10.4 -> 9.9, 1600 (8) 12.5 ->
+// 12.4, 1600 (64) 13.1 -> 13.4, 2400 (8) 13.2 -> 16.7; 1600 (128) 18.3 -> 14.2, 2400 (128) 20.9 -> 21.7, 2400 (256) 31.2 -> 27.3, of 200 to 2400 (256) 22.6 -> 20.3;
+// x 64 1600 (8) 10.7 -> 9.0, 2400 (8) 10.7 -> 10.2, 4000 (8) 11.7 -> 14.8; x 256 512 (8) 13.2 -> 8.9, 1000 (8) 14.0 -> 14.0, 1600 (8) 17.3 -> 20.3; fp32 x 128 512 (8) 11.2
+// -> 7.6, 1000 (64) 11.8 -> 12.1, 1600 (64) 15.4 -> 17.5, 1600 (128) 21.0 -> 19.0.
+bool one_workgroup_a_pair(const AttnArgs& a, int64_t pairs, int64_t cus)
+{
+    const int64_t size = (int64_t)a.max_ctx * (a.c.d + 64), line = a.c.dtype == AG_BF16 ? 320000 : 230000;
+    return pairs <= cus && a.max_ctx <= kDirectMaxTokens && 4 * size <= (2 * pairs > cus ? 5 : 4) * line;
 }
 
 }  // namespace
@@ -346,16 +508,26 @@ size_t decode_workspace(int batch, int hq, int d, int max_ctx)
 ag_status launch_decode(const Args& x, void* ws, hipStream_t st)
 {
     const AttnArgs& a = x.a;
-    const int pmax = splitk::pieces_max<kTok>(a.max_ctx);
-    int32_t* hdr = (int32_t*)ws;
-    float* ws_o = (float*)(hdr + splitk::header_ints(a.batch));
-    float* ws_ml = ws_o + (size_t)a.batch * a.hq * pmax * a.c.d;
+    const bool bf16 = a.c.dtype == AG_BF16;
+    const int64_t pairs = (int64_t)a.c.hkv * blocks_of(a.hq / a.c.hkv) * a.batch;
+    Partials p;
+    p.pmax = splitk::pieces_max<kTok>(a.max_ctx);
+    p.hdr = (int32_t*)ws;
+    p.o = (float*)(p.hdr + splitk::header_ints(a.batch));
+    p.ml = p.o + (size_t)a.batch * a.hq * p.pmax * a.c.d;
+    ag_status e = AG_OK;
+    if (a.max_ctx > 0 && one_workgroup_a_pair(a, pairs, stream_cus(st))) {
+        prof_before(st);
+        e = bf16 ? launch_typed<__bf16>(x, p, 0, st) : launch_typed<float>(x, p, 0, st);
+        prof_after(st);
+        return e;
+    }
     // Upper bound of the step count from the host-known bounds: a share is at most kMaxSteps steps even if every session is max_ctx long.
-    const int64_t f_max = (int64_t)a.c.hkv * blocks_of(a.hq / a.c.hkv) * a.batch * ((a.max_ctx + (kTok - 1)) / kTok);
+    const int64_t f_max = pairs * ((a.max_ctx + (kTok - 1)) / kTok);
     if (f_max > (1 << 30)) { set_error("decode batch of %lld steps of %d tokens is beyond one launch", (long long)f_max, kTok); return AG_ERR_INVALID_ARG; }
-    const int grid = a.max_ctx > 0 ? share_workgroups(f_max, st) : 0;
     prof_before(st);
-    ag_status e = a.c.dtype == AG_BF16 ? launch_typed<__bf16>(x, hdr, ws_o, ws_ml, pmax, grid, st) : launch_typed<float>(x, hdr, ws_o, ws_ml, pmax, grid, st);
+    if (a.max_ctx > 0) e = bf16 ? launch_typed<__bf16>(x, p, share_workgroups(f_max, st), st) : launch_typed<float>(x, p, share_workgroups(f_max, st), st);
+    if (!e) e = bf16 ? launch_merge<__bf16>(x, p, st) : launch_merge<float>(x, p, st);
     prof_after(st);
     return e;
 }

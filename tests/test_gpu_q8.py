@@ -217,26 +217,38 @@ def test_append_of_every_kind_of_number(dtype):
 
 
 
+@pytest.fixture(scope="module")
+def few_cus():
+    """A stream of eight CUs, on which small batches are many workgroups."""
+    stream = B.ag_stream_create_cumask(B.ag_cumask_build(256, 8, 0, 1))
+    yield stream
+    torch.cuda.synchronize()
+    B.ag_stream_destroy(stream)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,page", GEOMETRIES)
-def test_decode(dtype, d, page):
-    """Contexts of none, one and every few tokens around the ends of groups, pages, steps and shares; stale slots are NaN under infinite powers."""
+def test_decode(few_cus, dtype, d, page):
+    """Contexts of none, one and every few tokens around the ends of groups, pages, steps and shares; stale slots are NaN under infinite powers.
+    One workgroup a pair, and on few CUs shares (test_q8_dispatch.py)."""
     ctx = [0, 1, 15, 16, 17, 63, 64, 65, 0, 127, 200, 513, 1100]
     side = Side(dtype, d, page, 2, ctx, seed=d)
     side.append(ctx)
     hq = 8
     q = side.draw(len(ctx), hq, d)
-    check_decode(side, q, decode(side, q, hq, d ** -0.5), d ** -0.5, (dtype, d, page))
+    for stream in (None, few_cus):
+        check_decode(side, q, decode(side, q, hq, d ** -0.5, stream=stream), d ** -0.5, (dtype, d, page))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (6, 2), (3, 3), (16, 1), (24, 1), (40, 2), (17, 1), (32, 8)])
-def test_decode_groups(dtype, hq, hkv):
-    ctx = [5, 700, 64, 129]
+def test_decode_groups(few_cus, dtype, hq, hkv):
+    ctx = [5, 700, 64, 129] + [1] * 6
     side = Side(dtype, 128, 16, hkv, ctx, seed=hq)
     side.append(ctx)
     q = side.draw(len(ctx), hq, 128)
-    check_decode(side, q, decode(side, q, hq, 0.11, max_ctx=16 * side.bt.shape[1]), 0.11, (hq, hkv))
+    for stream in (None, few_cus):
+        check_decode(side, q, decode(side, q, hq, 0.11, max_ctx=16 * side.bt.shape[1], stream=stream), 0.11, (hq, hkv))
 
 
 def test_decode_of_many_sessions_and_of_a_long_one():
@@ -245,7 +257,9 @@ def test_decode_of_many_sessions_and_of_a_long_one():
     side = Side("bf16", 64, 16, 1, ctx)
     side.append(ctx)
     q = side.draw(len(ctx), 4, 64)
-    check_decode(side, q, decode(side, q, 4, 0.125), 0.125, "many")
+    for max_ctx in (None, 3200):                                  # one workgroup a pair, and shares
+        side.bt_dev = i32(np.pad(side.bt, ((0, 0), (0, 200 - side.bt.shape[1]))))
+        check_decode(side, q, decode(side, q, 4, 0.125, max_ctx=max_ctx), 0.125, "many")
     side = Side("bf16", 128, 16, 2, [20000])
     side.append([20000])
     q = side.draw(1, 8, 128)
@@ -277,15 +291,6 @@ def test_prefill_and_resume(dtype, d, page, lens):
     if not prefix.any():
         cold = resume(side, q, new, hq, d ** -0.5, cold=True)
         assert torch.equal(cold.view(torch.uint8), out.view(torch.uint8))
-
-
-@pytest.fixture(scope="module")
-def few_cus():
-    """A stream of eight CUs, on which small batches are many workgroups."""
-    stream = B.ag_stream_create_cumask(B.ag_cumask_build(256, 8, 0, 1))
-    yield stream
-    torch.cuda.synchronize()
-    B.ag_stream_destroy(stream)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

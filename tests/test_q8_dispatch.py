@@ -48,6 +48,17 @@ def test_tiles_of_the_gpu_tests(tmp, dtype, d, page):
             assert k[0] == WIDE, k
 
 
+@pytest.mark.parametrize("alone,batches", [
+    (True, [dict(batch=1, new=1000), dict(batch=8, new=1600), dict(batch=32, new=2000), dict(batch=1, new=1000, dtype="f32"), dict(batch=1, new=2400, d=64), dict(batch=1, new=900, d=256),
+            dict(batch=13, new=1100, hq=8, hkv=2), dict(batch=10, new=704, hq=40, hkv=2), dict(batch=150, new=90, d=64, hq=4, hkv=1)]),
+    (False, [dict(batch=1, new=1700), dict(batch=32, new=2100), dict(batch=33, new=64), dict(batch=1, new=1300, dtype="f32"), dict(batch=1, new=2700, d=64), dict(batch=64, new=4096),
+             dict(batch=13, new=1100, hq=8, hkv=2, cus=8), dict(batch=10, new=704, hq=1, hkv=1, cus=8), dict(batch=150, new=3200, d=64, hq=4, hkv=1)]),
+])
+def test_decode(tmp, alone, batches):
+    for b, k in zip(batches, kernels(tmp, *(dict(call="decode", **b) for b in batches))):
+        assert [x.split("<")[0] for x in k] == (["decode_q8_direct_kernel"] if alone else ["decode_q8_split_kernel", "decode_q8_merge_kernel"]), (b, k)
+
+
 def test_rows_past_a_launch_are_refused(tmp):
     call = dict(call="resume", batch=1 << 20, total=0x7fffffff, max_new=2048, max_ctx=2048, hq=8, hkv=1)
     (k,) = launched([call], tmp)
