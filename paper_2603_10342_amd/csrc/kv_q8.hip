@@ -1,8 +1,8 @@
 // Append to the 8-bit KV cache, and the way back (include/ag_q8.h): rows of activations <-> e4m3 numbers with a power of two a
 // row, in pages.
 //
-// Bound by HBM, a row once and its bytes once: T * 2 Hkv * (D * sizeof + D + 1).  One workgroup per (touched 16-token group of a
-// session, KV head), as the append of the other caches: a group is what the value pool keeps together, 16 slots of a channel in a
+// Bound by HBM, a row once and its bytes once: T * 2 Hkv * (D * sizeof + D + 1).  One workgroup per touched 16-token group of a
+// session and KV head, or several heads (grid_of()): a group is what the value pool keeps together, 16 slots of a channel in a
 // 16-byte run, so that its transposition stays inside the workgroup (through LDS, 16 bytes a lane on both sides of HBM).
 // A lane takes 16 channels of a row; the lanes of a row, 2^k >= D / 16 of them in one wave, find its largest size by k exchanges.
 #include <algorithm>
@@ -92,94 +92,122 @@ __device__ __forceinline__ u32x4 gather_bytes(Word word, int at)
     return r;
 }
 
-template <typename A>
+// kHeads KV heads a workgroup: their rows of a token lie side by side.
+template <typename A, int kHeads>
 __global__ __launch_bounds__(256) void append_q8_kernel(RowArgs x)
 {
-    extern __shared__ __attribute__((aligned(16))) uint8_t s_v[];      // [token][d] e4m3
+    constexpr int kAtOnce = kHeads == 1 ? 1 : 2;
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_v[];      // [head][token][d] e4m3
     Group o;
     if (!find_group(x, o)) return;
-    const int tid = threadIdx.x, h = blockIdx.y, d = x.d, chunks = d >> 4;
-    uint8_t* const kp = x.k_pool + (o.page * x.hkv + h) * (int64_t)(d * x.ps);
-    uint8_t* const vp = x.v_pool + (o.page * x.hkv + h) * (int64_t)(d * x.ps);
-    uint8_t* const ep = x.exps + (o.page * x.hkv + h) * (int64_t)(2 * x.ps);
-    for (int idx = tid; idx < (2 * o.n_tok) << x.lanes_log2; idx += 256) {             // keys, then values
-        const int line = idx >> x.lanes_log2, c = idx & ((1 << x.lanes_log2) - 1);
-        const bool value = line >= o.n_tok;
-        const int t = value ? line - o.n_tok : line;
-        Row16<A> raw = {};
-        if (c < chunks) {
-            const u32x4* src = reinterpret_cast<const u32x4*>((const A*)(value ? x.v : x.k) + ((o.row0 + t) * x.hkv + h) * d + c * 16);
+    const int tid = threadIdx.x, h0 = blockIdx.y * kHeads, d = x.d, chunks = d >> 4, ll = x.lanes_log2;
+    const int64_t block = (int64_t)d * x.ps, at = o.page * x.hkv + h0;
+    const int lines = 2 * o.n_tok * kHeads;                            // rows: keys of the tokens, then values; the heads of a token in turn
+    struct Piece { Row16<A> raw; };
+    for (int i0 = tid; i0 < lines << ll; i0 += 256 * kAtOnce) {
+        Piece p[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(A); ++i) raw.w[i] = src[i];
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int idx = i0 + j * 256, line = idx >> ll, c = idx & ((1 << ll) - 1), tt = line / kHeads, t = tt >= o.n_tok ? tt - o.n_tok : tt;
+            p[j].raw = {};
+            if (line < lines && c < chunks) {
+                const u32x4* src = reinterpret_cast<const u32x4*>((const A*)(tt >= o.n_tok ? x.v : x.k) + ((o.row0 + t) * x.hkv + h0 + line % kHeads) * d + c * 16);
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(A); ++i) p[j].raw.w[i] = src[i];
+            }
         }
-        float f[16];
-        channels(raw, f);
-        uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) most = max(most, size_of(f[i]));
-        for (int m = 1; m < 1 << x.lanes_log2; m <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m));
-        const uint32_t e = exponent_byte(most);
-        u32x4 q;
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int idx = i0 + j * 256, line = idx >> ll, c = idx & ((1 << ll) - 1), tt = line / kHeads, hh = line % kHeads;
+            if (line >= lines) break;                                  // (a row's lanes alike)
+            const bool value = tt >= o.n_tok;
+            const int t = value ? tt - o.n_tok : tt, slot = o.slot0 + t;
+            float f[16];
+            channels(p[j].raw, f);
+            uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = quantise4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3], e);
-        const int slot = o.slot0 + t;
-        if (c < chunks) {
-            if (value) *reinterpret_cast<u32x4*>(s_v + t * d + c * 16) = q;
-            else *reinterpret_cast<u32x4*>(kp + ((slot >> 2) * chunks + c) * 64 + (slot & 3) * 16) = q;
+            for (int i = 0; i < 16; ++i) most = max(most, size_of(f[i]));
+            for (int m = 1; m < 1 << ll; m <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m));
+            const uint32_t e = exponent_byte(most);
+            u32x4 q;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = quantise4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3], e);
+            if (c < chunks) {
+                if (value) *reinterpret_cast<u32x4*>(s_v + (hh * kGroup + t) * d + c * 16) = q;
+                else *reinterpret_cast<u32x4*>(x.k_pool + (at + hh) * block + ((slot >> 2) * chunks + c) * 64 + (slot & 3) * 16) = q;
+            }
+            if (c == 0) x.exps[(at + hh) * (2 * x.ps) + (value ? x.ps + slot : (slot & ~15) + key_place(slot))] = (uint8_t)e;
         }
-        if (c == 0) ep[value ? x.ps + slot : (slot & ~15) + key_place(slot)] = (uint8_t)e;
     }
     __syncthreads();
-    uint8_t* const vg = vp + (o.slot0 >> 4) * 16 * d;                // [channel][16 slots]
+    uint8_t* const vg = x.v_pool + at * block + (o.slot0 >> 4) * 16 * d;              // [channel][16 slots]
     if (o.n_tok == kGroup) {
-        for (int ch = tid; ch < d; ch += 256)
-            *reinterpret_cast<u32x4*>(vg + ch * 16) = gather_bytes([&](int t) { return *reinterpret_cast<const uint32_t*>(s_v + t * d + (ch & ~3)); }, ch & 3);
+        for (int i = tid; i < kHeads * d; i += 256) {
+            const int hh = kHeads == 1 ? 0 : i / d, ch = i - hh * d;
+            const uint8_t* src = s_v + hh * kGroup * d + (ch & ~3);
+            *reinterpret_cast<u32x4*>(vg + hh * block + ch * 16) = gather_bytes([&](int t) { return *reinterpret_cast<const uint32_t*>(src + t * d); }, ch & 3);
+        }
     } else {                                                         // the other slots' bytes stay as they are
-        for (int idx = tid; idx < o.n_tok * d; idx += 256) {
-            const int t = idx / d, ch = idx - t * d;
-            vg[ch * 16 + (o.slot0 & 15) + t] = s_v[idx];
+        for (int i = tid; i < kHeads * o.n_tok * d; i += 256) {
+            const int line = i / d, ch = i - line * d, hh = kHeads == 1 ? 0 : line / o.n_tok, t = line - hh * o.n_tok;
+            vg[hh * block + ch * 16 + (o.slot0 & 15) + t] = s_v[(hh * kGroup + t) * d + ch];
         }
     }
 }
 
-template <typename A>
+template <typename A, int kHeads>
 __global__ __launch_bounds__(256) void read_q8_kernel(RowArgs x)
 {
-    extern __shared__ __attribute__((aligned(16))) uint8_t s_v[];      // [chunk of 16 channels][channel][16 slots], chunks 16 bytes apart
+    constexpr int kAtOnce = kHeads == 1 ? 1 : 2;
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_v[];      // [head][chunk of 16 channels][channel][16 slots], chunks 16 bytes apart
     constexpr int kChunk = 16 * 16 + 16;
     Group o;
     if (!find_group(x, o)) return;
-    const int tid = threadIdx.x, h = blockIdx.y, d = x.d, chunks = d >> 4;
-    const uint8_t* const kp = x.k_pool + (o.page * x.hkv + h) * (int64_t)(d * x.ps);
-    const uint8_t* const vg = x.v_pool + (o.page * x.hkv + h) * (int64_t)(d * x.ps) + (o.slot0 >> 4) * 16 * d;
-    const uint8_t* const ep = x.exps + (o.page * x.hkv + h) * (int64_t)(2 * x.ps);
-    for (int ch = tid; ch < d; ch += 256)
-        *reinterpret_cast<u32x4*>(s_v + (ch >> 4) * kChunk + (ch & 15) * 16) = *reinterpret_cast<const u32x4*>(vg + ch * 16);
+    const int tid = threadIdx.x, h0 = blockIdx.y * kHeads, d = x.d, chunks = d >> 4;
+    const int64_t block = (int64_t)d * x.ps, at = o.page * x.hkv + h0;
+    const uint8_t* const vg = x.v_pool + at * block + (o.slot0 >> 4) * 16 * d;
+    for (int i = tid; i < kHeads * d; i += 256) {
+        const int hh = kHeads == 1 ? 0 : i / d, ch = i - hh * d;
+        *reinterpret_cast<u32x4*>(s_v + (hh * chunks + (ch >> 4)) * kChunk + (ch & 15) * 16) = *reinterpret_cast<const u32x4*>(vg + hh * block + ch * 16);
+    }
     __syncthreads();
-    for (int idx = tid; idx < 2 * o.n_tok * chunks; idx += 256) {      // keys, then values
-        const int line = idx / chunks, c = idx - line * chunks;
-        const bool value = line >= o.n_tok;
-        const int t = value ? line - o.n_tok : line, slot = o.slot0 + t;
-        u32x4 q;
-        if (value) {
-            const uint8_t* at = s_v + c * kChunk + (slot & 12);
-            q = gather_bytes([&](int i) { return *reinterpret_cast<const uint32_t*>(at + i * 16); }, slot & 3);
-        } else {
-            q = *reinterpret_cast<const u32x4*>(kp + ((slot >> 2) * chunks + c) * 64 + (slot & 3) * 16);
-        }
-        const Row16<A> r = row_of(q, power(ep[value ? x.ps + slot : (slot & ~15) + key_place(slot)]), A(0));
-        u32x4* dst = reinterpret_cast<u32x4*>((A*)(value ? x.v : x.k) + ((o.row0 + t) * x.hkv + h) * d + c * 16);
+    const int lines = 2 * o.n_tok * kHeads;                            // rows: keys of the tokens, then values; the heads of a token in turn
+    for (int i0 = tid; i0 < lines * chunks; i0 += 256 * kAtOnce) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(A); ++i) dst[i] = r.w[i];
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int idx = i0 + j * 256, line = idx / chunks, c = idx - line * chunks, tt = line / kHeads, hh = line % kHeads;
+            if (line >= lines) break;
+            const bool value = tt >= o.n_tok;
+            const int t = value ? tt - o.n_tok : tt, slot = o.slot0 + t;
+            u32x4 q;
+            if (value) {
+                const uint8_t* src = s_v + (hh * chunks + c) * kChunk + (slot & 12);
+                q = gather_bytes([&](int i) { return *reinterpret_cast<const uint32_t*>(src + i * 16); }, slot & 3);
+            } else {
+                q = *reinterpret_cast<const u32x4*>(x.k_pool + (at + hh) * block + ((slot >> 2) * chunks + c) * 64 + (slot & 3) * 16);
+            }
+            const uint32_t e = x.exps[(at + hh) * (2 * x.ps) + (value ? x.ps + slot : (slot & ~15) + key_place(slot))];
+            const Row16<A> r = row_of(q, power(e), A(0));
+            u32x4* dst = reinterpret_cast<u32x4*>((A*)(value ? x.v : x.k) + ((o.row0 + t) * x.hkv + h0 + hh) * d + c * 16);
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(A); ++i) dst[i] = r.w[i];
+        }
     }
 }
 
 // every session touches at most N_s / 16 + 2 groups, and every group has a token
-ag_status grid_of(const CacheView& c, int batch, int total, dim3* grid)
+ag_status grid_of(const CacheView& c, int batch, int total, dim3* grid, int* heads)
 {
     const int64_t items = std::min<int64_t>(total / 16 + 2 * (int64_t)batch, total);
     if (items > 0x7fffffff || c.hkv > 65535) { set_error("too many groups or heads for one launch"); return AG_ERR_INVALID_ARG; }
-    *grid = dim3((unsigned)items, c.hkv);
+    // KV heads a workgroup takes.  A group of one is the least latency, but the chip starts a workgroup every 2 ns: past 8192 of them several
+    // heads together, up to 256 channels.  1, 2, 4 heads, us, 8 KV heads: 100 sessions of 1000..2000 tokens append x 64 156, 109, 93,
+    // x 128 213, 182, 183, x 256 424, 416, 459, fp32 x 128 303, 301, 319; read x 64 172, 117, 93, x 128 254, 188, 194, x 256 385, 389, 437; but 32 of
+    // 100..300 append x 128 10.4, 13.1, 14.7, 64 of 2..20 6.0, 8.8, 11.2.
+    *heads = 1;
+    if (items * c.hkv > 8192)
+        while (*heads < 4 && c.hkv % (2 * *heads) == 0 && 2 * *heads * c.d <= 256) *heads *= 2;
+    *grid = dim3((unsigned)items, c.hkv / *heads);
     return AG_OK;
 }
 
@@ -190,18 +218,35 @@ int lanes_log2(int chunks)
     return k;
 }
 
+template <typename A>
+void append_heads(int heads, dim3 grid, int lds, hipStream_t st, const RowArgs& x)
+{
+    if (heads == 4) hipLaunchKernelGGL((append_q8_kernel<A, 4>), grid, dim3(256), lds, st, x);
+    else if (heads == 2) hipLaunchKernelGGL((append_q8_kernel<A, 2>), grid, dim3(256), lds, st, x);
+    else hipLaunchKernelGGL((append_q8_kernel<A, 1>), grid, dim3(256), lds, st, x);
+}
+template <typename A>
+void read_heads(int heads, dim3 grid, int lds, hipStream_t st, const RowArgs& x)
+{
+    if (heads == 4) hipLaunchKernelGGL((read_q8_kernel<A, 4>), grid, dim3(256), lds, st, x);
+    else if (heads == 2) hipLaunchKernelGGL((read_q8_kernel<A, 2>), grid, dim3(256), lds, st, x);
+    else hipLaunchKernelGGL((read_q8_kernel<A, 1>), grid, dim3(256), lds, st, x);
+}
+
 }  // namespace
 
 ag_status launch_append(const CacheView& c, uint8_t* exps, const void* k_new, const void* v_new, const int32_t* bt, int max_pages,
                         const int32_t* prefix_lens, const int32_t* new_lens, const int32_t* cu_new, int batch, int total_new, hipStream_t st)
 {
     dim3 grid;
-    ag_status e = grid_of(c, batch, total_new, &grid);
+    int heads;
+    ag_status e = grid_of(c, batch, total_new, &grid, &heads);
     if (e) return e;
     const RowArgs x = {(uint8_t*)c.k, (uint8_t*)c.v, exps, (void*)k_new, (void*)v_new, bt, max_pages, prefix_lens, new_lens, cu_new,
                        batch, c.hkv, c.d, c.ps, c.ps_shift, lanes_log2(c.d / 16)};
-    if (c.dtype == AG_BF16) hipLaunchKernelGGL(append_q8_kernel<__bf16>, grid, dim3(256), kGroup * c.d, st, x);
-    else hipLaunchKernelGGL(append_q8_kernel<float>, grid, dim3(256), kGroup * c.d, st, x);
+    const int lds = heads * kGroup * c.d;
+    if (c.dtype == AG_BF16) append_heads<__bf16>(heads, grid, lds, st, x);
+    else append_heads<float>(heads, grid, lds, st, x);
     return hip_check(hipGetLastError(), "append launch");
 }
 
@@ -209,13 +254,14 @@ ag_status launch_read(const CacheView& c, const uint8_t* exps, void* k_out, void
                       const int32_t* prefix_lens, const int32_t* new_lens, const int32_t* cu_new, int batch, int total_new, hipStream_t st)
 {
     dim3 grid;
-    ag_status e = grid_of(c, batch, total_new, &grid);
+    int heads;
+    ag_status e = grid_of(c, batch, total_new, &grid, &heads);
     if (e) return e;
     const RowArgs x = {(uint8_t*)c.k, (uint8_t*)c.v, (uint8_t*)exps, k_out, v_out, bt, max_pages, prefix_lens, new_lens, cu_new,
                        batch, c.hkv, c.d, c.ps, c.ps_shift, lanes_log2(c.d / 16)};
-    const int lds = c.d / 16 * (16 * 16 + 16);
-    if (c.dtype == AG_BF16) hipLaunchKernelGGL(read_q8_kernel<__bf16>, grid, dim3(256), lds, st, x);
-    else hipLaunchKernelGGL(read_q8_kernel<float>, grid, dim3(256), lds, st, x);
+    const int lds = heads * (c.d / 16) * (16 * 16 + 16);
+    if (c.dtype == AG_BF16) read_heads<__bf16>(heads, grid, lds, st, x);
+    else read_heads<float>(heads, grid, lds, st, x);
     return hip_check(hipGetLastError(), "read launch");
 }
 

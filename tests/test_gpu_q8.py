@@ -188,6 +188,26 @@ def test_append_and_read_back_to_the_bit(dtype, d, page):
             assert bool((got[t:] == 9.0).all())
 
 
+@pytest.mark.parametrize("dtype,d,hkv", [("bf16", 64, 8), ("bf16", 128, 6), ("f32", 48, 4), ("f32", 128, 2)])
+def test_many_groups_take_several_heads_a_workgroup(dtype, d, hkv):
+    """Past 8192 (group, head) pairs (test_q8_dispatch.py has the line): bytes as before, appended and read back, ragged."""
+    new = [40] * (8192 // (4 * hkv) + 60) + [1, 17, 33]
+    side = Side(dtype, d, 32, hkv, new, seed=d, fill=0xA5)
+    side.append(new)
+    n, t = np.array(new), sum(new)
+    out = [torch.full((t + 1, hkv, d), 9.0, dtype=TD[dtype], device=DEV) for _ in range(2)]
+    B.ag_kv_read_q8(side.cache, *out, side.bt_dev, i32(np.zeros(len(new))), i32(n), i32(np.concatenate([[0], np.cumsum(n)])), t + 1)
+    torch.cuda.synchronize()
+    for got, want in zip(out, (side.k, side.v)):
+        assert np.array_equal(got[:t].double().cpu().numpy(), np.concatenate(want)) and bool((got[t:] == 9.0).all())
+    mine = np.zeros((side.cache.num_pages, 32), bool)
+    for s in range(len(new)):
+        pos = np.arange(new[s])
+        mine[side.bt[s, pos // 32], pos % 32] = True
+    for pool in (side.cache.k_pool_token_major(), side.cache.v_pool_token_major(), *side.cache.exps_token_major()):
+        assert bool((pool.cpu().numpy().swapaxes(1, 2)[~mine] == 0xA5).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_append_of_every_kind_of_number(dtype):
     """Rows of zeros, infinities, NaN, denormal and the largest numbers, ties, sizes at both sides of a power's end."""

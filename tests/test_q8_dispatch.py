@@ -59,6 +59,18 @@ def test_decode(tmp, alone, batches):
         assert [x.split("<")[0] for x in k] == (["decode_q8_direct_kernel"] if alone else ["decode_q8_split_kernel", "decode_q8_merge_kernel"]), (b, k)
 
 
+def test_heads_of_an_append_workgroup(tmp):
+    few, many = dict(batch=64, total=704, max_ctx=200), dict(batch=100, total=150000, max_ctx=2000)
+    calls = [(dict(few), 1), (dict(many, d=64), 4), (dict(many), 2), (dict(many, d=256), 1), (dict(many, hkv=6, d=64), 2), (dict(many, hkv=3, d=64), 1), (dict(many, d=64, dtype="f32"), 4)]
+    # ... and those of the GPU test
+    for dtype, d, hkv, heads in [("bf16", 64, 8, 4), ("bf16", 128, 6, 2), ("f32", 48, 4, 4), ("f32", 128, 2, 2)]:
+        n = 8192 // (4 * hkv) + 60
+        calls.append((dict(batch=n + 3, total=40 * n + 52, max_ctx=40, page=32, dtype=dtype, d=d, hkv=hkv), heads))
+    for name in ("append", "read"):
+        for (c, heads), k in zip(calls, kernels(tmp, *(dict(call=name, **c) for c, _ in calls))):
+            assert k == ["%s_q8_kernel<%s,%d>" % (name, "float" if c.get("dtype") == "f32" else "__bf16", heads)], (c, k)
+
+
 def test_rows_past_a_launch_are_refused(tmp):
     call = dict(call="resume", batch=1 << 20, total=0x7fffffff, max_new=2048, max_ctx=2048, hq=8, hkv=1)
     (k,) = launched([call], tmp)
