@@ -104,30 +104,35 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
     }
 
     const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
-    const int64_t block = (int64_t)D * ps;                       // bytes of one (page, head)
-    const uint8_t* const kpool = (const uint8_t*)a.c.k;
-    const uint8_t* const vpool = (const uint8_t*)a.c.v;
-    // page ids by scalar loads: the index is uniform and the table read-only for the kernel's lifetime
+    // page ids by scalar loads: the index is uniform and the table read-only for the kernel's lifetime; fetched a step before they are used
     typedef const __attribute__((address_space(4))) int32_t* cptr_t;
     const cptr_t bt = (cptr_t)(uintptr_t)(a.bt + (int64_t)s * a.max_pages);
-    struct Pages { int k, v; };                                  // of this lane's group of the keys, and of the values
-    auto pages_of = [&](int st) {
-        Pages p = {0, 0};
+    const Finder find(a.c, D, g);
+    struct Ids { int id[4]; };
+    auto ids_of = [&](int st) {
+        Ids p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p.id[i] = bt[min(4 * (u0 + st) + i, last_grp) >> gshift];
+        return p;
+    };
+    // where this lane's group of a step stands: group r / 4 of the keys, c of the values
+    auto place = [&](int st, const Ids& p, int mine) {
+        Where w = {0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int id = bt[min(4 * (u0 + st) + i, last_grp) >> gshift];
-            p.k |= id & ((r >> 2) == i ? -1 : 0);
-            p.v |= id & (c == i ? -1 : 0);
+            const Where x = find.at(p.id[i], min(4 * (u0 + st) + i, last_grp) & gmask);
+            const uint32_t mask = mine == i ? ~0u : 0u;
+            w.data |= x.data & mask;
+            w.exps |= x.exps & mask;
         }
-        return p;
+        return w;
     };
 
     u32x4 k[4][kH], v[kV], ve;
     uint32_t ke;
-    auto load_k = [&](int st, Pages p) {
-        const int gi = min(4 * (u0 + st) + (r >> 2), last_grp) & gmask;
-        const int64_t at = (int64_t)p.k * hkv + g;
-        const uint8_t* kp = kpool + at * block + gi * 16 * D + (r & 3) * 16;
+    auto load_k = [&](int st, const Ids& p) {
+        const Where w = place(st, p, r >> 2);
+        const uint8_t* kp = data_at(a.c.k, w.data) + (r & 3) * 16;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -135,21 +140,20 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
                 const int chunk = kExact ? 4 * h + c : min(4 * h + c, chunks - 1);       // (beyond: times zeros of the query)
                 k[j][h] = stream16(kp + (j * chunks + chunk) * 64);
             }
-        ke = *reinterpret_cast<const uint32_t*>(x.exps + at * (2 * ps) + gi * 16 + (r & 3) * 4);
+        ke = *reinterpret_cast<const uint32_t*>(exps_at(x.exps, w.exps) + (r & 3) * 4);
     };
-    auto load_v = [&](int st, Pages p) {
-        const int gi = min(4 * (u0 + st) + c, last_grp) & gmask;
-        const int64_t at = (int64_t)p.v * hkv + g;
-        const uint8_t* vp = vpool + at * block + gi * 16 * D;
+    auto load_v = [&](int st, const Ids& p) {
+        const Where w = place(st, p, c);
+        const uint8_t* vp = data_at(a.c.v, w.data);
 #pragma unroll
         for (int mb = 0; mb < kV; ++mb) v[mb] = stream16(vp + (kExact ? mb * 16 + r : min(mb * 16 + r, D - 1)) * 16);
-        ve = *reinterpret_cast<const u32x4*>(x.exps + at * (2 * ps) + ps + gi * 16);
+        ve = *reinterpret_cast<const u32x4*>(exps_at(x.exps, w.exps) + ps);
     };
 
-    Pages pg = pages_of(0);
-    load_k(0, pg);
-    load_v(0, pg);
-    pg = pages_of(1);
+    Ids ids = ids_of(0);
+    load_k(0, ids);
+    load_v(0, ids);
+    ids = ids_of(1);
     __builtin_amdgcn_sched_barrier(0);
 
     // One step; unless it is the wave's last, the next step's keys are requested as soon as the scores have taken this one's, and
@@ -175,7 +179,7 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
             }
         if constexpr (!kLast) {
             __builtin_amdgcn_sched_barrier(0);
-            load_k(st + 1, pg);
+            load_k(st + 1, ids);
             __builtin_amdgcn_sched_barrier(0);
         }
         // sc[j][i]: slot 4 j + i of group c
@@ -225,8 +229,8 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
         }
         if constexpr (!kLast) {
             __builtin_amdgcn_sched_barrier(0);
-            load_v(st + 1, pg);
-            pg = pages_of(st + 2);
+            load_v(st + 1, ids);
+            ids = ids_of(st + 2);
             __builtin_amdgcn_sched_barrier(0);
         }
     };

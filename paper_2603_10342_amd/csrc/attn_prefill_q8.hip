@@ -110,11 +110,9 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
 
     // ---- tile requests: this wave's group of the tile, 16 keys; pieces [chunk][key] of the keys, [channel] of the values ----
     const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
-    const int64_t block = (int64_t)D * ps;                                    // bytes of one (page, head)
+    const Finder find(a.c, D, g);
     const int my_grp = w / kWavesPerGroup, piece0 = (w % kWavesPerGroup) * kPer * 64 + lane;
     const int key = lane & 15;                                                // of the group, in every piece of a lane
-    const uint8_t* const kpool = (const uint8_t*)a.c.k;
-    const uint8_t* const vpool = (const uint8_t*)a.c.v;
     // Page ids of 64 groups, 16 tiles, a lane each, and of the next 64: everything that is in flight in the loop is a vector load, as a
     // scalar one shares its counter with the LDS operands and turns every wait for one of them into a wait for all.
     auto ids_of = [&](int win) { return a.bt[(int64_t)s * a.max_pages + (min(win * 64 + lane, last_grp) >> gshift)]; };
@@ -124,26 +122,24 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
     const uint32_t k_off = (uint32_t)((key >> 2) * chunks * 64 + (key & 3) * 16 + (piece0 >> 4) * 64), v_off = (uint32_t)(piece0 * 16);
     const uint32_t ke_off = (uint32_t)key_place(key), ve_off = (uint32_t)(ps + (lane & 3) * 4);
     auto request_k = [&](int t, int page, Raw& x8) {
-        const int gi = min(t * 4 + my_grp, last_grp) & gmask;
-        const int64_t at = (int64_t)page * hkv + g;
-        const uint8_t* kp = kpool + at * block + gi * 16 * D;
+        const Where w8 = find.at(page, min(t * 4 + my_grp, last_grp) & gmask);
+        const uint8_t* kp = data_at(a.c.k, w8.data);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             x8.k[i] = u32x4{0, 0, 0, 0};
             if (kExact || (piece0 >> 4) + i * 4 < chunks) x8.k[i] = *reinterpret_cast<const u32x4*>(kp + (k_off + i * 256));
         }
-        x8.ke = (x.exps + at * (2 * ps) + gi * 16)[ke_off];
+        x8.ke = exps_at(x.exps, w8.exps)[ke_off];
     };
     auto request_v = [&](int t, int page, Raw& x8) {
-        const int gi = min(t * 4 + my_grp, last_grp) & gmask;
-        const int64_t at = (int64_t)page * hkv + g;
-        const uint8_t* vp = vpool + at * block + gi * 16 * D;
+        const Where w8 = find.at(page, min(t * 4 + my_grp, last_grp) & gmask);
+        const uint8_t* vp = data_at(a.c.v, w8.data);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             x8.v[i] = u32x4{0, 0, 0, 0};
             if (kExact || piece0 + i * 64 < D) x8.v[i] = *reinterpret_cast<const u32x4*>(vp + (v_off + i * 1024));
         }
-        x8.ve = *reinterpret_cast<const uint32_t*>(x.exps + at * (2 * ps) + gi * 16 + ve_off);
+        x8.ve = *reinterpret_cast<const uint32_t*>(exps_at(x.exps, w8.exps) + ve_off);
     };
     // Into LDS as bf16: K [chunk of 8 channels][64 keys], V [chunk of 8 keys][channel], 16-byte pieces, in kUnits steps of about four
     // instructions: of every piece the two halves of its keys, then the eight pairs of its values.
@@ -310,19 +306,21 @@ ag_status launch(const Args& x, hipStream_t st)
 }
 
 // Few rows on long contexts: the keys of 32 columns dealt to the waves of a workgroup (attn_split_q8.hip) instead of whole tiles, each a chain
-// of all of them.  Both chains grow with the context, that of tiles 3.5 times as fast (fp32: 4.2); a launch is as long as a chain, or as
-// many as a CU's workgroups come to.  Graph replay, 32 / 8 heads x 128 unless said otherwise, tiles -> split, us (workgroups of 32 columns): one chunk on
-// 6007 tokens of 50 rows (56) 128 -> 34.5, 211 (216) 133 -> 40, 600 (600) 142 -> 106, 1000 (1000) 150 -> 152; on 2000 of 211 51 -> 18.6, 1000 72 -> 75;
-// 16 of 30 on 600 (512) 20.9 -> 17.7; 8 of 50..300 on 2000..4000 (1328) 105 -> 124, x 256 on 500..1000 91 -> 101, x 64 74 -> 73; 4 prompts of 100 (416)
-// 9.8 -> 9.7, 16 of 50 (896) 9.3 -> 17.4, one of 1000 (1000) 29 -> 31; fp32: 211 on 6007 235 -> 79, x 64 6 of 20..300 on 100..2000 (784) 55 -> 45, 8 prompts of 300..1500
-// (8000) 266 -> 373.
+// of all of them.  A launch is as long as a chain, or as many as a CU's workgroups come to, and a chain is a start and its share of the
+// context; in units of what a context token costs eight waves: 1500 + L, of four 1500 + 2.1 L with two workgroups a CU, of tiles 1500 + 4.5 L;
+// with one wave a SIMD (fp32 past 64 channels, bf16 past 128) of four 1500 + 2.1 L and of tiles 1500 + 7 L, one workgroup a CU.  Graph replay, 32 / 8
+// heads x 128 unless said otherwise, tiles -> split, us (workgroups of 32 columns): one chunk on 6007 tokens of 50 rows (56) 128 -> 32, 211 (216) 133 -> 34, 400 (400) 136
+// -> 66, 1000 (1000) 150 -> 152; on 2000 of 300 (304) 53 -> 27, 1000 72 -> 75; 16 of 30 on 600 (512) 20.4 -> 12.6; 8 of 50..300 on 2000..4000 (1328) 105 -> 124; prompts: 4 of
+// 100 (416) 9.8 -> 7.0, 3 of 250 (768) 13.0 -> 13.1, one of 500 (504) 17.8 -> 9.7; x 64: 211 on 6007 100 -> 26, 3 prompts of 250 9.9 -> 8.3; x 256: 8 of 50..300 on 500..1000 (1328)
+// 91 -> 101; fp32: 211 on 6007 235 -> 67, 8 prompts of 300..1500 (8000) 266 -> 373, x 64 6 of 20..300 on 100..2000 (784) 55 -> 32.
 bool split_preferred(const AttnArgs& a, hipStream_t st)
 {
-    const bool wide = a.c.d > 128 || a.c.dtype == AG_F32;
+    const bool fp32 = a.c.dtype == AG_F32, wide = a.c.d > 128 || (fp32 && a.c.d > 64);
     const double cus = stream_cus(st), heads = a.c.hkv, ctx = a.max_ctx;
-    const double chains = std::max(1.0, heads * (double)tiles_bound(a, 32) / (cus * (a.c.d <= 64 && !wide ? 2 : 1)));       // workgroups of eight waves, or four of up to 512 registers
-    const double tiles = std::max(1.0, heads * (double)tiles_bound(a, 128) / (cus * (wide ? 1 : 2)));
-    return chains * (1200 + ctx) < tiles * (600 + ctx) * (a.c.dtype == AG_F32 ? 4.2 : 3.5);
+    const double few = heads * (double)tiles_bound(a, 32), whole = heads * (double)tiles_bound(a, 128);
+    const double split = !wide && few <= cus ? 1500 + ctx : std::max(1.0, few / (wide ? cus : 2 * cus)) * (1500 + 2.1 * ctx);
+    const double tiles = std::max(1.0, whole / (wide || fp32 ? cus : 2 * cus)) * (1500 + (wide ? 7.0 : 4.5) * ctx);
+    return split < tiles;
 }
 
 // 256 columns a workgroup, bf16 x 128: a tile is brought in for twice the columns, but a launch ends on longer chains.  Where the context is

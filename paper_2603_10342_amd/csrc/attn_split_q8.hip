@@ -35,16 +35,16 @@ __device__ __forceinline__ f32x16 product(const bf16x8& a, const bf16x8 (&b)[kTe
     return acc;
 }
 
-// Waves of a workgroup: eight, two a SIMD, where queries, O and a step's operands fit 256 registers.
+// Whether two waves a SIMD fit: queries, O and a step's operands in 256 registers.
 template <typename A>
-constexpr int waves_of(int dt) { return dt > 128 || (dt > 64 && sizeof(A) == 4) ? 4 : 8; }
+constexpr bool two_a_simd(int dt) { return dt <= 64 || (dt <= 128 && sizeof(A) == 2); }
 // per wave O, and m and l per column
 constexpr int lds_bytes(int waves, int dt) { return waves * (kCols * dt * 4 + 2 * kCols * 4); }
 
-template <typename A, int DT, bool kExact>
-__global__ __launch_bounds__(64 * waves_of<A>(DT), waves_of<A>(DT) / 4) void prefill_q8_split_kernel(Args x, Deal deal)
+template <typename A, int DT, bool kExact, int W>
+__global__ __launch_bounds__(64 * W, two_a_simd<A>(DT) ? 2 : 1) void prefill_q8_split_kernel(Args x, Deal deal)
 {
-    constexpr int W = waves_of<A>(DT), kTerms = terms_of<A>(), kK = DT / 32, kV = DT / 32;      // 16-byte loads of a lane for a step's keys, and for its values
+    constexpr int kTerms = terms_of<A>(), kK = DT / 32, kV = DT / 32;      // 16-byte loads of a lane for a step's keys, and for its values
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const AttnArgs& a = x.a;
     const int hkv = a.c.hkv, hq = a.hq, G = hq / hkv, D = kExact ? DT : a.c.d, ps = a.c.ps, chunks = D >> 4;
@@ -76,15 +76,7 @@ __global__ __launch_bounds__(64 * waves_of<A>(DT), waves_of<A>(DT) / 4) void pre
         typedef const __attribute__((address_space(4))) int32_t* cptr_t;
         const cptr_t bt = (cptr_t)(uintptr_t)(a.bt + (int64_t)s * a.max_pages);
         const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
-        const int64_t block = (int64_t)D * ps;                                // bytes of one (page, head)
-        const uint8_t* const kpool = (const uint8_t*)a.c.k;
-        const uint8_t* const vpool = (const uint8_t*)a.c.v;
         const int kg = (n >> 2) & 1;                                          // this lane's group of the keys
-        struct Pages { int a, b; };
-        auto pages_of = [&](int st) {
-            const int grp = 2 * (u0 + st);
-            return Pages{bt[min(grp, last_grp) >> gshift], bt[min(grp + 1, last_grp) >> gshift]};
-        };
         // columns' queries as B operands: k-step (i, half) covers channels (2 i + hi) * 16 + half * 8 .. + 7
         bf16x8 q[kK][2][kTerms];
         {
@@ -101,30 +93,38 @@ __global__ __launch_bounds__(64 * waves_of<A>(DT), waves_of<A>(DT) / 4) void pre
         u32x4 k[kK], v[kV], ve;
         uint32_t ke;
         const uint32_t k_off = (uint32_t)((n >> 3) * chunks * 64 + (n & 3) * 16), ke_off = (uint32_t)((n & 3) * 4 + (n >> 3));
-        auto load_k = [&](int st, Pages p) {
-            const int gi = min(2 * (u0 + st) + kg, last_grp) & gmask;
-            const int64_t at = (int64_t)(kg ? p.b : p.a) * hkv + g;
-            const uint8_t* kp = kpool + at * block + gi * 16 * D + k_off;
+        const Finder find(a.c, D, g);
+        struct Ids { int a, b; };                                             // pages of a step's two groups, fetched a step before they are used
+        auto ids_of = [&](int st) {
+            const int grp = 2 * (u0 + st);
+            return Ids{bt[min(grp, last_grp) >> gshift], bt[min(grp + 1, last_grp) >> gshift]};
+        };
+        struct Places { Where a, b; };
+        auto places_of = [&](int st, Ids id) {
+            const int grp = 2 * (u0 + st);
+            return Places{find.at(id.a, min(grp, last_grp) & gmask), find.at(id.b, min(grp + 1, last_grp) & gmask)};
+        };
+        auto load_k = [&](const Places& p) {
+            const uint8_t* kp = data_at(a.c.k, kg ? p.b.data : p.a.data) + k_off;
 #pragma unroll
             for (int i = 0; i < kK; ++i) {
                 const int chunk = kExact ? 2 * i + hi : min(2 * i + hi, chunks - 1);     // (beyond: times zeros of the query)
                 k[i] = *reinterpret_cast<const u32x4*>(kp + chunk * 64);
             }
-            ke = (x.exps + at * (2 * ps) + gi * 16)[ke_off];
+            ke = exps_at(x.exps, kg ? p.b.exps : p.a.exps)[ke_off];
         };
-        auto load_v = [&](int st, Pages p) {
-            const int gi = min(2 * (u0 + st) + hi, last_grp) & gmask;
-            const int64_t at = (int64_t)(hi ? p.b : p.a) * hkv + g;
-            const uint8_t* vp = vpool + at * block + gi * 16 * D;
+        auto load_v = [&](const Places& p) {
+            const uint8_t* vp = data_at(a.c.v, hi ? p.b.data : p.a.data);
 #pragma unroll
             for (int mb = 0; mb < kV; ++mb) v[mb] = *reinterpret_cast<const u32x4*>(vp + (kExact ? mb * 32 + n : min(mb * 32 + n, D - 1)) * 16);
-            ve = *reinterpret_cast<const u32x4*>(x.exps + at * (2 * ps) + ps + gi * 16);
+            ve = *reinterpret_cast<const u32x4*>(exps_at(x.exps, hi ? p.b.exps : p.a.exps) + ps);
         };
         const float sl2 = a.scale * kLog2e;
-        Pages pg = pages_of(0);
-        load_k(0, pg);
-        load_v(0, pg);
-        pg = pages_of(1);
+        Ids ids = ids_of(0);
+        Places at = places_of(0, ids);
+        load_k(at);
+        load_v(at);
+        ids = ids_of(1);
         __builtin_amdgcn_sched_barrier(0);
         // (past the wave's last step the requests run on: clamped to the context, never used)
 #pragma unroll 1
@@ -139,7 +139,8 @@ __global__ __launch_bounds__(64 * waves_of<A>(DT), waves_of<A>(DT) / 4) void pre
                 sc = product(widen8(k[i][2], k[i][3], scale), q[i][1], sc);
             }
             __builtin_amdgcn_sched_barrier(0);
-            load_k(st + 1, pg);
+            at = places_of(st + 1, ids);
+            load_k(at);
             __builtin_amdgcn_sched_barrier(0);
             // sc[i]: slot i of group hi
             const int tok0 = (u0 + st) * kTok + hi * 16;
@@ -187,13 +188,12 @@ __global__ __launch_bounds__(64 * waves_of<A>(DT), waves_of<A>(DT) / 4) void pre
             }
             lsum += psum;
 #pragma unroll
-            for (int mb = 0; mb < kV; ++mb) {
-                o[mb] = product(widen8(v[mb][0], v[mb][1], 1.f), wt[0], o[mb]);
-                o[mb] = product(widen8(v[mb][2], v[mb][3], 1.f), wt[1], o[mb]);
-            }
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int mb = 0; mb < kV; ++mb) o[mb] = product(widen8(v[mb][2 * half], v[mb][2 * half + 1], 1.f), wt[half], o[mb]);
             __builtin_amdgcn_sched_barrier(0);
-            load_v(st + 1, pg);
-            pg = pages_of(st + 2);
+            load_v(at);
+            ids = ids_of(st + 2);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -247,13 +247,13 @@ int64_t tiles_bound(const AttnArgs& a)
     return std::min<int64_t>((int64_t)a.total_rows * G / kCols + a.batch, (int64_t)a.batch * ((a.max_new * G + kCols - 1) / kCols));
 }
 
-template <typename A, int DT, bool kExact>
+template <typename A, int DT, bool kExact, int W>
 ag_status launch(const Args& x, hipStream_t st)
 {
-    constexpr int W = waves_of<A>(DT), lds = lds_bytes(W, DT);
+    constexpr int lds = lds_bytes(W, DT);
     if constexpr (lds > 64 * 1024) {
         static std::atomic<uint64_t> told{0};
-        ag_status e = allow_dynamic_lds((const void*)prefill_q8_split_kernel<A, DT, kExact>, lds, told);
+        ag_status e = allow_dynamic_lds((const void*)prefill_q8_split_kernel<A, DT, kExact, W>, lds, told);
         if (e) return e;
     }
     const AttnArgs& a = x.a;
@@ -261,20 +261,34 @@ ag_status launch(const Args& x, hipStream_t st)
         set_error("too many rows for one launch");
         return AG_ERR_INVALID_ARG;
     }
-    const Deal deal = deal_of(a, tiles_bound(a), std::max(1, stream_cus(st) / 8));
+    const Deal deal = deal_of(a, tiles_bound(a), std::max(1, stream_cus(st) * (two_a_simd<A>(DT) ? 8 / W : 1) / 8));
     prof_before(st);
-    hipLaunchKernelGGL((prefill_q8_split_kernel<A, DT, kExact>), dim3((unsigned)workgroups_of(deal)), dim3(64 * W), lds, st, x, deal);
+    hipLaunchKernelGGL((prefill_q8_split_kernel<A, DT, kExact, W>), dim3((unsigned)workgroups_of(deal)), dim3(64 * W), lds, st, x, deal);
     prof_after(st);
     return hip_check(hipGetLastError(), "prefill launch");
+}
+
+// Eight waves a workgroup and one workgroup a CU, or four and two: a chain is half as long, or there is room for twice as many, and on
+// short contexts less to start and to add up.  Graph replay, eight -> four, us (workgroups): 211 rows on 6007 tokens (216) 34.6 -> 37.2, x 64 25.7 -> 30.5, fp32 x 64
+// 43.4 -> 46.0; 400 on 6007 (400) 75 -> 66, 500 rows (504) 13.5 -> 9.7, 16 of 30 on 600 (512) 17.0 -> 12.6, fp32 x 64 18.4 -> 13.7; 8 of 30 on 100 (256) 6.6 -> 6.1.
+bool four_waves(const AttnArgs& a, hipStream_t st) { return a.c.hkv * tiles_bound(a) > stream_cus(st) || a.max_ctx <= 256; }
+
+template <typename A, int DT, bool kExact>
+ag_status launch_waves(const Args& x, hipStream_t st)
+{
+    if constexpr (two_a_simd<A>(DT)) {
+        if (!four_waves(x.a, st)) return launch<A, DT, kExact, 8>(x, st);
+    }
+    return launch<A, DT, kExact, 4>(x, st);
 }
 
 template <typename A>
 ag_status launch_typed(const Args& x, hipStream_t st)
 {
     const int d = x.a.c.d;
-    return d == 64 ? launch<A, 64, true>(x, st) : d < 64 ? launch<A, 64, false>(x, st)
-         : d == 128 ? launch<A, 128, true>(x, st) : d < 128 ? launch<A, 128, false>(x, st)
-         : d == 256 ? launch<A, 256, true>(x, st) : launch<A, 256, false>(x, st);
+    return d == 64 ? launch_waves<A, 64, true>(x, st) : d < 64 ? launch_waves<A, 64, false>(x, st)
+         : d == 128 ? launch_waves<A, 128, true>(x, st) : d < 128 ? launch_waves<A, 128, false>(x, st)
+         : d == 256 ? launch_waves<A, 256, true>(x, st) : launch_waves<A, 256, false>(x, st);
 }
 
 }  // namespace

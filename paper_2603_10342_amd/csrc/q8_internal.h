@@ -120,6 +120,23 @@ __device__ __forceinline__ void no_terms(bf16x8 (&t)[kTerms])
     for (int i = 0; i < kTerms; ++i) t[i] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
 }
 
+// Where a 16-token group of KV head g stands in the pools, in units of 256 bytes, and in the exponents, in units of 16: 32 bits for pools of
+// a terabyte.  (Byte offsets are 64-bit products, which took the loops of the attention kernels up to 60 scalar instructions a step.)
+struct Where { uint32_t data, exps; };
+struct Finder {
+    uint32_t page_data, page_exps, data0, exps0, group;
+    __device__ __forceinline__ Finder(const CacheView& c, int d, int g)
+        : page_data((uint32_t)c.hkv * (uint32_t)(d * c.ps >> 8)), page_exps((uint32_t)c.hkv * (uint32_t)(c.ps >> 3)),
+          data0((uint32_t)g * (uint32_t)(d * c.ps >> 8)), exps0((uint32_t)g * (uint32_t)(c.ps >> 3)), group((uint32_t)d >> 4) {}
+    // group gi of the page
+    __device__ __forceinline__ Where at(int page, int gi) const
+    {
+        return Where{(uint32_t)page * page_data + data0 + (uint32_t)gi * group, (uint32_t)page * page_exps + exps0 + (uint32_t)gi};
+    }
+};
+__device__ __forceinline__ const uint8_t* data_at(const void* pool, uint32_t data) { return (const uint8_t*)pool + ((uint64_t)data << 8); }
+__device__ __forceinline__ const uint8_t* exps_at(const uint8_t* exps, uint32_t at) { return exps + ((uint64_t)at << 4); }
+
 // K and V are read once by a decode step: the streaming hint
 __device__ __forceinline__ u32x4 stream16(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
 

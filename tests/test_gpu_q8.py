@@ -17,7 +17,7 @@ import torch
 import q8_oracle as Q
 from gpu_helpers import i32
 from paper_2603_10342_amd import binding as B
-from test_q8_dispatch import TILED
+from test_q8_dispatch import FOUR_LENS, TILED
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -329,6 +329,17 @@ def test_whole_tiles(few_cus, dtype, d, page, lens):
     if not prefix.any():
         cold = resume(side, q, new, hq, d ** -0.5, cold=True, stream=few_cus)
         assert torch.equal(cold.view(torch.uint8), out.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(128, 16), (64, 32), (96, 16), (48, 128)])
+def test_few_rows_by_four_waves(few_cus, dtype, d, page):
+    prefix, new = (np.array(x) for x in FOUR_LENS)
+    side = Side(dtype, d, page, 2, prefix + new, seed=d)
+    side.append(prefix)
+    side.append(new)
+    q = side.draw(int(new.sum()), 16, d)
+    check_resume(side, q, resume(side, q, new, 16, d ** -0.5, stream=few_cus), new, d ** -0.5, (d, page))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

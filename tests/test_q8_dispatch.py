@@ -39,6 +39,19 @@ def tiled(name, **more):
     return dict(call="resume", batch=len(new), total=sum(new), max_new=max(new), max_ctx=max(p + n for p, n in zip(prefix, new)), cus=8, **more)
 
 
+def test_waves_of_a_split_workgroup(tmp):
+    """Eight up to one workgroup a CU and past 256 tokens, where two waves a SIMD fit; the last is the GPU test's."""
+    for b, w in [(dict(batch=1, prefix=6007, new=211), 8), (dict(batch=1, prefix=6007, new=400), 4), (dict(batch=8, prefix=100, new=30), 4), (dict(batch=8, prefix=300, new=30), 8),
+                 (dict(batch=1, prefix=6007, new=211, d=256), 4), (dict(batch=1, prefix=6007, new=211, dtype="f32"), 4), (dict(batch=1, prefix=6007, new=211, dtype="f32", d=64), 8),
+                 (dict(FOUR, d=128), 4), (dict(FOUR, d=64, dtype="f32"), 4)]:
+        (k,) = kernels(tmp, dict(call="resume", **b))
+        assert k[0].startswith(SPLIT) and k[0].endswith(",%d>" % w), (b, k)
+
+
+FOUR_LENS = ([900, 17], [20, 5])                                  # prefix, new; on eight CUs at 16 / 2 heads
+FOUR = dict(batch=2, total=25, max_new=20, max_ctx=920, hq=16, hkv=2, cus=8)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,page", [(128, 16), (128, 64), (64, 32), (256, 16), (48, 128), (96, 32), (208, 256)])
 def test_tiles_of_the_gpu_tests(tmp, dtype, d, page):
