@@ -53,30 +53,6 @@ __device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q
     }
 }
 
-// An iteration's vector work and value product one after the other: at 256 channels, where there are two products to a score and
-// nothing is gained by laying them side by side (tile32::softmax_and_value_product).
-template <int DT, bool kLo>
-__device__ __forceinline__ void softmax_after_value_product(bool do_sm, bool do_pv, const unsigned char* vb, const f32x16 (&sc)[2], float sl2, float& m,
-                                                            float& lsum, const Weights<kLo>& p_prev, Weights<kLo>& p_cur, f32x16 (&o)[DT / 32])
-{
-    if (do_pv) tile32::pv_tile<DT, kLo>(vb, p_prev, o);
-    if (!do_sm) return;
-    float mx = tile32::row_max(sc) * sl2;
-    // m is shared by the two lanes of a query: if either lane's own maximum outgrew it, combine them
-    if (__builtin_amdgcn_ballot_w64(mx > m + tile32::kRescaleSlack) != 0) {
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float m_new = fmaxf(m, mx);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-        lsum *= alpha;
-#pragma unroll
-        for (int mb = 0; mb < DT / 32; ++mb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[mb][i] *= alpha;
-        m = m_new;
-    }
-    tile32::exp_tile<kLo>(sc, sl2, m == -INFINITY ? 0.f : m, lsum, p_cur);
-}
-
 template <typename A, int NW, int DT, bool kExact>
 __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void prefill_q8_kernel(Args x, Deal deal)
 {
@@ -247,8 +223,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
 #pragma unroll
             for (int unit = 0; unit < kUnits; ++unit) put_unit(unit, t, now, put);
         }
-        if constexpr (DT > 128) softmax_after_value_product<DT, kLo>(do_sm, do_pv, vb, sc, sl2, m, lsum, p_prev, p_cur, o);
-        else tile32::softmax_and_value_product<DT, kLo>(do_sm, do_pv, vb, sc, sl2, m, lsum, p_prev, p_cur, o);
+        tile32::softmax_and_value_product<DT, kLo>(do_sm, do_pv, vb, sc, sl2, m, lsum, p_prev, p_cur, o);
         __syncthreads();
     };
 #pragma unroll 1

@@ -181,7 +181,8 @@ __device__ __forceinline__ void softmax_and_value_product(bool do_sm, bool do_pv
         // the common case: two independent pieces, interleaved by hand.  Step i issues the operand read
         // of matrix instruction i + kAhead, matrix instruction i (with low terms: both of its operand), and the exp of
         // its share of the 16 score pairs; the fences keep the compiler from regrouping them.
-        constexpr int kAhead = kOperandsAhead, kMb = DT / 32, kN = 4 * kMb, kPairs = 16 / kN;
+        constexpr int kAhead = kOperandsAhead, kMb = DT / 32, kN = 4 * kMb;
+        constexpr int kEvery = kN > 16 ? kN / 16 : 1, kPairs = 16 * kEvery / kN, kStages = kN / kEvery;      // (at 256 channels a pair every other step)
         bf16x8 opnd[kAhead + 1];
         auto operand = [&](int i) -> const unsigned char* { return vb + (i % kMb) * 512 + (i / kMb) * DT * 32; };
 #pragma unroll
@@ -205,26 +206,27 @@ __device__ __forceinline__ void softmax_and_value_product(bool do_sm, bool do_pv
             pr_prev[k] = bf16x2{(__bf16)0.f, (__bf16)0.f};
         }
 #pragma unroll
-        for (int i = 0; i < kN + 2; ++i) {
-            if (i < kN) {
-                if (i + kAhead < kN) opnd[(i + kAhead) % (kAhead + 1)] = *reinterpret_cast<const bf16x8*>(operand(i + kAhead));
-                value_step<DT, kLo>(i, opnd[i % (kAhead + 1)], p_prev, terms, o);
+        for (int step = 0; step < kN + 2 * kEvery; ++step) {
+            if (step < kN) {
+                if (step + kAhead < kN) opnd[(step + kAhead) % (kAhead + 1)] = *reinterpret_cast<const bf16x8*>(operand(step + kAhead));
+                value_step<DT, kLo>(step, opnd[step % (kAhead + 1)], p_prev, terms, o);
             }
+            const int i = step / kEvery;                     // of the vector work
 #pragma unroll
-            for (int k = 0; k < kPairs; ++k) {
+            for (int k = 0; k < (step % kEvery == 0 ? kPairs : 0); ++k) {
                 if (i >= 2) {
                     if constexpr (kLo) psum += s_prev[k];
                     else psum = __builtin_amdgcn_fdot2_f32_bf16(pr_prev[k], kOnes, psum, false);   // l sums the weights as rounded
                 }
-                if (i >= 1 && i <= kN) {
+                if (i >= 1 && i <= kStages) {
                     pr_prev[k] = pack_pair<kLo>((i - 1) * kPairs + k, q0[k], q1[k], p_cur);
                     s_prev[k] = q0[k] + q1[k];
                 }
-                if (i < kN) {
+                if (i < kStages) {
                     q0[k] = __builtin_amdgcn_exp2f(x0[k]);
                     q1[k] = __builtin_amdgcn_exp2f(x1[k]);
                 }
-                if (i + 1 < kN) { x0[k] = scaled((i + 1) * kPairs + k, 0); x1[k] = scaled((i + 1) * kPairs + k, 1); }
+                if (i + 1 < kStages) { x0[k] = scaled((i + 1) * kPairs + k, 0); x1[k] = scaled((i + 1) * kPairs + k, 1); }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
