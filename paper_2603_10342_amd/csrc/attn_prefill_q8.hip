@@ -283,14 +283,14 @@ ag_status launch(const Args& x, hipStream_t st)
 // Few rows on long contexts: the keys of 32 columns dealt to the waves of a workgroup (attn_split_q8.hip) instead of whole tiles, each a chain
 // of all of them.  A launch is as long as a chain, or as many as a CU's workgroups come to, and a chain is a start and its share of the
 // context; in units of what a context token costs eight waves: 1500 + L, of four 1500 + 2.1 L with two workgroups a CU, of tiles 1500 + 4.5 L;
-// with one wave a SIMD (fp32 past 64 channels, bf16 past 128) of four 1500 + 2.1 L and of tiles 1500 + 7 L, one workgroup a CU.  Graph replay, 32 / 8
+// with one wave a SIMD (past 128 channels) of four 1500 + 2.1 L and of tiles 1500 + 7 L, one workgroup a CU, as tiles of fp32 always.  Graph replay, 32 / 8
 // heads x 128 unless said otherwise, tiles -> split, us (workgroups of 32 columns): one chunk on 6007 tokens of 50 rows (56) 128 -> 32, 211 (216) 133 -> 34, 400 (400) 136
 // -> 66, 1000 (1000) 150 -> 152; on 2000 of 300 (304) 53 -> 27, 1000 72 -> 75; 16 of 30 on 600 (512) 20.4 -> 12.6; 8 of 50..300 on 2000..4000 (1328) 105 -> 124; prompts: 4 of
 // 100 (416) 9.8 -> 7.0, 3 of 250 (768) 13.0 -> 13.1, one of 500 (504) 17.8 -> 9.7; x 64: 211 on 6007 100 -> 26, 3 prompts of 250 9.9 -> 8.3; x 256: 8 of 50..300 on 500..1000 (1328)
-// 91 -> 101; fp32: 211 on 6007 235 -> 67, 8 prompts of 300..1500 (8000) 266 -> 373, x 64 6 of 20..300 on 100..2000 (784) 55 -> 32.
+// 91 -> 101; fp32: 211 on 6007 235 -> 66, 8 prompts of 300..1500 (8000) 266 -> 373, x 64 6 of 20..300 on 100..2000 (784) 55 -> 32.
 bool split_preferred(const AttnArgs& a, hipStream_t st)
 {
-    const bool fp32 = a.c.dtype == AG_F32, wide = a.c.d > 128 || (fp32 && a.c.d > 64);
+    const bool fp32 = a.c.dtype == AG_F32, wide = a.c.d > 128;
     const double cus = stream_cus(st), heads = a.c.hkv, ctx = a.max_ctx;
     const double few = heads * (double)tiles_bound(a, 32), whole = heads * (double)tiles_bound(a, 128);
     const double split = !wide && few <= cus ? 1500 + ctx : std::max(1.0, few / (wide ? cus : 2 * cus)) * (1500 + 2.1 * ctx);

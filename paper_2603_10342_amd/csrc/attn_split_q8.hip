@@ -35,14 +35,18 @@ __device__ __forceinline__ f32x16 product(const bf16x8& a, const bf16x8 (&b)[kTe
     return acc;
 }
 
-// Whether two waves a SIMD fit: queries, O and a step's operands in 256 registers.
+// fp32 queries are three operands for each of a bf16 one.  Past 64 channels they stand in LDS, the same for every wave, as the lanes take them,
+// [block][half][term][lane]: in registers they leave one wave a SIMD at 128 channels (50 rows on 6007 tokens 65 -> 57 us, 400 on 3000 74.5 -> 67.6), and
+// spill at 256 (211 on 6007 202 -> 129).  At 64 they fit, and reading them costs more (211 on 6007, four waves, 46.9 -> 52.0).
 template <typename A>
-constexpr bool two_a_simd(int dt) { return dt <= 64 || (dt <= 128 && sizeof(A) == 2); }
+constexpr bool queries_in_lds(int dt) { return sizeof(A) == 4 && dt > 64; }
+// Whether two waves a SIMD fit: (queries,) O and a step's operands in 256 registers.
+constexpr bool two_a_simd(int dt) { return dt <= 128; }
 // per wave O, and m and l per column
 constexpr int lds_bytes(int waves, int dt) { return waves * (kCols * dt * 4 + 2 * kCols * 4); }
 
 template <typename A, int DT, bool kExact, int W>
-__global__ __launch_bounds__(64 * W, two_a_simd<A>(DT) ? 2 : 1) void prefill_q8_split_kernel(Args x, Deal deal)
+__global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_split_kernel(Args x, Deal deal)
 {
     constexpr int kTerms = terms_of<A>(), kK = DT / 32, kV = DT / 32;      // 16-byte loads of a lane for a step's keys, and for its values
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -72,23 +76,32 @@ __global__ __launch_bounds__(64 * W, two_a_simd<A>(DT) ? 2 : 1) void prefill_q8_
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[mb][i] = 0.f;
 
+    // columns' queries as B operands: k-step (i, half) covers channels (2 i + hi) * 16 + half * 8 .. + 7
+    auto query = [&](int i, int half, bf16x8 (&q)[kTerms]) {
+        const int chunk = 2 * i + hi;
+        if (kExact || chunk < chunks) to_terms((const A*)a.q + row * D + chunk * 16 + half * 8, q);
+        else no_terms(q);
+    };
+    if constexpr (queries_in_lds<A>(DT)) {
+        for (int i = w; i < 2 * kK; i += W) {
+            bf16x8 q[kTerms];
+            query(i >> 1, i & 1, q);
+#pragma unroll
+            for (int t = 0; t < kTerms; ++t) *reinterpret_cast<bf16x8*>(lds + (i * kTerms + t) * 1024 + lane * 16) = q[t];
+        }
+        __syncthreads();
+    }
     if (my_n > 0) {
         typedef const __attribute__((address_space(4))) int32_t* cptr_t;
         const cptr_t bt = (cptr_t)(uintptr_t)(a.bt + (int64_t)s * a.max_pages);
         const int last_grp = (ctx - 1) >> 4, gshift = a.c.ps_shift - 4, gmask = (1 << gshift) - 1;
         const int kg = (n >> 2) & 1;                                          // this lane's group of the keys
-        // columns' queries as B operands: k-step (i, half) covers channels (2 i + hi) * 16 + half * 8 .. + 7
-        bf16x8 q[kK][2][kTerms];
-        {
-            const A* qp = (const A*)a.q + row * D;
+        bf16x8 q[queries_in_lds<A>(DT) ? 1 : kK][2][kTerms];
+        if constexpr (!queries_in_lds<A>(DT)) {
 #pragma unroll
             for (int i = 0; i < kK; ++i)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int chunk = 2 * i + hi;
-                    if (kExact || chunk < chunks) to_terms(qp + chunk * 16 + half * 8, q[i][half]);
-                    else no_terms(q[i][half]);
-                }
+                for (int half = 0; half < 2; ++half) query(i, half, q[i][half]);
         }
         u32x4 k[kK], v[kV], ve;
         uint32_t ke;
@@ -134,10 +147,16 @@ __global__ __launch_bounds__(64 * W, two_a_simd<A>(DT) ? 2 : 1) void prefill_q8_
             for (int i = 0; i < 16; ++i) sc[i] = 0.f;
             const float scale = power(ke);
 #pragma unroll
-            for (int i = 0; i < kK; ++i) {
-                sc = product(widen8(k[i][0], k[i][1], scale), q[i][0], sc);
-                sc = product(widen8(k[i][2], k[i][3], scale), q[i][1], sc);
-            }
+            for (int i = 0; i < kK; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    bf16x8(&qh)[kTerms] = q[queries_in_lds<A>(DT) ? 0 : i][half];
+                    if constexpr (queries_in_lds<A>(DT)) {
+#pragma unroll
+                        for (int t = 0; t < kTerms; ++t) qh[t] = *reinterpret_cast<const bf16x8*>(lds + ((2 * i + half) * kTerms + t) * 1024 + lane * 16);
+                    }
+                    sc = product(widen8(k[i][2 * half], k[i][2 * half + 1], scale), qh, sc);
+                }
             __builtin_amdgcn_sched_barrier(0);
             at = places_of(st + 1, ids);
             load_k(at);
@@ -199,6 +218,7 @@ __global__ __launch_bounds__(64 * W, two_a_simd<A>(DT) ? 2 : 1) void prefill_q8_
     }
     lsum += __shfl_xor(lsum, 32);
 
+    if constexpr (queries_in_lds<A>(DT)) __syncthreads();                       // (no wave reads its queries any more)
     // the waves' sums, lane by lane: O as quads of channels [wave][quad][lane], then m and l [wave][column]
     f32x4* const part = reinterpret_cast<f32x4*>(lds);
     float* const s_m = reinterpret_cast<float*>(lds + W * kCols * DT * 4);
@@ -261,7 +281,7 @@ ag_status launch(const Args& x, hipStream_t st)
         set_error("too many rows for one launch");
         return AG_ERR_INVALID_ARG;
     }
-    const Deal deal = deal_of(a, tiles_bound(a), std::max(1, stream_cus(st) * (two_a_simd<A>(DT) ? 8 / W : 1) / 8));
+    const Deal deal = deal_of(a, tiles_bound(a), std::max(1, stream_cus(st) * (two_a_simd(DT) ? 8 / W : 1) / 8));
     prof_before(st);
     hipLaunchKernelGGL((prefill_q8_split_kernel<A, DT, kExact, W>), dim3((unsigned)workgroups_of(deal)), dim3(64 * W), lds, st, x, deal);
     prof_after(st);
@@ -269,14 +289,14 @@ ag_status launch(const Args& x, hipStream_t st)
 }
 
 // Eight waves a workgroup and one workgroup a CU, or four and two: a chain is half as long, or there is room for twice as many, and on
-// short contexts less to start and to add up.  Graph replay, eight -> four, us (workgroups): 211 rows on 6007 tokens (216) 34.6 -> 37.2, x 64 25.7 -> 30.5, fp32 x 64
-// 43.4 -> 46.0; 400 on 6007 (400) 75 -> 66, 500 rows (504) 13.5 -> 9.7, 16 of 30 on 600 (512) 17.0 -> 12.6, fp32 x 64 18.4 -> 13.7; 8 of 30 on 100 (256) 6.6 -> 6.1.
+// short contexts less to start and to add up.  Graph replay, eight -> four, us (workgroups): 211 rows on 6007 tokens (216) 34.6 -> 37.2, x 64 25.7 -> 30.5, fp32
+// 65.7 -> 73.8, x 64 43.4 -> 46.0; 400 on 6007 (400) 75 -> 66, 500 rows (504) 13.5 -> 9.7, 16 of 30 on 600 (512) 17.0 -> 12.6, fp32 25.3 -> 20.5, x 64 18.4 -> 13.7; 8 of 30 on 100 (256) 6.6 -> 6.1.
 bool four_waves(const AttnArgs& a, hipStream_t st) { return a.c.hkv * tiles_bound(a) > stream_cus(st) || a.max_ctx <= 256; }
 
 template <typename A, int DT, bool kExact>
 ag_status launch_waves(const Args& x, hipStream_t st)
 {
-    if constexpr (two_a_simd<A>(DT)) {
+    if constexpr (two_a_simd(DT)) {
         if (!four_waves(x.a, st)) return launch<A, DT, kExact, 8>(x, st);
     }
     return launch<A, DT, kExact, 4>(x, st);

@@ -42,7 +42,7 @@ def tiled(name, **more):
 def test_waves_of_a_split_workgroup(tmp):
     """Eight up to one workgroup a CU and past 256 tokens, where two waves a SIMD fit; the last is the GPU test's."""
     for b, w in [(dict(batch=1, prefix=6007, new=211), 8), (dict(batch=1, prefix=6007, new=400), 4), (dict(batch=8, prefix=100, new=30), 4), (dict(batch=8, prefix=300, new=30), 8),
-                 (dict(batch=1, prefix=6007, new=211, d=256), 4), (dict(batch=1, prefix=6007, new=211, dtype="f32"), 4), (dict(batch=1, prefix=6007, new=211, dtype="f32", d=64), 8),
+                 (dict(batch=1, prefix=6007, new=211, d=256), 4), (dict(batch=1, prefix=6007, new=211, dtype="f32"), 8), (dict(batch=1, prefix=6007, new=211, dtype="f32", d=64), 8),
                  (dict(FOUR, d=128), 4), (dict(FOUR, d=64, dtype="f32"), 4)]:
         (k,) = kernels(tmp, dict(call="resume", **b))
         assert k[0].startswith(SPLIT) and k[0].endswith(",%d>" % w), (b, k)
