@@ -344,14 +344,15 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
 }
 
 // A batch of few, short contexts: one workgroup a pair, which writes its result itself - no plan, no partials, no merge, whose dependent
-// round trips are most of a small step.  Eight waves, two a SIMD, where they fit its registers.
-constexpr int direct_waves(int dt) { return dt > 128 ? 4 : 8; }
+// round trips are most of a small step.  Four waves and two workgroups a CU: eight are no faster alone (one session of 500 to 1000 tokens 7.8 us, four
+// 7.5) and leave room for half as many pairs (256 sessions of 1 to 512 46 us, four 29).
 constexpr int kDirectMaxTokens = 16 << 10;
+constexpr int64_t kDirectMaxPairs = 1 << 30;        // of a launch
 
 template <typename A, int DT, bool kExact>
-__global__ __launch_bounds__(64 * direct_waves(DT), DT > 128 ? 1 : 2) void decode_q8_direct_kernel(Args x)
+__global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_direct_kernel(Args x)
 {
-    constexpr int W = direct_waves(DT);
+    constexpr int W = kWaves;
     extern __shared__ __attribute__((aligned(16))) unsigned char s_q[];   // as in the split kernel
     float* const s_o = reinterpret_cast<float*>(s_q + query_bytes<A>(DT));
     const AttnArgs& a = x.a;
@@ -387,13 +388,13 @@ __global__ __launch_bounds__(64 * direct_waves(DT), DT > 128 ? 1 : 2) void decod
     }
 }
 
-// D / 4 lanes per (session, query head), `rows` of them a workgroup.  The first kAtOnce partials, the plan and the context's length are fetched
-// together, before anything says how many there are: one memory round trip instead of three, of which this launch consists.
+// D / 4 lanes per (session, query head), `rows` of them a workgroup.  The first four partials, the plan and the context's length are fetched
+// together, before anything says how many there are: one memory round trip instead of three, of which this launch consists.  Further ones come
+// eight at a time (one session of 16000 tokens, 32 partials: 18.2 -> 16.2 us).
 template <typename A>
 __global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int32_t* __restrict__ hdr, const float* __restrict__ ws_o,
                                                               const float* __restrict__ ws_ml, int pmax, int rows)
 {
-    constexpr int kAtOnce = 4;
     const AttnArgs& a = x.a;
     const int D = a.c.d, G = a.hq / a.c.hkv, nb = blocks_of(G);
     const int mine = threadIdx.x / (D / 4);
@@ -403,35 +404,25 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int3
     const float* const po = ws_o + row * pmax * D + d;
     const float* const pml = ws_ml + row * pmax * 2;
     const int ctx = a.ctx_lens[s], share = hdr[0], before = hdr[1 + s];
-    float ml[kAtOnce][2];
-    f32x4 y[kAtOnce];
-    auto fetch = [&](int first) {                                      // (partials that were not written hold anything: not used)
+    float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    int pieces = 0;
+    // partials first .. first + N - 1, in their order (those that were not written hold anything: not used)
+    auto take = [&](int first, auto count, auto known) {
+        constexpr int N = decltype(count)::value;
+        float ml[N][2];
+        f32x4 y[N];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
+        for (int i = 0; i < N; ++i) {
             const int64_t at = min(first + i, pmax - 1);
             ml[i][0] = pml[at * 2];
             ml[i][1] = pml[at * 2 + 1];
             y[i] = *reinterpret_cast<const f32x4*>(po + at * D);
         }
-    };
-    fetch(0);
-    A* out = (A*)a.out + row * D;
-    if (ctx <= 0) {
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        splitk::store_quad(out + d, zero);
-        return;
-    }
-    const int g = h / G, pair = g * nb + (h - g * G) / kCols;
-    const int q = max(1, share), n = steps_of(ctx);
-    const int first = a.c.hkv * nb * before + pair * n;                // the pair's first flat step
-    const int pieces = min(pmax, (first + n - 1) / q - first / q + 1);
-    float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < pieces; i0 += kAtOnce) {                     // in their order
-        if (i0 > 0) fetch(i0);
+        known();
         float m_new = m;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (i0 + i >= pieces) ml[i][0] = -INFINITY;
+        for (int i = 0; i < N; ++i) {
+            if (first + i >= pieces) ml[i][0] = -INFINITY;
             m_new = fmaxf(m_new, ml[i][0]);
         }
         const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f(m - ref);
@@ -439,8 +430,8 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int3
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] *= keep;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (i0 + i < pieces) {
+        for (int i = 0; i < N; ++i) {
+            if (first + i < pieces) {
                 const float f = __builtin_amdgcn_exp2f(ml[i][0] - ref);
                 l += f * ml[i][1];
 #pragma unroll
@@ -448,9 +439,18 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int3
             }
         }
         m = m_new;
-    }
-    const float r[4] = {acc[0] / l, acc[1] / l, acc[2] / l, acc[3] / l};
-    splitk::store_quad(out + d, r);
+    };
+    take(0, std::integral_constant<int, 4>{}, [&] {
+        if (ctx <= 0) return;
+        const int g = h / G, pair = g * nb + (h - g * G) / kCols;
+        const int q = max(1, share), n = steps_of(ctx);
+        const int first = a.c.hkv * nb * before + pair * n;            // the pair's first flat step
+        pieces = min(pmax, (first + n - 1) / q - first / q + 1);
+    });
+    for (int first = 4; first < pieces; first += 8) take(first, std::integral_constant<int, 8>{}, [] {});
+    const float inv = pieces > 0 ? 1.f / l : 0.f;                      // (a session without context: zeros)
+    const float r[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    splitk::store_quad((A*)a.out + row * D + d, r);
 }
 
 struct Partials { int32_t* hdr; float *o, *ml; int pmax; };
@@ -460,16 +460,16 @@ template <typename A, int DT, bool kExact>
 ag_status launch(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
     const AttnArgs& a = x.a;
-    const int G = a.hq / a.c.hkv, rows = std::min(G, kCols), W = grid ? kWaves : direct_waves(DT);
-    const size_t lds = query_bytes<A>(DT) + lds_of(W, rows, a.c.d);
+    const int G = a.hq / a.c.hkv;
+    const size_t lds = query_bytes<A>(DT) + lds_of(kWaves, std::min(G, kCols), a.c.d);
     if (lds > 64 * 1024) {
         static std::atomic<uint64_t> told[2] = {};
         const void* kernel = grid ? (const void*)decode_q8_split_kernel<A, DT, kExact> : (const void*)decode_q8_direct_kernel<A, DT, kExact>;
-        ag_status e = allow_dynamic_lds(kernel, query_bytes<A>(DT) + (int)lds_of(W, kCols, DT), told[grid ? 0 : 1]);
+        ag_status e = allow_dynamic_lds(kernel, query_bytes<A>(DT) + (int)lds_of(kWaves, kCols, DT), told[grid ? 0 : 1]);
         if (e) return e;
     }
     if (grid) hipLaunchKernelGGL((decode_q8_split_kernel<A, DT, kExact>), dim3(grid), dim3(64 * kWaves), lds, st, x, p.hdr, p.o, p.ml, p.pmax);
-    else hipLaunchKernelGGL((decode_q8_direct_kernel<A, DT, kExact>), dim3(a.batch * a.c.hkv * blocks_of(G)), dim3(64 * direct_waves(DT)), lds, st, x);
+    else hipLaunchKernelGGL((decode_q8_direct_kernel<A, DT, kExact>), dim3(a.batch * a.c.hkv * blocks_of(G)), dim3(64 * kWaves), lds, st, x);
     return hip_check(hipGetLastError(), "decode launch");
 }
 
@@ -490,16 +490,18 @@ ag_status launch_merge(const Args& x, const Partials& p, hipStream_t st)
     return hip_check(hipGetLastError(), "decode merge launch");
 }
 
-// A workgroup alone takes 2 us for every 64 tokens of its eight waves, with fp32 queries 2.8, and the longest pair's is what a launch
-// takes (the host knows no other length); shares take about 10 whatever the context of few pairs, 12 to 16 beyond half of the CUs.  Graph
-// replay, shares -> one workgroup a pair, us (pairs at 256 CUs), 8 KV heads: bf16 x 128, 512 tokens (8) 9.5 -> 5.9, 1000 (8) 9.8 -> 8.2, 1000 (64) 10.4 -> 9.9, 1600 (8) 12.5 ->
-// 12.4, 1600 (64) 13.1 -> 13.4, 2400 (8) 13.2 -> 16.7; 1600 (128) 18.3 -> 14.2, 2400 (128) 20.9 -> 21.7, 2400 (256) 31.2 -> 27.3, of 200 to 2400 (256) 22.6 -> 20.3;
-// x 64 1600 (8) 10.7 -> 9.0, 2400 (8) 10.7 -> 10.2, 4000 (8) 11.7 -> 14.8; x 256 512 (8) 13.2 -> 8.9, 1000 (8) 14.0 -> 14.0, 1600 (8) 17.3 -> 20.3; fp32 x 128 512 (8) 11.2
-// -> 7.6, 1000 (64) 11.8 -> 12.1, 1600 (64) 15.4 -> 17.5, 1600 (128) 21.0 -> 19.0.
+// A workgroup alone takes 2 us for every 256 tokens, with fp32 queries 2.6, and the longest pair's is the least a launch takes (the host
+// knows no other length); shares take about 10 whatever the context of few pairs, and a segment each - 2.5 us - for short pairs one after
+// the other.  Past half of the CUs a pair each keeps them busy anyway; long contexts are left to shares, as one among short ones would be
+// all that a launch waits for.  Graph replay, shares -> one workgroup a pair, us (pairs at 256 CUs), 8 KV heads, x 128: one session of 1000 tokens (8) 9.3 -> 8.5, 1600 (8)
+// 11.8 -> 12.3, 2400 (8) 12.7 -> 16.5, 8 of 1000 (64) 10.1 -> 10.0, 16 of 1600 (128) 16.8 -> 14.4, 32 of 2400 (256) 30.6 -> 27.1, of 500 to 4000 (256) 31.0 -> 30.6, 64 of 1 to 128
+// (512) 25.7 -> 6.9, of 1 to 512 28.2 -> 9.7, of 1000 to 2000 39.0 -> 35.2, of 1024 to 4096 64.5 -> 65.4, 256 of 1000 to 2000 (2048) 145 -> 130; x 64: one of 1600 10.1 -> 9.4,
+// 2400 11.1 -> 12.6, 64 of 1000 to 2000 23.1 -> 19.6; x 256: one of 1000 13.6 -> 16.3, 64 of 1000 to 2000 75.5 -> 68.9; fp32 x 128: one of 1000 11.1 -> 12.2, 16 of 1600 20.6 -> 18.8, 64 of
+// 1000 to 2000 41.7 -> 38.3, 16 of 1024 to 4096 25.0 -> 32.4.
 bool one_workgroup_a_pair(const AttnArgs& a, int64_t pairs, int64_t cus)
 {
-    const int64_t size = (int64_t)a.max_ctx * (a.c.d + 64), line = a.c.dtype == AG_BF16 ? 320000 : 230000;
-    return pairs <= cus && a.max_ctx <= kDirectMaxTokens && 4 * size <= (2 * pairs > cus ? 5 : 4) * line;
+    const int64_t size = (int64_t)a.max_ctx * (a.c.d + 64), line = a.c.dtype == AG_BF16 ? 400000 : 290000;
+    return pairs <= kDirectMaxPairs && a.max_ctx <= kDirectMaxTokens && 8 * size <= (2 * pairs > cus ? 8 : 5) * line;
 }
 
 }  // namespace

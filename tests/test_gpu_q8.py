@@ -17,7 +17,7 @@ import torch
 import q8_oracle as Q
 from gpu_helpers import i32
 from paper_2603_10342_amd import binding as B
-from test_q8_dispatch import FOUR_LENS, TILED
+from test_q8_dispatch import FOUR_LENS, SHARED_CTX, TILED
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -112,8 +112,10 @@ def decode(side, q, hq, scale, ctx=None, max_ctx=None, ws_fill=float("nan"), str
     ws = torch.full((nbytes // 4,), ws_fill, dtype=torch.float32, device=DEV)
     out = torch.full((len(ctx), hq, side.d), float("nan"), dtype=TD[side.dtype], device=DEV)
     args = side.dev(q), i32(ctx)
+    pages = max(side.bt.shape[1], -(-max_ctx // side.page))          # a larger bound than there are tokens: pages that no session has
+    bt = i32(np.pad(side.bt, ((0, 0), (0, pages - side.bt.shape[1]))))
     torch.cuda.synchronize()
-    B.ag_attn_decode_q8(side.cache, args[0], out, side.bt_dev, args[1], max_ctx, hq, scale, ws, stream)
+    B.ag_attn_decode_q8(side.cache, args[0], out, bt, args[1], max_ctx, hq, scale, ws, stream)
     torch.cuda.synchronize()
     return out
 
@@ -250,14 +252,14 @@ def few_cus():
 @pytest.mark.parametrize("d,page", GEOMETRIES)
 def test_decode(few_cus, dtype, d, page):
     """Contexts of none, one and every few tokens around the ends of groups, pages, steps and shares; stale slots are NaN under infinite powers.
-    One workgroup a pair, and on few CUs shares (test_q8_dispatch.py)."""
+    One workgroup a pair, and with a larger bound shares (test_q8_dispatch.py), also on few CUs, where they are longer."""
     ctx = [0, 1, 15, 16, 17, 63, 64, 65, 0, 127, 200, 513, 1100]
     side = Side(dtype, d, page, 2, ctx, seed=d)
     side.append(ctx)
     hq = 8
     q = side.draw(len(ctx), hq, d)
-    for stream in (None, few_cus):
-        check_decode(side, q, decode(side, q, hq, d ** -0.5, stream=stream), d ** -0.5, (dtype, d, page))
+    for max_ctx, stream in ((None, None), (SHARED_CTX, None), (SHARED_CTX, few_cus)):
+        check_decode(side, q, decode(side, q, hq, d ** -0.5, max_ctx=max_ctx, stream=stream), d ** -0.5, (dtype, d, page))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -267,8 +269,8 @@ def test_decode_groups(few_cus, dtype, hq, hkv):
     side = Side(dtype, 128, 16, hkv, ctx, seed=hq)
     side.append(ctx)
     q = side.draw(len(ctx), hq, 128)
-    for stream in (None, few_cus):
-        check_decode(side, q, decode(side, q, hq, 0.11, max_ctx=16 * side.bt.shape[1], stream=stream), 0.11, (hq, hkv))
+    for max_ctx, stream in ((None, None), (SHARED_CTX, None), (SHARED_CTX, few_cus)):
+        check_decode(side, q, decode(side, q, hq, 0.11, max_ctx=max_ctx, stream=stream), 0.11, (hq, hkv))
 
 
 def test_decode_of_many_sessions_and_of_a_long_one():
@@ -277,8 +279,7 @@ def test_decode_of_many_sessions_and_of_a_long_one():
     side = Side("bf16", 64, 16, 1, ctx)
     side.append(ctx)
     q = side.draw(len(ctx), 4, 64)
-    for max_ctx in (None, 3200):                                  # one workgroup a pair, and shares
-        side.bt_dev = i32(np.pad(side.bt, ((0, 0), (0, 200 - side.bt.shape[1]))))
+    for max_ctx in (None, SHARED_CTX):                            # one workgroup a pair, and shares
         check_decode(side, q, decode(side, q, 4, 0.125, max_ctx=max_ctx), 0.125, "many")
     side = Side("bf16", 128, 16, 2, [20000])
     side.append([20000])

@@ -61,11 +61,15 @@ def test_tiles_of_the_gpu_tests(tmp, dtype, d, page):
             assert k[0] == WIDE, k
 
 
+SHARED_CTX = 6400                                                 # the bound on contexts at which the GPU tests' decodes take shares, whatever their geometry
+
+
 @pytest.mark.parametrize("alone,batches", [
-    (True, [dict(batch=1, new=1000), dict(batch=8, new=1600), dict(batch=32, new=2000), dict(batch=1, new=1000, dtype="f32"), dict(batch=1, new=2400, d=64), dict(batch=1, new=900, d=256),
-            dict(batch=13, new=1100, hq=8, hkv=2), dict(batch=10, new=704, hq=40, hkv=2), dict(batch=150, new=90, d=64, hq=4, hkv=1)]),
-    (False, [dict(batch=1, new=1700), dict(batch=32, new=2100), dict(batch=33, new=64), dict(batch=1, new=1300, dtype="f32"), dict(batch=1, new=2700, d=64), dict(batch=64, new=4096),
-             dict(batch=13, new=1100, hq=8, hkv=2, cus=8), dict(batch=10, new=704, hq=1, hkv=1, cus=8), dict(batch=150, new=3200, d=64, hq=4, hkv=1)]),
+    (True, [dict(batch=1, new=1000), dict(batch=17, new=2000), dict(batch=64, new=2000), dict(batch=256, new=512), dict(batch=1, new=900, dtype="f32"), dict(batch=1, new=1900, d=64),
+            dict(batch=64, new=1250, d=256), dict(batch=13, new=1100, hq=8, hkv=2), dict(batch=10, new=704, hq=40, hkv=2), dict(batch=150, new=90, d=64, hq=4, hkv=1)]),
+    (False, [dict(batch=1, new=1600), dict(batch=17, new=2400), dict(batch=64, new=4096), dict(batch=1, new=1000, dtype="f32"), dict(batch=16, new=2400, dtype="f32"), dict(batch=1, new=2400, d=64),
+             dict(batch=1, new=900, d=256), dict(batch=13, new=SHARED_CTX, hq=8, hkv=2), dict(batch=10, new=SHARED_CTX, hq=1, hkv=1), dict(batch=150, new=SHARED_CTX, d=64, hq=4, hkv=1),
+             *(dict(batch=13, new=SHARED_CTX, hq=8, hkv=2, d=d) for d in (16, 48, 64, 96, 112, 208, 240, 256))]),
 ])
 def test_decode(tmp, alone, batches):
     for b, k in zip(batches, kernels(tmp, *(dict(call="decode", **b) for b in batches))):
