@@ -1,4 +1,4 @@
-// Cold and resume prefill over the 8-bit paged KV cache: causal attention of ragged chunks behind cached prefixes, any group
+// Cold and resume prefill over the 8-bit paged KV cache, bf16: causal attention of ragged chunks behind cached prefixes, any group
 // size, head_dim a multiple of 16 up to 256.
 //
 // A dense contraction, bound by the matrix cores.  A workgroup of NW waves owns 32 * NW columns of one (session, KV head), a
@@ -11,7 +11,7 @@
 //   in registers, converted and written to LDS; P(t) side by side with O += V(t - 1) P(t - 1); barrier.
 // The conversions - 40 vector instructions a wave and tile at NW = 8 and 128 channels, beside 100 of the softmax - so run while the vector units
 // have nothing else; ahead of the products eight prompts of 4096 tokens took 1222 us, so 1134 (970 TFLOP/s; over a bf16 cache 1120).
-// bf16 activations: weights rounded to bf16 for the value product; fp32: queries and weights as three bf16 terms.
+// Weights are rounded to bf16 for the value product, as over a bf16 cache.  fp32 activations, and few rows, take attn_split_q8.hip (split_preferred()).
 #include <algorithm>
 #include <atomic>
 
@@ -31,10 +31,9 @@ using tile32::tile_bytes;
 // two key and two value tiles
 constexpr int lds_bytes(int dt) { return 4 * tile_bytes(dt); }
 
-// S^T tile = K tile . Q^T with queries in terms, smallest first.  Vector units have nothing to do meanwhile: between(i) of DT / 8
-// runs behind product i.
-template <int DT, int kTerms, class Between>
-__device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q)[DT / 16][kTerms], f32x16 (&sc)[2], Between between)
+// S^T tile = K tile . Q^T, as tile32::qk_tile.  Vector units have nothing to do meanwhile: between(i) of DT / 8 runs behind product i.
+template <int DT, class Between>
+__device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q)[DT / 16], f32x16 (&sc)[2], Between between)
 {
     constexpr int kAhead = tile32::kOperandsAhead, kN = DT / 8;
     bf16x8 opnd[kAhead + 1];
@@ -45,19 +44,15 @@ __device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
         if (i + kAhead < kN) opnd[(i + kAhead) % (kAhead + 1)] = *reinterpret_cast<const bf16x8*>(operand(i + kAhead));
-#pragma unroll
-        for (int t = kTerms - 1; t >= 0; --t)
-            sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opnd[i % (kAhead + 1)], q[i >> 1][t], i < 2 && t == kTerms - 1 ? zero : sc[i & 1], 0, 0, 0);
+        sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opnd[i % (kAhead + 1)], q[i >> 1], i < 2 ? zero : sc[i & 1], 0, 0, 0);
         between(i);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-template <typename A, int NW, int DT, bool kExact>
-__global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void prefill_q8_kernel(Args x, Deal deal)
+template <int NW, int DT, bool kExact>
+__global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(Args x, Deal deal)
 {
-    constexpr int kTerms = terms_of<A>();
-    constexpr bool kLo = kTerms > 1;
     constexpr int kCols = 32 * NW, kTile = tile_bytes(DT);
     constexpr int kWavesPerGroup = NW / 4, kPer = DT / 64 / kWavesPerGroup;       // 16-byte pieces of a lane for a K tile, and for a V tile
     static_assert(kPer >= 1, "a wave brings whole pieces");
@@ -152,13 +147,13 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
     request_k(0, __builtin_amdgcn_readlane(ids, my_grp), rb);
 
     // ---- Q^T as B operand: column n, k-step ks covers channels ks * 16 + hi * 8 .. + 7 ----
-    bf16x8 qf[DT / 16][kTerms];
+    bf16x8 qf[DT / 16];
     {
-        const A* qp = (const A*)a.q + row * D + hi * 8;
+        const __bf16* qp = (const __bf16*)a.q + row * D + hi * 8;
 #pragma unroll
         for (int ks = 0; ks < DT / 16; ++ks) {
-            if (kExact || ks < chunks) to_terms(qp + ks * 16, qf[ks]);
-            else no_terms(qf[ks]);
+            qf[ks] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            if (kExact || ks < chunks) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
         }
     }
     const float sl2 = a.scale * tile32::kLog2e;
@@ -184,9 +179,9 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
 
     const unsigned char* const k_lane = lds + n * 16 + hi * 1024;
     const unsigned char* const v_lane = lds + 2 * kTile + n * 16 + hi * (DT * 16);
-    Weights<kLo> pa, pb;
+    Weights<false> pa, pb;
     // Requests past the last tile repeat it; what they bring is written to a place that nobody reads.
-    auto iter = [&](int t, Weights<kLo>& p_prev, Weights<kLo>& p_cur, Raw& now, Raw& next) {
+    auto iter = [&](int t, Weights<false>& p_prev, Weights<false>& p_cur, Raw& now, Raw& next) {
         const int tk = min(t + 2, n_tiles - 1);
         request_v(min(t + 1, n_tiles - 1), page, next);
         if (((t + 2) & 15) == 0) {                                            // K(t + 2) is the next window's first
@@ -203,7 +198,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
         begin_put(t, now, put);
         if (do_sm) {
             constexpr int kSteps = DT / 8;
-            scores<DT, kTerms>(kb, qf, sc, [&](int i) {
+            scores<DT>(kb, qf, sc, [&](int i) {
 #pragma unroll
                 for (int unit = i * kUnits / kSteps; unit < (i + 1) * kUnits / kSteps; ++unit) put_unit(unit, t, now, put);
             });
@@ -223,7 +218,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
 #pragma unroll
             for (int unit = 0; unit < kUnits; ++unit) put_unit(unit, t, now, put);
         }
-        tile32::softmax_and_value_product<DT, kLo>(do_sm, do_pv, vb, sc, sl2, m, lsum, p_prev, p_cur, o);
+        tile32::softmax_and_value_product<DT, false>(do_sm, do_pv, vb, sc, sl2, m, lsum, p_prev, p_cur, o);
         __syncthreads();
     };
 #pragma unroll 1
@@ -236,18 +231,17 @@ __global__ __launch_bounds__(64 * NW, DT > 128 || sizeof(A) == 4 ? 1 : 2) void p
     lsum += __shfl_xor(lsum, 32);
     const float inv = 1.0f / lsum;
     if (n < cols_w) {
-        A* out = (A*)a.out + row * D + hi * 4;
-        typedef A quad __attribute__((ext_vector_type(4)));
+        __bf16* out = (__bf16*)a.out + row * D + hi * 4;
 #pragma unroll
         for (int mb = 0; mb < DT / 32; ++mb)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
                 const int d = mb * 32 + q4 * 8;
                 if (!kExact && d >= D) break;
-                quad y;
+                tile32::bf16x4 y;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = (A)(o[mb][q4 * 4 + e] * inv);
-                *reinterpret_cast<quad*>(out + d) = y;
+                for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[mb][q4 * 4 + e] * inv);
+                *reinterpret_cast<tile32::bf16x4*>(out + d) = y;
             }
     }
 }
@@ -259,13 +253,13 @@ int64_t tiles_bound(const AttnArgs& a, int cols)
     return std::min<int64_t>((int64_t)a.total_rows * G / cols + a.batch, (int64_t)a.batch * ((a.max_new * G + cols - 1) / cols));
 }
 
-template <typename A, int NW, int DT, bool kExact>
+template <int NW, int DT, bool kExact>
 ag_status launch(const Args& x, hipStream_t st)
 {
     constexpr int lds = lds_bytes(DT);
     if constexpr (lds > 64 * 1024) {
         static std::atomic<uint64_t> told{0};
-        ag_status e = allow_dynamic_lds((const void*)prefill_q8_kernel<A, NW, DT, kExact>, lds, told);
+        ag_status e = allow_dynamic_lds((const void*)prefill_q8_kernel<NW, DT, kExact>, lds, told);
         if (e) return e;
     }
     const AttnArgs& a = x.a;
@@ -275,26 +269,30 @@ ag_status launch(const Args& x, hipStream_t st)
     }
     const Deal deal = deal_of(a, tiles_bound(a, 32 * NW), std::max(1, stream_cus(st) * (8 / NW) / 8));
     prof_before(st);
-    hipLaunchKernelGGL((prefill_q8_kernel<A, NW, DT, kExact>), dim3((unsigned)workgroups_of(deal)), dim3(64 * NW), lds, st, x, deal);
+    hipLaunchKernelGGL((prefill_q8_kernel<NW, DT, kExact>), dim3((unsigned)workgroups_of(deal)), dim3(64 * NW), lds, st, x, deal);
     prof_after(st);
     return hip_check(hipGetLastError(), "prefill launch");
 }
 
 // Few rows on long contexts: the keys of 32 columns dealt to the waves of a workgroup (attn_split_q8.hip) instead of whole tiles, each a chain
 // of all of them.  A launch is as long as a chain, or as many as a CU's workgroups come to, and a chain is a start and its share of the
-// context; in units of what a context token costs eight waves: 1500 + L, of four 1500 + 2.1 L with two workgroups a CU, of tiles 1500 + 4.5 L;
-// with one wave a SIMD (past 128 channels) of four 1500 + 2.1 L and of tiles 1500 + 7 L, one workgroup a CU, as tiles of fp32 always.  Graph replay, 32 / 8
-// heads x 128 unless said otherwise, tiles -> split, us (workgroups of 32 columns): one chunk on 6007 tokens of 50 rows (56) 128 -> 32, 211 (216) 133 -> 34, 400 (400) 136
-// -> 66, 1000 (1000) 150 -> 152; on 2000 of 300 (304) 53 -> 27, 1000 72 -> 75; 16 of 30 on 600 (512) 20.4 -> 12.6; 8 of 50..300 on 2000..4000 (1328) 105 -> 124; prompts: 4 of
-// 100 (416) 9.8 -> 7.0, 3 of 250 (768) 13.0 -> 13.1, one of 500 (504) 17.8 -> 9.7; x 64: 211 on 6007 100 -> 26, 3 prompts of 250 9.9 -> 8.3; x 256: 8 of 50..300 on 500..1000 (1328)
-// 91 -> 101; fp32: 211 on 6007 235 -> 66, 8 prompts of 300..1500 (8000) 266 -> 373, x 64 6 of 20..300 on 100..2000 (784) 55 -> 32.
+// context; in units of what a context token costs eight waves: 1500 + L, of four 1500 + 2.1 L with two workgroups a CU (three to 64 channels), of tiles 1500 + 4.5 L;
+// past 128 channels, one workgroup of one wave a SIMD a CU, of four 1500 + 2.1 L and of tiles 1500 + 9 L.  Of several sessions, where more than one round
+// evens them out, the mean context is taken for three quarters of the longest.  Graph replay, 32 / 8 heads x 128 unless said otherwise, tiles -> split, us
+// (workgroups of 32 columns): one chunk on 6007 tokens of 50 rows (56) 128 -> 32, 211 (216) 133 -> 34, 400 (400) 136 -> 66, 1000 (1000) 150 -> 152; on 2000 of 300 (304) 53 ->
+// 27, 1000 72 -> 75; 16 of 30 on 600 (512) 20.4 -> 12.6; 8 of 50..300 on 2000..4000 (1328) 106 -> 100, of 100..200 on 500..1000 (1184) 36 -> 34; 16 of 50..100 on 100..300
+// (1248) 19.5 -> 22.1; prompts: 4 of 100 (416) 9.8 -> 7.0, 3 of 250 (768) 13.0 -> 13.1, one of 500 (504) 17.8 -> 9.7, 16 of 200..600 (6568) 58 -> 96; x 64: 211 on 6007 100 -> 26, 8 of
+// 50..300 on 2000..4000 73 -> 65, 16 prompts of 200..600 41 -> 50; x 256: 8 of 50..300 on 2000..4000 231 -> 230, 4 of them (696) 161 -> 133, 16 prompts of 200..600 144 -> 240.
+// fp32 always: tiles with their queries and weights in three terms have one wave a SIMD, and 256 channels spill (eight prompts of 2000 rows x 64 497 -> 457, x 128 782 ->
+// 781, x 256 2560 -> 1804; 8 of 100..200 on 500..1000 50 -> 37, 76 -> 59, 225 -> 129).
 bool split_preferred(const AttnArgs& a, hipStream_t st)
 {
-    const bool fp32 = a.c.dtype == AG_F32, wide = a.c.d > 128;
-    const double cus = stream_cus(st), heads = a.c.hkv, ctx = a.max_ctx;
-    const double few = heads * (double)tiles_bound(a, 32), whole = heads * (double)tiles_bound(a, 128);
-    const double split = !wide && few <= cus ? 1500 + ctx : std::max(1.0, few / (wide ? cus : 2 * cus)) * (1500 + 2.1 * ctx);
-    const double tiles = std::max(1.0, whole / (wide || fp32 ? cus : 2 * cus)) * (1500 + (wide ? 7.0 : 4.5) * ctx);
+    if (a.c.dtype == AG_F32) return true;
+    const bool wide = a.c.d > 128;
+    const double cus = stream_cus(st), slots = wide ? cus : 2 * cus, few_slots = a.c.d <= 64 ? 3 * cus : slots, heads = a.c.hkv, ctx = a.max_ctx, mean = a.batch > 1 ? 0.75 * ctx : ctx;
+    const double few = heads * (double)tiles_bound(a, 32), whole = heads * (double)tiles_bound(a, 128), step = wide ? 9.0 : 4.5;
+    const double split = !wide && few <= cus ? 1500 + ctx : few <= few_slots ? 1500 + 2.1 * ctx : few / few_slots * (1500 + 2.1 * mean);
+    const double tiles = whole <= slots ? 1500 + step * ctx : whole / slots * (1500 + step * mean);
     return split < tiles;
 }
 
@@ -309,22 +307,16 @@ bool wide_workgroups(const AttnArgs& a, hipStream_t st)
     return ctx > 1536 && (large >= 2 * cus || (large >= cus && ctx >= 2 * (int64_t)a.max_new));
 }
 
-template <typename A>
-ag_status launch_typed(const Args& x, hipStream_t st)
-{
-    const int d = x.a.c.d;
-    if (sizeof(A) == 2 && d == 128 && wide_workgroups(x.a, st)) return launch<__bf16, 8, 128, true>(x, st);
-    return d == 64 ? launch<A, 4, 64, true>(x, st) : d < 64 ? launch<A, 4, 64, false>(x, st)
-         : d == 128 ? launch<A, 4, 128, true>(x, st) : d < 128 ? launch<A, 4, 128, false>(x, st)
-         : d == 256 ? launch<A, 4, 256, true>(x, st) : launch<A, 4, 256, false>(x, st);
-}
-
 }  // namespace
 
 ag_status launch_prefill(const Args& x, hipStream_t st)
 {
     if (split_preferred(x.a, st)) return launch_prefill_split(x, st);
-    return x.a.c.dtype == AG_BF16 ? launch_typed<__bf16>(x, st) : launch_typed<float>(x, st);
+    const int d = x.a.c.d;
+    if (d == 128 && wide_workgroups(x.a, st)) return launch<8, 128, true>(x, st);
+    return d == 64 ? launch<4, 64, true>(x, st) : d < 64 ? launch<4, 64, false>(x, st)
+         : d == 128 ? launch<4, 128, true>(x, st) : d < 128 ? launch<4, 128, false>(x, st)
+         : d == 256 ? launch<4, 256, true>(x, st) : launch<4, 256, false>(x, st);
 }
 
 }  // namespace q8

@@ -1,4 +1,4 @@
-// Prefill of few rows over the 8-bit paged KV cache: the keys of 32 columns - (token, query head of the group) pairs of one (session, KV
+// Prefill of few rows over the 8-bit paged KV cache, and of any number with fp32 activations: the keys of 32 columns - (token, query head of the group) pairs of one (session, KV
 // head) - are dealt to the waves of one workgroup, whose sums meet in LDS.
 //
 // A chunk of a few hundred rows on a long context makes few workgroups of whole tiles, each a chain of as many key tiles as the context has
@@ -291,7 +291,13 @@ ag_status launch(const Args& x, hipStream_t st)
 // Eight waves a workgroup and one workgroup a CU, or four and two: a chain is half as long, or there is room for twice as many, and on
 // short contexts less to start and to add up.  Graph replay, eight -> four, us (workgroups): 211 rows on 6007 tokens (216) 34.6 -> 37.2, x 64 25.7 -> 30.5, fp32
 // 65.7 -> 73.8, x 64 43.4 -> 46.0; 400 on 6007 (400) 75 -> 66, 500 rows (504) 13.5 -> 9.7, 16 of 30 on 600 (512) 17.0 -> 12.6, fp32 25.3 -> 20.5, x 64 18.4 -> 13.7; 8 of 30 on 100 (256) 6.6 -> 6.1.
-bool four_waves(const AttnArgs& a, hipStream_t st) { return a.c.hkv * tiles_bound(a) > stream_cus(st) || a.max_ctx <= 256; }
+// Of several sessions on long contexts the longest make the launch, and half as many again still gain from eight: 6 of 180..305 rows on 110..6229 at 6 / 2
+// heads x 64 (294) 27.7 -> 40, 11 of 27..286 on 472..7169 x 128 (314) 45 -> 66.
+bool four_waves(const AttnArgs& a, hipStream_t st)
+{
+    const int64_t few = a.c.hkv * tiles_bound(a), cus = stream_cus(st);
+    return a.max_ctx <= 256 || 2 * few > (a.batch > 1 && a.max_ctx >= 2000 ? 3 : 2) * cus;
+}
 
 template <typename A, int DT, bool kExact>
 ag_status launch_waves(const Args& x, hipStream_t st)

@@ -14,16 +14,16 @@ def kernels(tmp, *calls):
     return [[l.split(" ")[0].replace("q8::", "") for l in r] for r in launched(calls, tmp)]
 
 
-SPLIT, TILES, WIDE = "prefill_q8_split_kernel<", "prefill_q8_kernel<__bf16,4", "prefill_q8_kernel<__bf16,8,128,true>"
+SPLIT, TILES, WIDE = "prefill_q8_split_kernel<", "prefill_q8_kernel<4,", "prefill_q8_kernel<8,128,true>"
 
 
 @pytest.mark.parametrize("want,batches", [
     (SPLIT, [dict(batch=1, prefix=6007, new=211), dict(batch=1, prefix=6007, new=600), dict(batch=1, prefix=2000, new=211), dict(batch=16, prefix=600, new=30),
              dict(batch=1, prefix=6007, new=211, dtype="f32"), dict(batch=6, total=784, max_new=300, max_ctx=2300, d=64, page=32, dtype="f32"),
-             dict(batch=4, prefix=2000, new=16, hq=24, hkv=1)]),
-    (TILES, [dict(batch=1, prefix=2000, new=1000), dict(batch=16, new=50), dict(batch=1, new=1000), dict(batch=8, new=512), dict(batch=64, new=600), dict(batch=1, new=2048)]),
+             dict(batch=4, prefix=2000, new=16, hq=24, hkv=1), dict(batch=8, new=1500, dtype="f32"), dict(batch=8, total=1300, max_new=300, max_ctx=4300, d=64), dict(batch=4, total=690, max_new=300, max_ctx=4300, d=256)]),
+    (TILES, [dict(batch=1, prefix=2000, new=1000), dict(batch=16, new=50), dict(batch=1, new=1000), dict(batch=8, new=512), dict(batch=64, new=600), dict(batch=1, new=2048), dict(batch=16, total=1200, max_new=100, max_ctx=400), dict(batch=16, total=6500, max_new=600, max_ctx=600, d=64),
+             dict(batch=16, total=6500, max_new=600, max_ctx=600, d=256)]),
     (WIDE, [dict(batch=8, new=4096), dict(batch=2, prefix=2000, new=1000), dict(batch=32, prefix=3000, new=200)]),
-    ("prefill_q8_kernel<float,4,128,true>", [dict(batch=8, new=1500, dtype="f32")]),
 ])
 def test_prefill(tmp, want, batches):
     for b, k in zip(batches, kernels(tmp, *(dict(call="resume", **b) for b in batches))):
@@ -42,6 +42,7 @@ def tiled(name, **more):
 def test_waves_of_a_split_workgroup(tmp):
     """Eight up to one workgroup a CU and past 256 tokens, where two waves a SIMD fit; the last is the GPU test's."""
     for b, w in [(dict(batch=1, prefix=6007, new=211), 8), (dict(batch=1, prefix=6007, new=400), 4), (dict(batch=8, prefix=100, new=30), 4), (dict(batch=8, prefix=300, new=30), 8),
+                 (dict(batch=11, total=1100, max_new=286, max_ctx=7400, hq=6, hkv=2), 8), (dict(batch=1, prefix=2000, new=300), 4),
                  (dict(batch=1, prefix=6007, new=211, d=256), 4), (dict(batch=1, prefix=6007, new=211, dtype="f32"), 8), (dict(batch=1, prefix=6007, new=211, dtype="f32", d=64), 8),
                  (dict(FOUR, d=128), 4), (dict(FOUR, d=64, dtype="f32"), 4)]:
         (k,) = kernels(tmp, dict(call="resume", **b))
@@ -52,12 +53,11 @@ FOUR_LENS = ([900, 17], [20, 5])                                  # prefix, new;
 FOUR = dict(batch=2, total=25, max_new=20, max_ctx=920, hq=16, hkv=2, cus=8)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,page", [(128, 16), (128, 64), (64, 32), (256, 16), (48, 128), (96, 32), (208, 256)])
-def test_tiles_of_the_gpu_tests(tmp, dtype, d, page):
-    for name, k in zip(TILED, kernels(tmp, *(tiled(name, dtype=dtype, d=d, page=page, hq=16, hkv=2) for name in TILED))):
+def test_tiles_of_the_gpu_tests(tmp, d, page):
+    for name, k in zip(TILED, kernels(tmp, *(tiled(name, d=d, page=page, hq=16, hkv=2) for name in TILED))):
         assert k[0].startswith("prefill_q8_kernel<"), (name, k)
-        if dtype == "bf16" and d == 128 and name == "long":
+        if d == 128 and name == "long":
             assert k[0] == WIDE, k
 
 
