@@ -74,6 +74,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
     const int n_tiles = (P + columns.token(cols - 1)) / BN + 1;               // tiles the workgroup stages
     const int wave_tiles = cols_w > 0 ? (P + columns.token(32 * w + cols_w - 1)) / BN + 1 : 0;      // tiles this wave uses
     const int first_masked = (P + columns.token(32 * w) + 1) / BN;            // first tile holding a key this wave's first column may not see
+    constexpr int kDiagonal = kCols / BN + 1;                                 // only the workgroup's last ones can hold a key that some column may not see
     const int col = min(32 * w + n, cols - 1);                                // columns beyond the tile repeat the last one
     const int token = columns.token(col), head = columns.head(col, token);
     const int qpos = P + token;
@@ -118,15 +119,20 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
     unsigned char* const k_put = lds + (my_grp * 16 + key) * 16;
     unsigned char* const v_put = lds + 2 * kTile + my_grp * (DT * 32);
     struct Put { float e[16]; u32x4 y; };                                     // the values' powers, a piece in the making
+    bool noted = false;                                                      // NaN among the values that this wave brought in
     auto begin_put = [&](int t, Raw& x8, Put& p) {
-        const int keep = ctx - (t * BN + my_grp * 16);       // slots behind the last token may hold anything, NaN included: zeros
-        if (keep < 16) {                                     // uniform
+        const int keep = ctx - (t * BN + my_grp * 16);
+        if (t + kDiagonal >= n_tiles) {                      // uniform
             asm volatile("");                                // (a branch, not a select for every word)
-            x8.ve = keep_bytes(x8.ve, keep - 4 * (lane & 3));            // (a byte of zero is a power of zero: a stale one may be an infinity)
+            if (keep < 16) {                                 // slots behind the last token may hold anything, NaN included: zeros
+                asm volatile("");
+                x8.ve = keep_bytes(x8.ve, keep - 4 * (lane & 3));        // (a byte of zero is a power of zero: a stale one may be an infinity)
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
+                for (int i = 0; i < kPer; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x8.v[i][k] = keep_bytes(x8.v[i][k], keep - 4 * k);
+                    for (int k = 0; k < 4; ++k) x8.v[i][k] = keep_bytes(x8.v[i][k], keep - 4 * k);
+            }
+            noted |= take_nan_out(x8.v);                     // (nan_to_those_that_see_it())
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) p.e[i] = power(((uint32_t)__builtin_amdgcn_readlane((int)x8.ve, i >> 2) >> (8 * (i & 3))) & 0xFFu);
@@ -226,6 +232,14 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
         iter(t, pb, pa, ra, rb);
         if (t + 1 <= n_tiles) iter(t + 1, pa, pb, rb, ra);
     }
+
+    uint32_t* const s_noted = reinterpret_cast<uint32_t*>(lds);               // (the tiles are done with)
+    if (lane == 0) s_noted[w] = noted;
+    __syncthreads();
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) any |= s_noted[i];
+    if (any != 0 && cols_w > 0) nan_to_those_that_see_it<DT / 32>(a, find, s, max(n_tiles - kDiagonal, 0) * BN, P + columns.token(32 * w + cols_w - 1), qpos, hi, o);
 
     // o[mb][q4 * 4 + e] is O^T[channel mb * 32 + q4 * 8 + hi * 4 + e][column n]
     lsum += __shfl_xor(lsum, 32);

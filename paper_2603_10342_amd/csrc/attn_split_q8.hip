@@ -133,6 +133,7 @@ __global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_spl
             ve = *reinterpret_cast<const u32x4*>(exps_at(x.exps, hi ? p.b.exps : p.a.exps) + ps);
         };
         const float sl2 = a.scale * kLog2e;
+        bool noted = false;                                                   // uniform
         Ids ids = ids_of(0);
         Places at = places_of(0, ids);
         load_k(at);
@@ -174,6 +175,7 @@ __global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_spl
                 for (int mb = 0; mb < kV; ++mb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[mb][i] = keep_bytes(v[mb][i], ctx - tok0 - 4 * i);
+                noted |= take_nan_out(v);                    // (nan_to_those_that_see_it())
             }
             float mx = sc[0];
 #pragma unroll
@@ -214,6 +216,10 @@ __global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_spl
             load_v(at);
             ids = ids_of(st + 2);
             __builtin_amdgcn_sched_barrier(0);
+        }
+        if (noted) {
+            const int last = min((u0 + my_n) * kTok - 1, P + columns.token(cols - 1));
+            nan_to_those_that_see_it<kV>(a, find, s, max(u0, first_masked) * kTok, last, qpos, hi, o);
         }
     }
     lsum += __shfl_xor(lsum, 32);

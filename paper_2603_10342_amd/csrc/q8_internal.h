@@ -90,6 +90,27 @@ __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int keep)
     return keep >= 4 ? w : keep <= 0 ? 0u : w & ((1u << (8 * keep)) - 1u);
 }
 
+// NaN has the largest byte of either sign.  Whether one of the wave's words has one - then those bytes become zeros.
+template <int N>
+__device__ __forceinline__ bool take_nan_out(u32x4 (&x)[N])
+{
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) any |= (x[i][k] & 0x7F7F7F7Fu) + 0x01010101u;          // (no byte carries)
+    if (__builtin_amdgcn_ballot_w64((any & 0x80808080u) != 0) == 0) return false;
+    asm volatile("");                                                                      // (a branch)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t nan = ((x[i][k] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+            x[i][k] &= ~((nan << 1) - (nan >> 7));
+        }
+    return true;
+}
+
 // Numbers of the activations' type, or their arithmetic's, as bf16 terms: operands of the products.  One term rounds.
 template <typename A>
 constexpr int terms_of() { return sizeof(A) == 4 ? 3 : 1; }
@@ -136,6 +157,29 @@ struct Finder {
 };
 __device__ __forceinline__ const uint8_t* data_at(const void* pool, uint32_t data) { return (const uint8_t*)pool + ((uint64_t)data << 8); }
 __device__ __forceinline__ const uint8_t* exps_at(const uint8_t* exps, uint32_t at) { return exps + ((uint64_t)at << 4); }
+
+// A weight of zero does not hide a NaN.  Where some of a workgroup's columns do not see a tile whole, prefill takes NaN among its values as
+// zeros and afterwards, if there was one, this takes them to the columns that do see them, byte by byte: tokens first .. last of session s,
+// o[mb][i] being channel mb * 32 + (i / 4) * 8 + hi * 4 + i % 4 of the lane's column, which sees positions up to qpos.
+template <int kMb, class O>
+__device__ __forceinline__ void nan_to_those_that_see_it(const AttnArgs& a, const Finder& find, int s, int first, int last, int qpos, int hi, O (&o)[kMb])
+{
+#pragma unroll 1
+    for (int at = first; at <= last; ++at) {
+        const Where w = find.at(a.bt[(int64_t)s * a.max_pages + (at >> a.c.ps_shift)], (at & (a.c.ps - 1)) >> 4);
+        const uint8_t* vp = data_at(a.c.v, w.data) + (at & 15) + hi * 64;
+#pragma unroll
+        for (int mb = 0; mb < kMb; ++mb)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (mb * 32 + q * 8 >= a.c.d) break;             // (a branch also where the caller knows better: fewer loads in flight, fewer registers)
+#pragma unroll
+                for (int i = q * 4; i < q * 4 + 4; ++i)
+                    o[mb][i] = at <= qpos && (vp[(mb * 32 + q * 8 + (i & 3)) * 16] & 0x7F) == 0x7F ? __builtin_nanf("") : o[mb][i];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+}
 
 // K and V are read once by a decode step: the streaming hint
 __device__ __forceinline__ u32x4 stream16(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }

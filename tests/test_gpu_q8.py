@@ -392,6 +392,51 @@ def test_nan_and_infinities_stay_with_the_rows_that_see_them(few_cus, dtype):
     check(dtype, got[1:], q[1:2], side.k[1], side.v[1], 79, 0.125)
 
 
+def seeing(side, s, prefix, n, hq):
+    """[n][hq][d]: outputs that a value of session s that is not finite reaches."""
+    bad = ~np.isfinite(side.v[s])                                 # [context][hkv][d]
+    seen = np.cumsum(bad, 0)[prefix:prefix + n] > 0
+    return np.repeat(seen, hq // side.hkv, axis=1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", GEOMETRIES)
+@pytest.mark.parametrize("lens,few,hq,hkv", [*((n, True, 16, 2) for n in TILED), *((n, False, 16, 2) for n in NEW), ("four", True, 16, 2), ("ragged", True, 3, 3),
+                                             ("long", True, 2, 2), ("ragged", True, 48, 1)])
+def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(few_cus, dtype, d, page, lens, few, hq, hkv):
+    """In prefixes, at the first, the last and other new tokens, in one channel each; by whole tiles and by few rows (test_q8_dispatch.py)."""
+    prefix, new = (np.array(x) for x in {**NEW, **TILED, "four": FOUR_LENS}[lens])
+    side = Side(dtype, d, page, hkv, prefix + new, seed=d + hq)
+    if prefix.any():
+        side.append(prefix)
+    t, scale = int(new.sum()), d ** -0.5
+    v, at = side.draw(t, hkv, d), 0
+    for s, n in enumerate(new):
+        for i, x in ((0, np.inf), (n // 3, np.nan), (n // 2 + 1, -np.inf), (n - 1, np.inf)):
+            if 0 <= i < n and (s + i) % 3:
+                v[at + i, i % hkv, (5 * i + 11 * s + 3) % d] = x
+        at += n
+    side.append(new, v=v)
+    q = side.draw(t, hq, d)
+    got, at = resume(side, q, new, hq, scale, stream=few_cus if few else None).double().cpu().numpy(), 0
+    clean = [np.where(np.isfinite(x), x, 0) for x in side.v]
+    for s, n in enumerate(new):
+        if n:
+            o, p = got[at:at + n], int(prefix[s])
+            seen = seeing(side, s, p, n, hq)
+            assert np.array_equal(np.isnan(o), seen), (s, np.argwhere(np.isnan(o) != seen)[:5])
+            ref = Q.attend(q[at:at + n], side.k[s], clean[s], p, scale)[0]
+            check(dtype, np.where(seen, ref, o), q[at:at + n], side.k[s], clean[s], p, scale, (lens, s))
+        at += n
+    ctx = prefix + np.where(new > 0, new // 2 + 1, 0)
+    q1 = side.draw(len(new), hq, d)
+    for bound in (None, SHARED_CTX):
+        got = decode(side, q1, hq, scale, ctx=ctx, max_ctx=bound).double().cpu().numpy()
+        for s, n in enumerate(ctx):
+            if n:
+                assert np.array_equal(np.isnan(got[s]), seeing(side, s, n - 1, 1, hq)[0])
+
+
 def test_a_session_from_prompt_to_decode():
     """The operators together: prompt appended and attended, a tool's output behind it, then decode steps; read back and appended elsewhere,
     the same outputs to the bit."""
