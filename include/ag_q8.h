@@ -8,8 +8,8 @@
  *     e  = the least exponent with max |x| <= 448 * 2^e over the row's finite entries, kept in [-110, 119], stored as the byte e + 127
  *     x8 = e4m3(x * 2^-e), to nearest, ties to even; what is not finite is stored as NaN
  *     x^ = x8 * 2^e, which is what attention reads (a bf16 number, exactly)
- * An entry is off by at most 2^-4 of itself, or 2^-10 * 2^e where that is more (2^-18 of the row's largest).  Rows of zeros are
- * stored as zeros.  Magnitudes above 448 * 2^119 (0.875 of bf16's and fp32's range) are stored as that.
+ * An entry is off by at most 2^-4 of itself, or 2^-10 * 2^e where that is more (2^-17 of the row's largest, unless e is
+ * at its lowest).  Rows of zeros are stored as zeros.  Magnitudes above 448 * 2^119 (0.875 of bf16's and fp32's range) are stored as that.
  *
  * Conventions (pointers, streams, status codes, block tables, lengths, cu_new, GQA, order between append and attention) are
  * those of ag.h.  What differs:
@@ -24,6 +24,9 @@
  *   - Slots that no token uses may hold anything, NaN included: they are read, but nothing depends on them.
  *   - fp32 activations keep 32 bits in the products (queries and softmax weights as three bf16 terms); bf16 activations multiply
  *     weights rounded to bf16, as attention over a bf16 cache does.
+ *   - What is not finite in a key or a value reaches the rows that see its token, a value's in its own channel only, and no other row.
+ *   - Attention divides by the sum of its weights at the end: queries, keys and values whose rows' largest entries lie between 2^-60 and 2^90
+ *     keep the accuracy above whatever the context; smaller ones may lose their last bits, sums of larger ones may overflow.
  */
 #ifndef AG_Q8_H
 #define AG_Q8_H

@@ -437,6 +437,28 @@ def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(few_cus, dt
                 assert np.array_equal(np.isnan(got[s]), seeing(side, s, n - 1, 1, hq)[0])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_powers_of_two_change_no_bit(few_cus, dtype, d):
+    """Keys and queries by opposite powers, values by any in the documented range: every rounding is relative, so that the outputs are the
+    same but for the power (scores are small: no weight below 2^-20)."""
+    lens, new, hq, hkv, scale = [300, 77], [120, 77], 8, 2, d ** -0.5 / 4
+    outs = []
+    for kq, pv in ((0, 0), (40, 60), (-40, -60)):
+        side = Side(dtype, d, 16, hkv, lens, seed=3)
+        old = [n - m for n, m in zip(lens, new)]
+        for n in (old, new):
+            k, v = (side.draw(sum(n), hkv, d) for _ in range(2))
+            side.append(n, k=np.ldexp(k, kq).astype(np.float32), v=np.ldexp(v, pv).astype(np.float32))
+        q = np.ldexp(side.draw(sum(new), hq, d), -kq)
+        got = [resume(side, q, new, hq, scale), resume(side, q, new, hq, scale, stream=few_cus)]
+        got += [decode(side, q[:2], hq, scale), decode(side, q[:2], hq, scale, max_ctx=SHARED_CTX)]
+        outs.append([np.ldexp(x.double().cpu().numpy(), -pv) for x in got])
+    for other in outs[1:]:
+        for x, y in zip(outs[0], other):
+            assert np.array_equal(x, y)
+
+
 def test_a_session_from_prompt_to_decode():
     """The operators together: prompt appended and attended, a tool's output behind it, then decode steps; read back and appended elsewhere,
     the same outputs to the bit."""
