@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
     const int n_tiles = (P + columns.token(cols - 1)) / BN + 1;               // tiles the workgroup stages
     const int wave_tiles = cols_w > 0 ? (P + columns.token(32 * w + cols_w - 1)) / BN + 1 : 0;      // tiles this wave uses
     const int first_masked = (P + columns.token(32 * w) + 1) / BN;            // first tile holding a key this wave's first column may not see
-    constexpr int kDiagonal = kCols / BN + 1;                                 // only the workgroup's last ones can hold a key that some column may not see
+    const int diagonal = n_tiles - (P + columns.token(0) + 1) / BN;           // how many of the last may hold a key that some column does not see
     const int col = min(32 * w + n, cols - 1);                                // columns beyond the tile repeat the last one
     const int token = columns.token(col), head = columns.head(col, token);
     const int qpos = P + token;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
     bool noted = false;                                                      // NaN among the values that this wave brought in
     auto begin_put = [&](int t, Raw& x8, Put& p) {
         const int keep = ctx - (t * BN + my_grp * 16);
-        if (t + kDiagonal >= n_tiles) {                      // uniform
+        if (t + diagonal >= n_tiles) {                      // uniform
             asm volatile("");                                // (a branch, not a select for every word)
             if (keep < 16) {                                 // slots behind the last token may hold anything, NaN included: zeros
                 asm volatile("");
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
     uint32_t any = 0;
 #pragma unroll
     for (int i = 0; i < NW; ++i) any |= s_noted[i];
-    if (any != 0 && cols_w > 0) nan_to_those_that_see_it<DT / 32>(a, find, s, max(n_tiles - kDiagonal, 0) * BN, P + columns.token(32 * w + cols_w - 1), qpos, hi, o);
+    if (any != 0 && cols_w > 0) nan_to_those_that_see_it<DT / 32>(a, find, s, (n_tiles - diagonal) * BN, P + columns.token(32 * w + cols_w - 1), qpos, hi, o);
 
     // o[mb][q4 * 4 + e] is O^T[channel mb * 32 + q4 * 8 + hi * 4 + e][column n]
     lsum += __shfl_xor(lsum, 32);
