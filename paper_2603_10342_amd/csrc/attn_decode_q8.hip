@@ -205,7 +205,7 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
                 const int e = half * 8 + i;
                 p[i] = __builtin_amdgcn_exp2f(xs[e] - m_ref);
                 psum += p[i];
-                p[i] = !kLast || e < keep ? p[i] * power_of(ve, e) : 0.f;      // (a stale power may be an infinity)
+                p[i] = times_power(p[i], ve, e);
             }
             to_terms(p, w[half]);
         }

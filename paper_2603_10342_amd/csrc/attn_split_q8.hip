@@ -168,9 +168,7 @@ __global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_spl
                 asm volatile("");                            // (a branch)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[i] = tok0 + i <= qpos ? sc[i] : -INFINITY;
-                // slots behind the last token may hold anything, NaN included: zeros, under powers of zero
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ve[i] = keep_bytes(ve[i], ctx - tok0 - 4 * i);
+                // slots behind the last token may hold anything, NaN included: zeros
 #pragma unroll
                 for (int mb = 0; mb < kV; ++mb)
 #pragma unroll
@@ -203,7 +201,7 @@ __global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_spl
                 for (int i = 0; i < 8; ++i) {
                     p[i] = __builtin_amdgcn_exp2f(fmaf(sc[half * 8 + i], sl2, -m_ref));
                     psum += p[i];
-                    p[i] *= power_of(ve, half * 8 + i);
+                    p[i] = times_power(p[i], ve, half * 8 + i);
                 }
                 to_terms(p, wt[half]);
             }
