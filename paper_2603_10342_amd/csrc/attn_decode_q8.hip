@@ -48,12 +48,17 @@ __device__ __forceinline__ f32x4 product(const bf16x8& a, const bf16x8 (&b)[kTer
     return acc;
 }
 
+// 64-channel blocks of the keys: the last may be half a one, whose other half is read again, times zeros of the query
+constexpr int key_blocks(int dt) { return (dt + 63) / 64; }
+template <int DT, bool kExact>
+__device__ __forceinline__ int chunk_of(int h, int c, int chunks) { return kExact && DT % 64 == 0 ? 4 * h + c : min(4 * h + c, chunks - 1); }
+
 // fp32 queries are three operands for each of a bf16 one and stand in LDS, as the lanes take them: [block][half][term][lane].  In registers they
 // leave one wave a SIMD (16 sessions of 1024..4096 tokens, 32 / 8 heads x 128, 32.0 -> 25.4 us).
 template <typename A>
 constexpr bool queries_in_lds() { return sizeof(A) == 4; }
 template <typename A>
-constexpr int query_bytes(int dt) { return queries_in_lds<A>() ? dt / 64 * 2 * terms_of<A>() * 1024 : 0; }
+constexpr int query_bytes(int dt) { return queries_in_lds<A>() ? key_blocks(dt) * 2 * terms_of<A>() * 1024 : 0; }
 
 // The queries of heads h0 .. h0 + nh - 1 of (session s, KV head g) as B operands: column = head r, k = channels (4 h + c) * 16 + 8 half .. + 7,
 // lane = 16 c + r; zero beyond the heads and channels.
@@ -62,15 +67,15 @@ __device__ __forceinline__ void query(const AttnArgs& a, int s, int g, int h0, i
 {
     const int r = lane & 15, c = lane >> 4, D = kExact ? DT : a.c.d, chunks = D >> 4;
     const A* row = (const A*)a.q + ((int64_t)s * a.hq + (int64_t)g * (a.hq / a.c.hkv) + h0 + min(r, nh - 1)) * D;
-    to_terms(row + (kExact ? 4 * h + c : min(4 * h + c, chunks - 1)) * 16 + half * 8, q);
-    if (r >= nh || (!kExact && 4 * h + c >= chunks)) no_terms(q);
+    to_terms(row + chunk_of<DT, kExact>(h, c, chunks) * 16 + half * 8, q);
+    if (r >= nh || 4 * h + c >= chunks) no_terms(q);
 }
 template <typename A, int DT, bool kExact, int kWaves>
 __device__ __forceinline__ void queries_to_lds(const AttnArgs& a, int s, int g, int h0, int nh, unsigned char* s_q)
 {
     constexpr int kTerms = terms_of<A>();
     const int lane = threadIdx.x & 63;
-    for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < DT / 32; i += kWaves) {
+    for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < 2 * key_blocks(DT); i += kWaves) {
         bf16x8 q[kTerms];
         query<A, DT, kExact>(a, s, g, h0, nh, lane, i >> 1, i & 1, q);
 #pragma unroll
@@ -84,7 +89,7 @@ template <typename A, int DT, bool kExact>
 __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0, int nh, int ctx, int u0, int n, int lane,
                                              const unsigned char* s_q, float& m, float& lsum, f32x4 (&o)[DT / 16])
 {
-    constexpr int kTerms = terms_of<A>(), kH = DT / 64, kV = DT / 16;          // 64-channel blocks of the keys, 16-channel blocks of the values
+    constexpr int kTerms = terms_of<A>(), kH = key_blocks(DT), kV = DT / 16;          // 64-channel blocks of the keys, 16-channel blocks of the values
     const AttnArgs& a = x.a;
     const int hkv = a.c.hkv, D = kExact ? DT : a.c.d, ps = a.c.ps, chunks = D >> 4;
     const int r = lane & 15, c = lane >> 4;
@@ -137,8 +142,7 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int h = 0; h < kH; ++h) {
-                const int chunk = kExact ? 4 * h + c : min(4 * h + c, chunks - 1);       // (beyond: times zeros of the query)
-                k[j][h] = stream16(kp + (j * chunks + chunk) * 64);
+                k[j][h] = stream16(kp + (j * chunks + chunk_of<DT, kExact>(h, c, chunks)) * 64);
             }
         ke = *reinterpret_cast<const uint32_t*>(exps_at(x.exps, w.exps) + (r & 3) * 4);
     };
@@ -473,12 +477,16 @@ ag_status launch(const Args& x, const Partials& p, int grid, hipStream_t st)
     return hip_check(hipGetLastError(), "decode launch");
 }
 
+// The least of five widths that holds a head: 96 channels in 128 are 15 to 25 % slower (64 sessions of 1000..2000 tokens 34.9 us, 27.6), 192 in 256 as much
+// (66.2, 58.1).
 template <typename A>
 ag_status launch_typed(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
     const int d = x.a.c.d;
     return d == 64 ? launch<A, 64, true>(x, p, grid, st) : d < 64 ? launch<A, 64, false>(x, p, grid, st)
+         : d == 96 ? launch<A, 96, true>(x, p, grid, st) : d < 96 ? launch<A, 96, false>(x, p, grid, st)
          : d == 128 ? launch<A, 128, true>(x, p, grid, st) : d < 128 ? launch<A, 128, false>(x, p, grid, st)
+         : d == 192 ? launch<A, 192, true>(x, p, grid, st) : d < 192 ? launch<A, 192, false>(x, p, grid, st)
          : d == 256 ? launch<A, 256, true>(x, p, grid, st) : launch<A, 256, false>(x, p, grid, st);
 }
 

@@ -160,7 +160,7 @@ def check_resume(side, q, out, new, scale, what):
     check_norm(side.dtype, side.d, *zip(*found), what)
 
 
-GEOMETRIES = [(128, 16), (128, 64), (64, 16), (64, 32), (256, 16), (16, 16), (48, 128), (96, 32), (112, 16), (208, 256), (240, 16)]
+GEOMETRIES = [(128, 16), (128, 64), (64, 16), (64, 32), (256, 16), (16, 16), (48, 128), (80, 64), (96, 32), (112, 16), (176, 32), (192, 16), (208, 256), (240, 16)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
