@@ -290,23 +290,27 @@ ag_status launch(const Args& x, hipStream_t st)
 
 // Few rows on long contexts: the keys of 32 columns dealt to the waves of a workgroup (attn_split_q8.hip) instead of whole tiles, each a chain
 // of all of them.  A launch is as long as a chain, or as many as a CU's workgroups come to, and a chain is a start and its share of the
-// context; in units of what a context token costs eight waves: 1500 + L, of four 1500 + 2.1 L with two workgroups a CU (three to 64 channels), of tiles 1500 + 4.5 L;
-// past 128 channels, one workgroup of one wave a SIMD a CU, of four 1500 + 2.1 L and of tiles 1500 + 9 L.  Of several sessions, where more than one round
+// context; in units of what a context token costs eight waves: 1500 + L, of four 1500 + 2.1 L with two workgroups a CU (three to 96 channels), of tiles 1500 + 4.5 L;
+// past 128 channels, one workgroup of one wave a SIMD a CU, of four 1500 + 2.1 L and of tiles 1500 + 9 L; a third more for tiles of 128 or 256 channels where
+// attn_split_q8.hip has 96 or 192.  Of several sessions, where more than one round
 // evens them out, the mean context is taken for three quarters of the longest.  Graph replay, 32 / 8 heads x 128 unless said otherwise, tiles -> split, us
 // (workgroups of 32 columns): one chunk on 6007 tokens of 50 rows (56) 128 -> 32, 211 (216) 133 -> 34, 400 (400) 136 -> 66, 1000 (1000) 150 -> 152; on 2000 of 300 (304) 53 ->
 // 27, 1000 72 -> 75; 16 of 30 on 600 (512) 20.4 -> 12.6; 8 of 50..300 on 2000..4000 (1328) 106 -> 100, of 100..200 on 500..1000 (1184) 36 -> 34; 16 of 50..100 on 100..300
 // (1248) 19.5 -> 22.1; prompts: 4 of 100 (416) 9.8 -> 7.0, 3 of 250 (768) 13.0 -> 13.1, one of 500 (504) 17.8 -> 9.7, 16 of 200..600 (6568) 58 -> 96; x 64: 211 on 6007 100 -> 26, 8 of
-// 50..300 on 2000..4000 73 -> 65, 16 prompts of 200..600 41 -> 50; x 256: 8 of 50..300 on 2000..4000 231 -> 230, 4 of them (696) 161 -> 133, 16 prompts of 200..600 144 -> 240.
+// 50..300 on 2000..4000 73 -> 65, 16 prompts of 200..600 41 -> 50; x 256: 8 of 50..300 on 2000..4000 231 -> 230, 4 of them (696) 161 -> 133, 16 prompts of 200..600 144 -> 240;
+// x 96: 8 of 50..300 on 2000..4000 115 -> 76, two prompts of 700 (1408) 25.2 -> 18.2, 16 of 200..600 61 -> 65; x 192: 8 of 100..200 on 500..1000 77 -> 62, two prompts of 700 40.5 -> 49.3.
 // fp32 always: tiles with their queries and weights in three terms have one wave a SIMD, and 256 channels spill (eight prompts of 2000 rows x 64 497 -> 457, x 128 782 ->
 // 781, x 256 2560 -> 1804; 8 of 100..200 on 500..1000 50 -> 37, 76 -> 59, 225 -> 129).
 bool split_preferred(const AttnArgs& a, hipStream_t st)
 {
     if (a.c.dtype == AG_F32) return true;
-    const bool wide = a.c.d > 128;
-    const double cus = stream_cus(st), slots = wide ? cus : 2 * cus, few_slots = a.c.d <= 64 ? 3 * cus : slots, heads = a.c.hkv, ctx = a.max_ctx, mean = a.batch > 1 ? 0.75 * ctx : ctx;
-    const double few = heads * (double)tiles_bound(a, 32), whole = heads * (double)tiles_bound(a, 128), step = wide ? 9.0 : 4.5;
+    const int d = a.c.d;
+    const bool wide = d > 128;
+    const double cus = stream_cus(st), slots = wide ? cus : 2 * cus, few_slots = d <= 96 ? 3 * cus : slots, heads = a.c.hkv, ctx = a.max_ctx, mean = a.batch > 1 ? 0.75 * ctx : ctx;
+    const double few = heads * (double)tiles_bound(a, 32), whole = heads * (double)tiles_bound(a, 128);
+    const double padding = (d > 64 && d <= 96) || (d > 128 && d <= 192) ? 4.0 / 3 : 1, start = 1500 * padding, step = (wide ? 9 : 4.5) * padding;
     const double split = !wide && few <= cus ? 1500 + ctx : few <= few_slots ? 1500 + 2.1 * ctx : few / few_slots * (1500 + 2.1 * mean);
-    const double tiles = whole <= slots ? 1500 + step * ctx : whole / slots * (1500 + step * mean);
+    const double tiles = whole <= slots ? start + step * ctx : whole / slots * (start + step * mean);
     return split < tiles;
 }
 

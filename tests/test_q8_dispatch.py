@@ -20,9 +20,10 @@ SPLIT, TILES, WIDE = "prefill_q8_split_kernel<", "prefill_q8_kernel<4,", "prefil
 @pytest.mark.parametrize("want,batches", [
     (SPLIT, [dict(batch=1, prefix=6007, new=211), dict(batch=1, prefix=6007, new=600), dict(batch=1, prefix=2000, new=211), dict(batch=16, prefix=600, new=30),
              dict(batch=1, prefix=6007, new=211, dtype="f32"), dict(batch=6, total=784, max_new=300, max_ctx=2300, d=64, page=32, dtype="f32"),
-             dict(batch=4, prefix=2000, new=16, hq=24, hkv=1), dict(batch=8, new=1500, dtype="f32"), dict(batch=8, total=1300, max_new=300, max_ctx=4300, d=64), dict(batch=4, total=690, max_new=300, max_ctx=4300, d=256)]),
+             dict(batch=4, prefix=2000, new=16, hq=24, hkv=1), dict(batch=8, new=1500, dtype="f32"), dict(batch=8, total=1300, max_new=300, max_ctx=4300, d=64), dict(batch=4, total=690, max_new=300, max_ctx=4300, d=256),
+             dict(batch=2, new=700, d=96), dict(batch=1, prefix=2000, new=1000, d=192)]),
     (TILES, [dict(batch=1, prefix=2000, new=1000), dict(batch=16, new=50), dict(batch=1, new=1000), dict(batch=8, new=512), dict(batch=64, new=600), dict(batch=1, new=2048), dict(batch=16, total=1200, max_new=100, max_ctx=400), dict(batch=16, total=6500, max_new=600, max_ctx=600, d=64),
-             dict(batch=16, total=6500, max_new=600, max_ctx=600, d=256)]),
+             dict(batch=16, total=6500, max_new=600, max_ctx=600, d=256), dict(batch=16, total=6500, max_new=600, max_ctx=600, d=96), dict(batch=2, new=700, d=192)]),
     (WIDE, [dict(batch=8, new=4096), dict(batch=2, prefix=2000, new=1000), dict(batch=32, prefix=3000, new=200)]),
 ])
 def test_prefill(tmp, want, batches):
