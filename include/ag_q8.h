@@ -21,6 +21,7 @@
  *                     slots the byte of slot s stands at 4 * (s % 4) + s / 4 for keys, at s for values.
  *   - Supported: AG_F32 and AG_BF16; head_dim a multiple of 16, <= 256; page_size a power of two in [16, 256]; any group size;
  *     q, out, k_new, v_new, k_out, v_out, the pools and exps 16-byte aligned (AG_ERR_INVALID_ARG otherwise).
+ *   - max_ctx is at most 2^31 - 1025 (AG_ERR_INVALID_ARG beyond it).
  *   - Slots that no token uses may hold anything, NaN included: they are read, but nothing depends on them.
  *   - fp32 activations keep 32 bits in the products (queries and softmax weights as three bf16 terms); bf16 activations multiply
  *     weights rounded to bf16, as attention over a bf16 cache does.

@@ -36,7 +36,10 @@ ag_status view(const ag_kv_cache_q8* c, CacheView* v)
     return AG_OK;
 }
 
-// q and out of every attention call, the heads and the scale
+// Positions are 32-bit numbers, and those of the steps after the last one too.
+constexpr int kMostCtx = 0x7fffffff - 1024;
+
+// q and out of every attention call, the heads, the scale and the longest context
 ag_status check_attention(const CacheView& c, const void* q, const void* out, int hq, float scale, int max_ctx, int max_pages)
 {
     if (!aligned(q) || !aligned(out)) { set_error("q and out must be 16-byte aligned"); return AG_ERR_INVALID_ARG; }
@@ -45,6 +48,7 @@ ag_status check_attention(const CacheView& c, const void* q, const void* out, in
         return AG_ERR_INVALID_ARG;
     }
     if (!(scale > 0.0f) || !(scale < 1e30f)) { set_error("scale must be positive and finite"); return AG_ERR_INVALID_ARG; }
+    if (max_ctx > kMostCtx) { set_error("max_ctx %d exceeds %d", max_ctx, kMostCtx); return AG_ERR_INVALID_ARG; }
     if ((int64_t)max_ctx > (int64_t)max_pages * c.ps) {
         set_error("max_ctx %d exceeds max_pages_per_seq * page_size = %lld", max_ctx, (long long)max_pages * c.ps);
         return AG_ERR_INVALID_ARG;
@@ -139,7 +143,7 @@ ag_status ag_attn_resume_q8(const ag_kv_cache_q8* cache, const void* q, void* ou
 
 size_t ag_attn_decode_q8_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t head_dim, int32_t max_ctx)
 {
-    if (batch <= 0 || num_q_heads <= 0 || head_dim <= 0 || max_ctx < 0) return 0;
+    if (batch <= 0 || num_q_heads <= 0 || head_dim <= 0 || max_ctx < 0 || max_ctx > q8::kMostCtx) return 0;
     return q8::decode_workspace(batch, num_q_heads, head_dim, max_ctx);
 }
 

@@ -564,6 +564,43 @@ def test_calls_on_two_streams_and_in_graphs():
         assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip((got[0], got[2], *back), eager)), r
 
 
+@pytest.mark.parametrize("dtype,d,hq,new", [("bf16", 128, 16, [130, 40, 1]), ("f32", 96, 6, [9, 140, 33]), ("bf16", 192, 4, [64, 1, 200])])
+def test_replays_of_every_kernel(few_cus, dtype, d, hq, new):
+    """Decode in shares with its merge, prefill by few rows and, on few CUs, by whole tiles: captured, and replayed over dirty workspaces."""
+    side = Side(dtype, d, 16, 2, [700, 300, 260], seed=9)
+    old = [n - m for n, m in zip([700, 300, 260], new)]
+    side.append(old)
+    side.append(new)
+    t, scale, s = sum(new), d ** -0.5, torch.cuda.ExternalStream(few_cus)
+    lens, cu, prefix, ctx = i32(new), i32(np.concatenate([[0], np.cumsum(new)])), i32(old), i32(side.lens())
+    bt = i32(np.pad(side.bt, ((0, 0), (0, SHARED_CTX // 16 - side.bt.shape[1]))))
+    q, q1 = side.dev(side.draw(t, hq, d)), side.dev(side.draw(3, hq, d))
+    ws = torch.empty(B.ag_attn_decode_q8_workspace_bytes(3, hq, d, SHARED_CTX), dtype=torch.uint8, device=DEV)
+    got = [torch.empty_like(q), torch.empty_like(q1)]
+
+    def step():
+        B.ag_attn_resume_q8(side.cache, q, got[0], bt, prefix, lens, cu, t, max(new), 700, hq, scale)
+        B.ag_attn_decode_q8(side.cache, q1, got[1], bt, ctx, SHARED_CTX, hq, scale, ws)
+
+    for stream in (torch.cuda.Stream(), s):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            step()
+        torch.cuda.synchronize()
+        eager = [x.clone() for x in got]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        for r in range(3):
+            for x in got:
+                x.fill_(float("nan"))
+            ws.random_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, eager)), r
+
+
 def test_plain_calls_and_those_through_ctypes_are_the_same(monkeypatch):
     outs = []
     for calls in (B._calls(), B._NoCalls()):

@@ -65,6 +65,14 @@ def test_decode_workspace():
     assert decode(cache(num_kv_heads=8), hq=8, batch=1 << 24, pages=1 << 20, max_ctx=1 << 20, nbytes=1 << 62) == B.AG_ERR_INVALID_ARG
 
 
+def test_contexts_past_32_bits():
+    most = (1 << 31) - 1025
+    assert resume(cache(), pages=1 << 27, max_ctx=most + 1) == B.AG_ERR_INVALID_ARG and b"max_ctx" in B.lib().ag_last_error()
+    assert prefill(cache(), pages=1 << 27, total=most + 1, max_new=most + 1) == B.AG_ERR_INVALID_ARG
+    assert decode(cache(), pages=1 << 27, max_ctx=most + 1, nbytes=1 << 62) == B.AG_ERR_INVALID_ARG
+    assert B.ag_attn_decode_q8_workspace_bytes(1, 4, 128, most + 1) == 0 and B.ag_attn_decode_q8_workspace_bytes(1, 4, 128, most) > 0
+
+
 def test_nothing_to_do_reaches_no_device():
     for call in CALLS[:2]:
         assert call(cache(), total=0) == B.AG_OK
