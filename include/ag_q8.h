@@ -23,8 +23,11 @@
  *     q, out, k_new, v_new, k_out, v_out, the pools and exps 16-byte aligned (AG_ERR_INVALID_ARG otherwise).
  *   - max_ctx is at most 2^31 - 1025 (AG_ERR_INVALID_ARG beyond it).
  *   - Slots that no token uses may hold anything, NaN included: they are read, but nothing depends on them.
- *   - fp32 activations keep 32 bits in the products (queries and softmax weights as three bf16 terms); bf16 activations multiply
- *     weights rounded to bf16, as attention over a bf16 cache does.
+ *   - fp32 activations keep 24 bits of queries and softmax weights in the products, as three bf16 terms, in every call.  bf16 activations: decode
+ *     keeps them too, but with head_dim 128, page_size 16 and up to 16 heads a group, where weights are rounded to bf16 as over a bf16 cache of that
+ *     shape; prefill and resume round them at every shape (over bf16 caches at that one only): off by up to 2^-8 of themselves, each for itself, beside
+ *     cached values that are off by up to 2^-4 and an output rounded by up to 2^-8.  The pools do not depend on `dtype`: whoever wants all bits of the
+ *     weights in prefill describes the same pools as AG_F32 and passes fp32 rows.
  *   - What is not finite in a key or a value reaches the rows that see its token, a value's in its own channel only, and no other row.
  *   - Attention divides by the sum of its weights at the end: queries, keys and values whose rows' largest entries lie between 2^-60 and 2^90
  *     keep the accuracy above whatever the context; smaller ones may lose their last bits, sums of larger ones may overflow.

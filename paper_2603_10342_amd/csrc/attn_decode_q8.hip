@@ -16,8 +16,7 @@
 // with that instruction, a value's is multiplied into its weight.
 // Two workgroups a CU; three (168 registers, of which 29 are spilled, or the same 198 dealt finer) take 64.3 to 81 us where two take 64 (64 sessions of
 // 1024..4096 tokens, 32 / 8 heads x 128, 352 MB: 5.9 TB/s in the split kernel, 4.7 us of merge).  Pages of 64 or 256 instead of 16 change 1 %.
-// bf16 activations: weights are rounded to bf16 for the value product, as over bf16 caches (half a step of 2^-8, independent for
-// every key, beside the output's own rounding); fp32: queries and weights as three bf16 terms, 24 bits.
+// Weights go into the value product as three bf16 terms, 24 bits, or rounded to bf16 (rounds_weights()); fp32 queries are three terms too.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -97,7 +96,7 @@ __device__ __forceinline__ Ids pages_of(const AttnArgs& a, int s, int step, int 
 
 // One wave's part of a segment, steps u0, u0 + kStride .. (n of them) of (session s, KV head g, heads h0 .. h0 + nh - 1 of its group): running maximum,
 // this lane's share of the sum, and O^T.  o[mb][i]: channel 16 mb + 4 c + i of head r, lane = 16 c + r.
-template <typename A, int DT, bool kExact, int kStride>
+template <typename A, int DT, bool kExact, int kWeightTerms, int kStride>
 __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0, int nh, int ctx, int u0, int n, int lane,
                                              const Ids* first, const unsigned char* s_q, float& m, float& lsum, f32x4 (&o)[DT / 16])
 {
@@ -203,7 +202,7 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
         const float m_ref = m_new == -INFINITY ? 0.f : m_new;    // (scores that are all -inf or NaN)
         const float alpha = __builtin_amdgcn_exp2f(m - m_ref);
         float psum = 0.f;
-        bf16x8 w[2][kTerms];
+        bf16x8 w[2][kWeightTerms];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             float p[8];
@@ -285,7 +284,7 @@ __device__ __forceinline__ f32x4 combine(const float* s_o, int rows, int D, int 
     return acc;
 }
 
-template <typename A, int DT, bool kExact>
+template <typename A, int DT, bool kExact, int kWeightTerms>
 __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split_kernel(Args x, int32_t* __restrict__ hdr, float* __restrict__ ws_o,
                                                                                                           float* __restrict__ ws_ml, int pmax)
 {
@@ -315,7 +314,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
             queries_to_lds<A, DT, kExact, kWaves>(a, s, g, h0, nh, s_q);
             __syncthreads();
         }
-        attend_steps<A, DT, kExact, 1>(x, s, g, h0, nh, ctx, u + w * per, max(0, min(per, k - w * per)), lane, nullptr, s_q, m, lsum, o);
+        attend_steps<A, DT, kExact, kWeightTerms, 1>(x, s, g, h0, nh, ctx, u + w * per, max(0, min(per, k - w * per)), lane, nullptr, s_q, m, lsum, o);
         lsum += __shfl_xor(lsum, 16);
         lsum += __shfl_xor(lsum, 32);
         results_to_lds<DT, kExact, kWaves>(s_o, w, rows, nh, D, lane, m, lsum, o);
@@ -356,7 +355,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
 constexpr int kDirectMaxTokens = 16 << 10;
 constexpr int64_t kDirectMaxPairs = 1 << 30;        // of a launch
 
-template <typename A, int DT, bool kExact>
+template <typename A, int DT, bool kExact, int kWeightTerms>
 __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_direct_kernel(Args x)
 {
     constexpr int W = kWaves;
@@ -385,7 +384,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_direc
         queries_to_lds<A, DT, kExact, W>(a, s, g, h0, nh, s_q);
         __syncthreads();
     }
-    attend_steps<A, DT, kExact, W>(x, s, g, h0, nh, ctx, w, max(0, (n - w + W - 1) / W), lane, &first, s_q, m, lsum, o);
+    attend_steps<A, DT, kExact, kWeightTerms, W>(x, s, g, h0, nh, ctx, w, max(0, (n - w + W - 1) / W), lane, &first, s_q, m, lsum, o);
     lsum += __shfl_xor(lsum, 16);
     lsum += __shfl_xor(lsum, 32);
     results_to_lds<DT, kExact, W>(s_o, w, rows, nh, D, lane, m, lsum, o);
@@ -467,7 +466,7 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(Args x, const int3
 struct Partials { int32_t* hdr; float *o, *ml; int pmax; };
 
 // grid: workgroups of the split kernel, or 0 for one workgroup a pair
-template <typename A, int DT, bool kExact>
+template <typename A, int DT, bool kExact, int kWeightTerms = 3>
 ag_status launch(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
     const AttnArgs& a = x.a;
@@ -475,14 +474,20 @@ ag_status launch(const Args& x, const Partials& p, int grid, hipStream_t st)
     const size_t lds = query_bytes<A>(DT) + lds_of(kWaves, std::min(G, kCols), a.c.d);
     if (lds > 64 * 1024) {
         static std::atomic<uint64_t> told[2] = {};
-        const void* kernel = grid ? (const void*)decode_q8_split_kernel<A, DT, kExact> : (const void*)decode_q8_direct_kernel<A, DT, kExact>;
+        const void* kernel = grid ? (const void*)decode_q8_split_kernel<A, DT, kExact, kWeightTerms> : (const void*)decode_q8_direct_kernel<A, DT, kExact, kWeightTerms>;
         ag_status e = allow_dynamic_lds(kernel, query_bytes<A>(DT) + (int)lds_of(kWaves, kCols, DT), told[grid ? 0 : 1]);
         if (e) return e;
     }
-    if (grid) hipLaunchKernelGGL((decode_q8_split_kernel<A, DT, kExact>), dim3(grid), dim3(64 * kWaves), lds, st, x, p.hdr, p.o, p.ml, p.pmax);
-    else hipLaunchKernelGGL((decode_q8_direct_kernel<A, DT, kExact>), dim3(a.batch * a.c.hkv * blocks_of(G)), dim3(64 * kWaves), lds, st, x);
+    if (grid) hipLaunchKernelGGL((decode_q8_split_kernel<A, DT, kExact, kWeightTerms>), dim3(grid), dim3(64 * kWaves), lds, st, x, p.hdr, p.o, p.ml, p.pmax);
+    else hipLaunchKernelGGL((decode_q8_direct_kernel<A, DT, kExact, kWeightTerms>), dim3(a.batch * a.c.hkv * blocks_of(G)), dim3(64 * kWaves), lds, st, x);
     return hip_check(hipGetLastError(), "decode launch");
 }
+
+// Decode keeps of a softmax weight what it keeps over a bf16 cache of the same shape (ag.h): all 24 bits, but for bf16 with 128 channels on pages
+// of 16 and up to 16 heads a group, where it is rounded to bf16, off by up to 2^-8 of itself, independently of the others.  Three terms there: one session
+// of 1000 tokens 8.2 -> 9.6 us, 64 of 1 to 512 9.4 -> 10.3, 64 of 1024 to 4096 63.3 -> 64.3.  One term elsewhere: 64 sessions of 1000 to 2000 x 64 19.2 -> 18.2 us, x 256
+// 75.5 -> 73.7.
+bool rounds_weights(const AttnArgs& a) { return a.c.dtype == AG_BF16 && a.c.d == 128 && a.c.ps == 16 && a.hq <= kCols * a.c.hkv; }
 
 // The least of five widths that holds a head: 96 channels in 128 are 15 to 25 % slower (64 sessions of 1000..2000 tokens 34.9 us, 27.6), 192 in 256 as much
 // (66.2, 58.1).
@@ -490,6 +495,9 @@ template <typename A>
 ag_status launch_typed(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
     const int d = x.a.c.d;
+    if constexpr (sizeof(A) == 2) {
+        if (rounds_weights(x.a)) return launch<A, 128, true, 1>(x, p, grid, st);
+    }
     return d == 64 ? launch<A, 64, true>(x, p, grid, st) : d < 64 ? launch<A, 64, false>(x, p, grid, st)
          : d == 96 ? launch<A, 96, true>(x, p, grid, st) : d < 96 ? launch<A, 96, false>(x, p, grid, st)
          : d == 128 ? launch<A, 128, true>(x, p, grid, st) : d < 128 ? launch<A, 128, false>(x, p, grid, st)

@@ -112,7 +112,7 @@ __device__ __forceinline__ bool take_nan_out(u32x4 (&x)[N])
     return true;
 }
 
-// Numbers of the activations' type, or their arithmetic's, as bf16 terms: operands of the products.  One term rounds.
+// Numbers of the activations' type, exactly, and softmax weights as bf16 terms: operands of the products.  One term of a weight rounds it.
 template <typename A>
 constexpr int terms_of() { return sizeof(A) == 4 ? 3 : 1; }
 __device__ __forceinline__ void as_terms(const Terms& x, bf16x8 (&t)[3])
