@@ -207,12 +207,10 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
         for (int half = 0; half < 2; ++half) {
             float p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int e = half * 8 + i;
-                p[i] = __builtin_amdgcn_exp2f(xs[e] - m_ref);
-                psum += p[i];
-                p[i] = times_power(p[i], ve, e);
-            }
+            for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(xs[half * 8 + i] - m_ref);
+            psum = add_weights<kWeightTerms>(psum, p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = times_power(p[i], ve, half * 8 + i);
             to_terms(p, w[half]);
         }
         lsum = lsum * alpha + psum;

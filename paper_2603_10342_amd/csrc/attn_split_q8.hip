@@ -199,11 +199,10 @@ __global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_spl
             for (int half = 0; half < 2; ++half) {
                 float p[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(fmaf(sc[half * 8 + i], sl2, -m_ref));
-                    psum += p[i];
-                    p[i] = times_power(p[i], ve, half * 8 + i);
-                }
+                for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(sc[half * 8 + i], sl2, -m_ref));
+                psum = add_weights<kTerms>(psum, p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = times_power(p[i], ve, half * 8 + i);
                 to_terms(p, wt[half]);
             }
             lsum += psum;

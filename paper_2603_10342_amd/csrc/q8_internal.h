@@ -135,6 +135,20 @@ __device__ __forceinline__ void to_terms(const float (&w)[8], bf16x8 (&t)[3])
     for (int i = 0; i < 4; ++i) x.set_pair(i, w[2 * i], w[2 * i + 1]);
     as_terms(x, t);
 }
+// Eight weights added to the normaliser as the value product takes them, rounded where they are one term: an error that they share is then in both
+// sums, and cancels.
+template <int kWeightTerms>
+__device__ __forceinline__ float add_weights(float sum, const float (&p)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        if constexpr (kWeightTerms == 1)
+            sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{(__bf16)p[i], (__bf16)p[i + 1]}, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, sum, false);
+        else
+            sum += p[i] + p[i + 1];
+    }
+    return sum;
+}
 template <int kTerms>
 __device__ __forceinline__ void no_terms(bf16x8 (&t)[kTerms])
 {

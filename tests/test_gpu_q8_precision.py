@@ -6,7 +6,7 @@ import torch
 import q8_oracle as Q
 from gpu_helpers import i32
 from paper_2603_10342_amd import binding as B
-from test_gpu_q8 import AG, DEV, TD, Side, decode
+from test_gpu_q8 import AG, DEV, TD, Side, decode, resume
 from test_q8_dispatch import SHARED_CTX
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +70,38 @@ def test_fp32_rows_over_a_cache_that_bf16_rows_wrote_keep_24_bits_in_every_call(
         for s in range(batch):
             ref = Q.attend(q[s:s + 1], side.k[s], side.v[s], prefix + 2, 0.125)[0][0]
             assert (np.abs(got[s] - ref) <= 2.0 ** -10 * np.abs(ref)).all(), (what, s)
+
+
+@pytest.fixture(scope="module")
+def few_cus():
+    """A stream of eight CUs, on which small batches are many workgroups."""
+    stream = B.ag_stream_create_cumask(B.ag_cumask_build(256, 8, 0, 1))
+    yield stream
+    torch.cuda.synchronize()
+    B.ag_stream_destroy(stream)
+
+
+# Every token of a session has the same value row c: whatever the weights are, the output is c, if they are divided by the sum of what they were
+# multiplied as.  c has four significant bits, half a step of bf16 away from rounding to anything else, 2^-9 of itself at least; the sums'
+# roundings are (n + 16) 2^-23.  The weights of all keys but one are the same number, so that what rounds it does not average out: up to 2^-8.
+@pytest.mark.parametrize("d,page", [(128, 16), (64, 32), (256, 16), (96, 32)])
+def test_equal_values_come_out_as_they_are(few_cus, d, page):
+    hq, hkv, new = 8, 2, np.array([100, 64, 1, 33])
+    n = np.array([700, 300, 130, 33])
+    side = Side("bf16", d, page, hkv, n, seed=d)
+    t = int(n.sum())
+    k, c = np.zeros((t, hkv, d), np.float32), np.zeros((4, hkv, d), np.float32)
+    for s, at in enumerate(np.cumsum(n) - n):
+        k[at + 1:at + n[s], :, 0] = -1.0
+        c[s] = (8 + side.rng.integers(0, 8, (hkv, d))) / 8 * np.exp2(side.rng.integers(-3, 4, (hkv, d))) * side.rng.choice([-1, 1], (hkv, d))
+    side.append(n, k=k, v=np.repeat(c, n, 0))
+    want = np.repeat(c, hq // hkv, 1)                             # [session][query head][channel]
+    q = np.zeros((int(new.sum()), hq, d), np.float32)
+    q[:, :, 0] = Q.bf16(side.rng.uniform(0.5, 16, q.shape[:2]).astype(np.float32))       # weights e^(-q / 8): 0.14 to 0.94
+    for stream in (None, few_cus):
+        got = resume(side, q, new, hq, 0.125, stream=stream).double().cpu().numpy()
+        assert np.array_equal(got, np.repeat(want, new, 0)), stream
+    for max_ctx in (None, SHARED_CTX):
+        for step in range(8):
+            got = decode(side, q[4 * step:4 * step + 4], hq, 0.125, max_ctx=max_ctx).double().cpu().numpy()
+            assert np.array_equal(got, want), max_ctx
