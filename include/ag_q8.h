@@ -29,8 +29,9 @@
  *     cached values that are off by up to 2^-4 and an output rounded by up to 2^-8.  The pools do not depend on `dtype`: whoever wants all bits of the
  *     weights in prefill describes the same pools as AG_F32 and passes fp32 rows.
  *   - What is not finite in a key or a value reaches the rows that see its token, a value's in its own channel only, and no other row.
- *   - Attention divides by the sum of its weights at the end: queries, keys and values whose rows' largest entries lie between 2^-60 and 2^90
- *     keep the accuracy above whatever the context; smaller ones may lose their last bits, sums of larger ones may overflow.
+ *   - Scores are summed up in fp32 before `scale`, and attention divides by the sum of its weights at the end.  The accuracy above holds whatever the
+ *     context for queries, keys and values whose rows' largest entries lie between 2^-60 and 2^80, a scale up to 2^60, and scores that fit: head_dim *
+ *     max |q| * max |k| below 2^127, and so that times scale * log2 e.  Below these, last bits may be lost; above, sums may overflow and rows become NaN.
  */
 #ifndef AG_Q8_H
 #define AG_Q8_H

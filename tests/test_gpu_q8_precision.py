@@ -105,3 +105,25 @@ def test_equal_values_come_out_as_they_are(few_cus, d, page):
         for step in range(8):
             got = decode(side, q[4 * step:4 * step + 4], hq, 0.125, max_ctx=max_ctx).double().cpu().numpy()
             assert np.array_equal(got, want), max_ctx
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_the_ends_of_the_documented_range_change_no_bit(few_cus, dtype, d):
+    """Queries and keys raised together, or lowered, with a scale that takes it back: the largest scores are 2^125 (d 256: entries up to 2^2.4, so
+    2^(112 + 4.8 + 8)) before the scale and as ever behind it.  Values at their ends.  Every rounding is relative: the same bits."""
+    lens, new, hq, hkv, scale = [300, 77], [120, 77], 8, 2, d ** -0.5 / 4
+    outs = []
+    for kp, qp, pv in ((0, 0, 0), (56, 56, 77), (77, 35, -57), (-30, -25, 70), (-57, 0, 0)):
+        side = Side(dtype, d, 16, hkv, lens, seed=3)
+        old = [n - m for n, m in zip(lens, new)]
+        for n in (old, new):
+            k, v = (side.draw(sum(n), hkv, d).clip(-5, 5) for _ in range(2))
+            side.append(n, k=np.ldexp(k, kp).astype(np.float32), v=np.ldexp(v, pv).astype(np.float32))
+        q, s = np.ldexp(side.draw(sum(new), hq, d).clip(-5, 5), qp), float(np.ldexp(scale, -kp - qp))
+        got = [resume(side, q, new, hq, s), resume(side, q, new, hq, s, stream=few_cus)]
+        got += [decode(side, q[:2], hq, s), decode(side, q[:2], hq, s, max_ctx=SHARED_CTX)]
+        outs.append([np.ldexp(x.double().cpu().numpy(), -pv) for x in got])
+    for other in outs[1:]:
+        for x, y in zip(outs[0], other):
+            assert np.isfinite(x).all() and np.array_equal(x, y)
