@@ -351,7 +351,6 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
 // round trips are most of a small step.  Four waves and two workgroups a CU: eight are no faster alone (one session of 500 to 1000 tokens 7.8 us, four
 // 7.5) and leave room for half as many pairs (256 sessions of 1 to 512 46 us, four 29).
 constexpr int kDirectMaxTokens = 16 << 10;
-constexpr int64_t kDirectMaxPairs = 1 << 30;        // of a launch
 
 template <typename A, int DT, bool kExact, int kWeightTerms>
 __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_direct_kernel(Args x)
@@ -503,11 +502,14 @@ ag_status launch_typed(const Args& x, const Partials& p, int grid, hipStream_t s
          : d == 256 ? launch<A, 256, true>(x, p, grid, st) : launch<A, 256, false>(x, p, grid, st);
 }
 
+int merge_rows(const AttnArgs& a) { return 256 / (a.c.d / 4); }
+int64_t merge_workgroups(const AttnArgs& a) { return ((int64_t)a.batch * a.hq + merge_rows(a) - 1) / merge_rows(a); }
+
 template <typename A>
 ag_status launch_merge(const Args& x, const Partials& p, hipStream_t st)
 {
-    const int rows = 256 / (x.a.c.d / 4);
-    hipLaunchKernelGGL(decode_q8_merge_kernel<A>, dim3((unsigned)(((int64_t)x.a.batch * x.a.hq + rows - 1) / rows)), dim3(256), 0, st, x, p.hdr, p.o, p.ml, p.pmax, rows);
+    const int rows = merge_rows(x.a);
+    hipLaunchKernelGGL(decode_q8_merge_kernel<A>, dim3((unsigned)merge_workgroups(x.a)), dim3(256), 0, st, x, p.hdr, p.o, p.ml, p.pmax, rows);
     return hip_check(hipGetLastError(), "decode merge launch");
 }
 
@@ -522,7 +524,7 @@ ag_status launch_merge(const Args& x, const Partials& p, hipStream_t st)
 bool one_workgroup_a_pair(const AttnArgs& a, int64_t pairs, int64_t cus)
 {
     const int64_t size = (int64_t)a.max_ctx * (a.c.d + 64), line = a.c.dtype == AG_BF16 ? 400000 : 290000;
-    return pairs <= kDirectMaxPairs && a.max_ctx <= kDirectMaxTokens && 8 * size <= (2 * pairs > cus ? 8 : 5) * line;
+    return pairs <= most_workgroups(64 * kWaves) && a.max_ctx <= kDirectMaxTokens && 8 * size <= (2 * pairs > cus ? 8 : 5) * line;
 }
 
 }  // namespace
@@ -552,6 +554,7 @@ ag_status launch_decode(const Args& x, void* ws, hipStream_t st)
     // Upper bound of the step count from the host-known bounds: a share is at most kMaxSteps steps even if every session is max_ctx long.
     const int64_t f_max = pairs * ((a.max_ctx + (kTok - 1)) / kTok);
     if (f_max > (1 << 30)) { set_error("decode batch of %lld steps of %d tokens is beyond one launch", (long long)f_max, kTok); return AG_ERR_INVALID_ARG; }
+    if (merge_workgroups(a) > most_workgroups(256)) { set_error("decode batch of %lld rows is beyond one launch", (long long)a.batch * a.hq); return AG_ERR_INVALID_ARG; }
     prof_before(st);
     if (a.max_ctx > 0) e = bf16 ? launch_typed<__bf16>(x, p, share_workgroups(f_max, st), st) : launch_typed<float>(x, p, share_workgroups(f_max, st), st);
     if (!e) e = bf16 ? launch_merge<__bf16>(x, p, st) : launch_merge<float>(x, p, st);

@@ -280,7 +280,7 @@ ag_status launch(const Args& x, hipStream_t st)
         if (e) return e;
     }
     const AttnArgs& a = x.a;
-    if (a.c.hkv * tiles_bound(a, 32 * NW) + kDealtPast > 0x7fffffff || (int64_t)a.total_rows * (a.hq / a.c.hkv) > 0x7fffffff) {
+    if (a.c.hkv * tiles_bound(a, 32 * NW) + kDealtPast > most_workgroups(64 * NW) || (int64_t)a.total_rows * (a.hq / a.c.hkv) > 0x7fffffff) {
         set_error("too many rows for one launch");
         return AG_ERR_INVALID_ARG;
     }

@@ -281,7 +281,7 @@ ag_status launch(const Args& x, hipStream_t st)
         if (e) return e;
     }
     const AttnArgs& a = x.a;
-    if (a.c.hkv * tiles_bound(a) + kDealtPast > 0x7fffffff || (int64_t)a.total_rows * (a.hq / a.c.hkv) > 0x7fffffff) {
+    if (a.c.hkv * tiles_bound(a) + kDealtPast > most_workgroups(64 * W) || (int64_t)a.total_rows * (a.hq / a.c.hkv) > 0x7fffffff) {
         set_error("too many rows for one launch");
         return AG_ERR_INVALID_ARG;
     }

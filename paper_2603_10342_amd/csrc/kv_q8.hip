@@ -199,7 +199,7 @@ __global__ __launch_bounds__(256) void read_q8_kernel(RowArgs x)
 ag_status grid_of(const CacheView& c, int batch, int total, dim3* grid, int* heads)
 {
     const int64_t items = std::min<int64_t>(total / 16 + 2 * (int64_t)batch, total);
-    if (items > 0x7fffffff || c.hkv > 65535) { set_error("too many groups or heads for one launch"); return AG_ERR_INVALID_ARG; }
+    if (items > most_workgroups(256) || c.hkv > 65535) { set_error("too many groups or heads for one launch"); return AG_ERR_INVALID_ARG; }
     // KV heads a workgroup takes.  A group of one is the least latency, but the chip starts a workgroup every 2 ns: past 8192 of them several
     // heads together, up to 256 channels.  1, 2, 4 heads, us, 8 KV heads: 100 sessions of 1000..2000 tokens append x 64 156, 109, 93,
     // x 128 213, 182, 183, x 256 424, 416, 459, fp32 x 128 303, 301, 319; read x 64 172, 117, 93, x 128 254, 188, 194, x 256 385, 389, 437; but 32 of

@@ -25,6 +25,9 @@ ag_status launch_prefill(const Args& x, hipStream_t st);
 // few rows: the keys of 32 columns dealt to the waves of one workgroup
 ag_status launch_prefill_split(const Args& x, hipStream_t st);
 
+// Workgroups of a launch: HIP refuses 2^32 threads along a dimension of the grid.
+constexpr int64_t most_workgroups(int threads) { return 0xFFFFFFFFll / threads; }
+
 // Where a key's exponent byte stands in its group of 16 slots: the four that a lane of the score product needs are one word.
 __host__ __device__ inline int key_place(int slot) { return (slot & 3) * 4 + ((slot >> 2) & 3); }
 
