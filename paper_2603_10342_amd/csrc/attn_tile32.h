@@ -1,4 +1,4 @@
-// The 64-key x 32-query tile arithmetic of the matrix-core attention kernels (bf16, head_dim DT = 64 or 128):
+// The 64-key x 32-query tile arithmetic of the matrix-core attention kernels (bf16, head_dim DT = 64, 128 or 256):
 // S^T = K . Q^T and O^T += V^T . P^T on 32x32x16 MFMA with K and V tiles in LDS, and the softmax weights of a
 // tile under a reference maximum.  Shared by the prefill kernel and by the rows items of the merged decode-queue
 // kernel, which walk the same tiles over a part of the keys.  Internal; nothing here is part of the ABI.
@@ -183,6 +183,7 @@ __device__ __forceinline__ void softmax_and_value_product(bool do_sm, bool do_pv
         // its share of the 16 score pairs; the fences keep the compiler from regrouping them.
         constexpr int kAhead = kOperandsAhead, kMb = DT / 32, kN = 4 * kMb;
         constexpr int kEvery = kN > 16 ? kN / 16 : 1, kPairs = 16 * kEvery / kN, kStages = kN / kEvery;      // (at 256 channels a pair every other step)
+        static_assert(kPairs * kStages == 16 && kStages * kEvery == kN, "every pair of scores has its step: 64, 128 and 256 channels");
         bf16x8 opnd[kAhead + 1];
         auto operand = [&](int i) -> const unsigned char* { return vb + (i % kMb) * 512 + (i / kMb) * DT * 32; };
 #pragma unroll
