@@ -32,6 +32,7 @@ using splitk::find_share;
 using splitk::Share;
 
 constexpr int kTok = 64;                // tokens of a step
+constexpr int kWaves = 4;               // of a workgroup
 constexpr int kCols = 16;               // query heads of a pair, at most
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -69,7 +70,7 @@ __device__ __forceinline__ void query(const AttnArgs& a, int s, int g, int h0, i
     to_terms(row + chunk_of<DT, kExact>(h, c, chunks) * 16 + half * 8, q);
     if (r >= nh || 4 * h + c >= chunks) no_terms(q);
 }
-template <typename A, int DT, bool kExact, int kWaves>
+template <typename A, int DT, bool kExact>
 __device__ __forceinline__ void queries_to_lds(const AttnArgs& a, int s, int g, int h0, int nh, unsigned char* s_q)
 {
     constexpr int kTerms = terms_of<A>();
@@ -102,7 +103,7 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
 {
     constexpr int kTerms = terms_of<A>(), kH = key_blocks(DT), kV = DT / 16;          // 64-channel blocks of the keys, 16-channel blocks of the values
     const AttnArgs& a = x.a;
-    const int hkv = a.c.hkv, D = kExact ? DT : a.c.d, ps = a.c.ps, chunks = D >> 4;
+    const int D = kExact ? DT : a.c.d, ps = a.c.ps, chunks = D >> 4;
     const int r = lane & 15, c = lane >> 4;
     const float unit = a.scale * kLog2e;
     m = -INFINITY;
@@ -244,40 +245,38 @@ __device__ __forceinline__ void attend_steps(const Args& x, int s, int g, int h0
 }
 
 // LDS of a workgroup: per wave and head O, then m and l
-constexpr int kWaves = 4;
-inline size_t lds_of(int waves, int nh, int d) { return (size_t)waves * nh * (d + 2) * sizeof(float); }
+inline size_t lds_of(int nh, int d) { return (size_t)kWaves * nh * (d + 2) * sizeof(float); }
 
 // A wave's results of a pair's nh heads into LDS (s_o: [wave][head][D], then m and l [wave][head], `rows` heads a wave) ...
-template <int DT, bool kExact, int W>
+template <int DT, bool kExact>
 __device__ __forceinline__ void results_to_lds(float* s_o, int w, int rows, int nh, int D, int lane, float m, float lsum, const f32x4 (&o)[DT / 16])
 {
     const int r = lane & 15, c = lane >> 4;
-    float* const s_m = s_o + W * rows * D;
+    float* const s_m = s_o + kWaves * rows * D;
     if (r < nh) {
 #pragma unroll
         for (int mb = 0; mb < DT / 16; ++mb)
             if (kExact || mb * 16 < D) *reinterpret_cast<f32x4*>(s_o + (w * rows + r) * D + mb * 16 + c * 4) = o[mb];
-        if (c == 0) { s_m[w * rows + r] = m; s_m[(W + w) * rows + r] = lsum; }
+        if (c == 0) { s_m[w * rows + r] = m; s_m[(kWaves + w) * rows + r] = lsum; }
     }
 }
 // ... and the waves' together, of four channels of a head.
-template <int W>
 __device__ __forceinline__ f32x4 combine(const float* s_o, int rows, int D, int head, int d, float& ms, float& l)
 {
-    const float* const s_m = s_o + W * rows * D;
+    const float* const s_m = s_o + kWaves * rows * D;
     ms = s_m[head];
 #pragma unroll
-    for (int ww = 1; ww < W; ++ww) ms = fmaxf(ms, s_m[ww * rows + head]);
+    for (int ww = 1; ww < kWaves; ++ww) ms = fmaxf(ms, s_m[ww * rows + head]);
     const float ref = ms == -INFINITY ? 0.f : ms;
     l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ww = 0; ww < W; ++ww) {
+    for (int ww = 0; ww < kWaves; ++ww) {
         const float fw = __builtin_amdgcn_exp2f(s_m[ww * rows + head] - ref);         // a wave without steps has m = -inf -> 0
         const f32x4 y = *reinterpret_cast<const f32x4*>(s_o + (ww * rows + head) * D + d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += fw * y[e];
-        l += fw * s_m[(W + ww) * rows + head];
+        l += fw * s_m[(kWaves + ww) * rows + head];
     }
     return acc;
 }
@@ -309,13 +308,13 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
         float m, lsum;
         f32x4 o[DT / 16];
         if constexpr (queries_in_lds<A>()) {
-            queries_to_lds<A, DT, kExact, kWaves>(a, s, g, h0, nh, s_q);
+            queries_to_lds<A, DT, kExact>(a, s, g, h0, nh, s_q);
             __syncthreads();
         }
         attend_steps<A, DT, kExact, kWeightTerms, 1>(x, s, g, h0, nh, ctx, u + w * per, max(0, min(per, k - w * per)), lane, nullptr, s_q, m, lsum, o);
         lsum += __shfl_xor(lsum, 16);
         lsum += __shfl_xor(lsum, 32);
-        results_to_lds<DT, kExact, kWaves>(s_o, w, rows, nh, D, lane, m, lsum, o);
+        results_to_lds<DT, kExact>(s_o, w, rows, nh, D, lane, m, lsum, o);
         __syncthreads();
         // the pair starts at flat step base + pair n; its segments are numbered from the workgroup holding that step
         const int piece = wg - (base + pair * n) / q;
@@ -323,7 +322,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
             for (int idx = tid; idx < nh * (D / 4); idx += 64 * kWaves) {      // four channels a thread
                 const int head = idx / (D / 4), d = (idx - head * (D / 4)) * 4;
                 float ms, l;
-                const f32x4 acc = combine<kWaves>(s_o, rows, D, head, d, ms, l);
+                const f32x4 acc = combine(s_o, rows, D, head, d, ms, l);
                 const int64_t slot = ((int64_t)s * hq + (int64_t)g * G + h0 + head) * pmax + piece;
                 *reinterpret_cast<f32x4*>(ws_o + slot * D + d) = acc;
                 if (d == 0) { ws_ml[slot * 2] = ms; ws_ml[slot * 2 + 1] = l; }
@@ -350,12 +349,10 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
 // A batch of few, short contexts: one workgroup a pair, which writes its result itself - no plan, no partials, no merge, whose dependent
 // round trips are most of a small step.  Four waves and two workgroups a CU: eight are no faster alone (one session of 500 to 1000 tokens 7.8 us, four
 // 7.5) and leave room for half as many pairs (256 sessions of 1 to 512 46 us, four 29).
-constexpr int kDirectMaxTokens = 16 << 10;
 
 template <typename A, int DT, bool kExact, int kWeightTerms>
 __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_direct_kernel(Args x)
 {
-    constexpr int W = kWaves;
     extern __shared__ __attribute__((aligned(16))) unsigned char s_q[];   // as in the split kernel
     float* const s_o = reinterpret_cast<float*>(s_q + query_bytes<A>(DT));
     const AttnArgs& a = x.a;
@@ -367,29 +364,29 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_direc
     // the first step's pages beside the length, as a wave's steps are every fourth one whatever that is: a round trip
     // less (one session of 1000 tokens 8.8 -> 8.3 us, of 500 6.3 -> 6.1)
     const Ids first = pages_of(a, s, w, a.max_pages - 1);
-    const int ctx = min(a.ctx_lens[s], kDirectMaxTokens);
+    const int ctx = a.ctx_lens[s];
     asm volatile("" :: "s"(ctx), "s"(first.id[0]), "s"(first.id[1]), "s"(first.id[2]), "s"(first.id[3]));
     A* const out = (A*)a.out + ((int64_t)s * hq + (int64_t)g * G + h0) * D;
     if (ctx <= 0) {                     // uniform over the workgroup
-        for (int idx = tid; idx < nh * D; idx += 64 * W) out[idx] = (A)0.0f;
+        for (int idx = tid; idx < nh * D; idx += 64 * kWaves) out[idx] = (A)0.0f;
         return;
     }
     const int n = steps_of(ctx);
     float m, lsum;
     f32x4 o[DT / 16];
     if constexpr (queries_in_lds<A>()) {
-        queries_to_lds<A, DT, kExact, W>(a, s, g, h0, nh, s_q);
+        queries_to_lds<A, DT, kExact>(a, s, g, h0, nh, s_q);
         __syncthreads();
     }
-    attend_steps<A, DT, kExact, kWeightTerms, W>(x, s, g, h0, nh, ctx, w, max(0, (n - w + W - 1) / W), lane, &first, s_q, m, lsum, o);
+    attend_steps<A, DT, kExact, kWeightTerms, kWaves>(x, s, g, h0, nh, ctx, w, max(0, (n - w + kWaves - 1) / kWaves), lane, &first, s_q, m, lsum, o);
     lsum += __shfl_xor(lsum, 16);
     lsum += __shfl_xor(lsum, 32);
-    results_to_lds<DT, kExact, W>(s_o, w, rows, nh, D, lane, m, lsum, o);
+    results_to_lds<DT, kExact>(s_o, w, rows, nh, D, lane, m, lsum, o);
     __syncthreads();
-    for (int idx = tid; idx < nh * (D / 4); idx += 64 * W) {
+    for (int idx = tid; idx < nh * (D / 4); idx += 64 * kWaves) {
         const int head = idx / (D / 4), d = (idx - head * (D / 4)) * 4;
         float ms, l;
-        const f32x4 acc = combine<W>(s_o, rows, D, head, d, ms, l);
+        const f32x4 acc = combine(s_o, rows, D, head, d, ms, l);
         const float y[4] = {acc[0] / l, acc[1] / l, acc[2] / l, acc[3] / l};
         splitk::store_quad(out + head * D + d, y);
     }
@@ -468,11 +465,11 @@ ag_status launch(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
     const AttnArgs& a = x.a;
     const int G = a.hq / a.c.hkv;
-    const size_t lds = query_bytes<A>(DT) + lds_of(kWaves, std::min(G, kCols), a.c.d);
+    const size_t lds = query_bytes<A>(DT) + lds_of(std::min(G, kCols), a.c.d);
     if (lds > 64 * 1024) {
         static std::atomic<uint64_t> told[2] = {};
         const void* kernel = grid ? (const void*)decode_q8_split_kernel<A, DT, kExact, kWeightTerms> : (const void*)decode_q8_direct_kernel<A, DT, kExact, kWeightTerms>;
-        ag_status e = allow_dynamic_lds(kernel, query_bytes<A>(DT) + (int)lds_of(kWaves, kCols, DT), told[grid ? 0 : 1]);
+        ag_status e = allow_dynamic_lds(kernel, query_bytes<A>(DT) + (int)lds_of(kCols, DT), told[grid ? 0 : 1]);
         if (e) return e;
     }
     if (grid) hipLaunchKernelGGL((decode_q8_split_kernel<A, DT, kExact, kWeightTerms>), dim3(grid), dim3(64 * kWaves), lds, st, x, p.hdr, p.o, p.ml, p.pmax);
@@ -524,7 +521,7 @@ ag_status launch_merge(const Args& x, const Partials& p, hipStream_t st)
 bool one_workgroup_a_pair(const AttnArgs& a, int64_t pairs, int64_t cus)
 {
     const int64_t size = (int64_t)a.max_ctx * (a.c.d + 64), line = a.c.dtype == AG_BF16 ? 400000 : 290000;
-    return pairs <= most_workgroups(64 * kWaves) && a.max_ctx <= kDirectMaxTokens && 8 * size <= (2 * pairs > cus ? 8 : 5) * line;
+    return pairs <= most_workgroups(64 * kWaves) && 8 * size <= (2 * pairs > cus ? 8 : 5) * line;
 }
 
 }  // namespace

@@ -34,25 +34,6 @@ using tile32::tile_bytes;
 // two key and two value tiles
 constexpr int lds_bytes(int dt) { return 4 * tile_bytes(dt); }
 
-// S^T tile = K tile . Q^T, as tile32::qk_tile.  Vector units have nothing to do meanwhile: between(i) of DT / 8 runs behind product i.
-template <int DT, class Between>
-__device__ __forceinline__ void scores(const unsigned char* kb, const bf16x8 (&q)[DT / 16], f32x16 (&sc)[2], Between between)
-{
-    constexpr int kAhead = tile32::kOperandsAhead, kN = DT / 8;
-    bf16x8 opnd[kAhead + 1];
-    auto operand = [&](int i) -> const unsigned char* { return kb + (i & 1) * 512 + (i >> 1) * 2048; };
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) opnd[i] = *reinterpret_cast<const bf16x8*>(operand(i));
-    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-        if (i + kAhead < kN) opnd[(i + kAhead) % (kAhead + 1)] = *reinterpret_cast<const bf16x8*>(operand(i + kAhead));
-        sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opnd[i % (kAhead + 1)], q[i >> 1], i < 2 ? zero : sc[i & 1], 0, 0, 0);
-        between(i);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-}
-
 template <int NW, int DT, bool kExact>
 __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(Args x, Deal deal)
 {
@@ -207,7 +188,7 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
         begin_put(t, now, put);
         if (do_sm) {
             constexpr int kSteps = DT / 8;
-            scores<DT>(kb, qf, sc, [&](int i) {
+            tile32::qk_tile<DT>(kb, qf, sc, [&](int i) {
 #pragma unroll
                 for (int unit = i * kUnits / kSteps; unit < (i + 1) * kUnits / kSteps; ++unit) put_unit(unit, t, now, put);
             });
@@ -261,13 +242,6 @@ __global__ __launch_bounds__(64 * NW, DT > 128 ? 1 : 2) void prefill_q8_kernel(A
                 *reinterpret_cast<tile32::bf16x4*>(out + d) = y;
             }
     }
-}
-
-// sum_s ceil(N_s G / cols) <= total G / cols + batch, and no session has more than ceil(max_new G / cols)
-int64_t tiles_bound(const AttnArgs& a, int cols)
-{
-    const int64_t G = a.hq / a.c.hkv;
-    return std::min<int64_t>((int64_t)a.total_rows * G / cols + a.batch, (int64_t)a.batch * ((a.max_new * G + cols - 1) / cols));
 }
 
 template <int NW, int DT, bool kExact>

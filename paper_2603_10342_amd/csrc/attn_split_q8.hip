@@ -265,12 +265,6 @@ __global__ __launch_bounds__(64 * W, two_a_simd(DT) ? 2 : 1) void prefill_q8_spl
     }
 }
 
-int64_t tiles_bound(const AttnArgs& a)
-{
-    const int64_t G = a.hq / a.c.hkv;
-    return std::min<int64_t>((int64_t)a.total_rows * G / kCols + a.batch, (int64_t)a.batch * ((a.max_new * G + kCols - 1) / kCols));
-}
-
 template <typename A, int DT, bool kExact, int W>
 ag_status launch(const Args& x, hipStream_t st)
 {
@@ -281,11 +275,11 @@ ag_status launch(const Args& x, hipStream_t st)
         if (e) return e;
     }
     const AttnArgs& a = x.a;
-    if (a.c.hkv * tiles_bound(a) + kDealtPast > most_workgroups(64 * W) || (int64_t)a.total_rows * (a.hq / a.c.hkv) > 0x7fffffff) {
+    if (a.c.hkv * tiles_bound(a, kCols) + kDealtPast > most_workgroups(64 * W) || (int64_t)a.total_rows * (a.hq / a.c.hkv) > 0x7fffffff) {
         set_error("too many rows for one launch");
         return AG_ERR_INVALID_ARG;
     }
-    const Deal deal = deal_of(a, tiles_bound(a), std::max(1, stream_cus(st) * (two_a_simd(DT) ? 8 / W : 1) / 8));
+    const Deal deal = deal_of(a, tiles_bound(a, kCols), std::max(1, stream_cus(st) * (two_a_simd(DT) ? 8 / W : 1) / 8));
     prof_before(st);
     hipLaunchKernelGGL((prefill_q8_split_kernel<A, DT, kExact, W>), dim3((unsigned)workgroups_of(deal)), dim3(64 * W), lds, st, x, deal);
     prof_after(st);
@@ -299,7 +293,7 @@ ag_status launch(const Args& x, hipStream_t st)
 // heads x 64 (294) 27.7 -> 40, 11 of 27..286 on 472..7169 x 128 (314) 45 -> 66.
 bool four_waves(const AttnArgs& a, hipStream_t st)
 {
-    const int64_t few = a.c.hkv * tiles_bound(a), cus = stream_cus(st);
+    const int64_t few = a.c.hkv * tiles_bound(a, kCols), cus = stream_cus(st);
     return a.max_ctx <= 256 || 2 * few > (a.batch > 1 && a.max_ctx >= 2000 ? 3 : 2) * cus;
 }
 

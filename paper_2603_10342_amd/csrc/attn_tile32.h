@@ -58,9 +58,11 @@ template <> struct Weights<true> { float p[32]; };
 
 // S^T tile (64 keys x 32 queries) = K tile . Q^T.  kb: this lane's base in a K tile (key n, chunk hi).
 // Operand reads run kAhead matrix instructions ahead of their use; the two key blocks alternate so that
-// neighbouring matrix instructions write different accumulators.
-template <int DT = D>
-__device__ __forceinline__ void qk_tile(const unsigned char* kb, const bf16x8 (&qf)[DT / 16], f32x16 (&sc)[2])
+// neighbouring matrix instructions write different accumulators.  between(i) of DT / 8 runs behind product i: the vector units
+// have nothing else to do meanwhile.
+struct Nothing { __device__ __forceinline__ void operator()(int) const {} };
+template <int DT = D, class Between = Nothing>
+__device__ __forceinline__ void qk_tile(const unsigned char* kb, const bf16x8 (&qf)[DT / 16], f32x16 (&sc)[2], Between between = {})
 {
     constexpr int kAhead = kOperandsAhead, kN = DT / 8;
     bf16x8 opnd[kAhead + 1];
@@ -73,6 +75,7 @@ __device__ __forceinline__ void qk_tile(const unsigned char* kb, const bf16x8 (&
     for (int i = 0; i < kN; ++i) {
         if (i + kAhead < kN) opnd[(i + kAhead) % (kAhead + 1)] = *reinterpret_cast<const bf16x8*>(operand(i + kAhead));
         sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opnd[i % (kAhead + 1)], qf[i >> 1], i < 2 ? zero : sc[i & 1], 0, 0, 0);
+        between(i);
         __builtin_amdgcn_sched_barrier(0);
     }
 }

@@ -103,17 +103,16 @@ __global__ __launch_bounds__(256) void append_q8_kernel(RowArgs x)
     const int tid = threadIdx.x, h0 = blockIdx.y * kHeads, d = x.d, chunks = d >> 4, ll = x.lanes_log2;
     const int64_t block = (int64_t)d * x.ps, at = o.page * x.hkv + h0;
     const int lines = 2 * o.n_tok * kHeads;                            // rows: keys of the tokens, then values; the heads of a token in turn
-    struct Piece { Row16<A> raw; };
     for (int i0 = tid; i0 < lines << ll; i0 += 256 * kAtOnce) {
-        Piece p[kAtOnce];
+        Row16<A> raw[kAtOnce];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             const int idx = i0 + j * 256, line = idx >> ll, c = idx & ((1 << ll) - 1), tt = line / kHeads, t = tt >= o.n_tok ? tt - o.n_tok : tt;
-            p[j].raw = {};
+            raw[j] = {};
             if (line < lines && c < chunks) {
                 const u32x4* src = reinterpret_cast<const u32x4*>((const A*)(tt >= o.n_tok ? x.v : x.k) + ((o.row0 + t) * x.hkv + h0 + line % kHeads) * d + c * 16);
 #pragma unroll
-                for (int i = 0; i < (int)sizeof(A); ++i) p[j].raw.w[i] = src[i];
+                for (int i = 0; i < (int)sizeof(A); ++i) raw[j].w[i] = src[i];
             }
         }
 #pragma unroll
@@ -123,7 +122,7 @@ __global__ __launch_bounds__(256) void append_q8_kernel(RowArgs x)
             const bool value = tt >= o.n_tok;
             const int t = value ? tt - o.n_tok : tt, slot = o.slot0 + t;
             float f[16];
-            channels(p[j].raw, f);
+            channels(raw[j], f);
             uint32_t most = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = max(most, size_of(f[i]));

@@ -2,6 +2,8 @@
 // e4m3 numbers and the types that arithmetic runs in.
 #pragma once
 
+#include <algorithm>
+
 #include "ag_internal.h"
 #include "ag_q8.h"
 #include "bf16_terms.h"
@@ -27,6 +29,13 @@ ag_status launch_prefill_split(const Args& x, hipStream_t st);
 
 // Workgroups of a launch: HIP refuses 2^32 threads along a dimension of the grid.
 constexpr int64_t most_workgroups(int threads) { return 0xFFFFFFFFll / threads; }
+
+// Tiles of `cols` columns of a KV head: sum_s ceil(N_s G / cols) <= total G / cols + batch, and no session has more than ceil(max_new G / cols).
+inline int64_t tiles_bound(const AttnArgs& a, int cols)
+{
+    const int64_t G = a.hq / a.c.hkv;
+    return std::min<int64_t>((int64_t)a.total_rows * G / cols + a.batch, (int64_t)a.batch * ((a.max_new * G + cols - 1) / cols));
+}
 
 // Where a key's exponent byte stands in its group of 16 slots: the four that a lane of the score product needs are one word.
 __host__ __device__ inline int key_place(int slot) { return (slot & 3) * 4 + ((slot >> 2) & 3); }

@@ -1,10 +1,13 @@
 """The tile arithmetic spreads 16 pairs of scores over its steps: widths where that leaves pairs out do not compile."""
+import os
+import shutil
 import subprocess
 
 import pytest
 
 from paper_2603_10342_amd import build
 
+pytestmark = pytest.mark.skipif(not os.path.exists(build.HIPCC) and shutil.which("hipcc") is None, reason="needs hipcc")
 SOURCE = """#include "attn_tile32.h"
 __global__ void k(float* p)
 {
