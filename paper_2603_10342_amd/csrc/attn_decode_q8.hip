@@ -348,7 +348,9 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_split
 
 // A batch of few, short contexts: one workgroup a pair, which writes its result itself - no plan, no partials, no merge, whose dependent
 // round trips are most of a small step.  Four waves and two workgroups a CU: eight are no faster alone (one session of 500 to 1000 tokens 7.8 us, four
-// 7.5) and leave room for half as many pairs (256 sessions of 1 to 512 46 us, four 29).
+// 7.5) and leave room for half as many pairs (256 sessions of 1 to 512 46 us, four 29).  Beside the split kernel's loop, whose steps follow one another, this
+// one holds about 50 registers more (239 of them for 188 at 128 channels, one term): two waves a SIMD instead of three at 96, and spills at padded widths - 12 registers at 112
+// channels, 45 at 208 to 240, with fp32 queries 4 and 3 (240 channels, 64 sessions of 1 to 512 27.8 us, with one term and 29 spilled 24.0).
 
 template <typename A, int DT, bool kExact, int kWeightTerms>
 __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void decode_q8_direct_kernel(Args x)
@@ -483,8 +485,8 @@ ag_status launch(const Args& x, const Partials& p, int grid, hipStream_t st)
 // 75.5 -> 73.7.
 bool rounds_weights(const AttnArgs& a) { return a.c.dtype == AG_BF16 && a.c.d == 128 && a.c.ps == 16 && a.hq <= kCols * a.c.hkv; }
 
-// The least of five widths that holds a head: 96 channels in 128 are 15 to 25 % slower (64 sessions of 1000..2000 tokens 34.9 us, 27.6), 192 in 256 as much
-// (66.2, 58.1).
+// The least of five widths that holds a head: 96 channels in 128 are 25 to 30 % slower (64 sessions of 1000..2000 tokens 36.5 us, 27.7; of 1..512 11.4, 9.1), 192 in 256 20 % (70.3,
+// 58.1).
 template <typename A>
 ag_status launch_typed(const Args& x, const Partials& p, int grid, hipStream_t st)
 {
@@ -513,11 +515,12 @@ ag_status launch_merge(const Args& x, const Partials& p, hipStream_t st)
 // A workgroup alone takes 2 us for every 256 tokens, with fp32 queries 2.6, and the longest pair's is the least a launch takes (the host
 // knows no other length); shares take about 10 whatever the context of few pairs, and a segment each - 2.5 us - for short pairs one after
 // the other.  Past half of the CUs a pair each keeps them busy anyway; long contexts are left to shares, as one among short ones would be
-// all that a launch waits for.  Graph replay, shares -> one workgroup a pair, us (pairs at 256 CUs), 8 KV heads, x 128: one session of 1000 tokens (8) 9.3 -> 8.5, 1600 (8)
-// 11.8 -> 12.3, 2400 (8) 12.7 -> 16.5, 8 of 1000 (64) 10.1 -> 10.0, 16 of 1600 (128) 16.8 -> 14.4, 32 of 2400 (256) 30.6 -> 27.1, of 500 to 4000 (256) 31.0 -> 30.6, 64 of 1 to 128
-// (512) 25.7 -> 6.9, of 1 to 512 28.2 -> 9.7, of 1000 to 2000 39.0 -> 35.2, of 1024 to 4096 64.5 -> 65.4, 256 of 1000 to 2000 (2048) 145 -> 130; x 64: one of 1600 10.1 -> 9.4,
-// 2400 11.1 -> 12.6, 64 of 1000 to 2000 23.1 -> 19.6; x 256: one of 1000 13.6 -> 16.3, 64 of 1000 to 2000 75.5 -> 68.9; fp32 x 128: one of 1000 11.1 -> 12.2, 16 of 1600 20.6 -> 18.8, 64 of
-// 1000 to 2000 41.7 -> 38.3, 16 of 1024 to 4096 25.0 -> 32.4.
+// all that a launch waits for.  Graph replay, shares -> one workgroup a pair, us (pairs at 256 CUs), 8 KV heads, x 128 on pages of 16: one session of 1000 tokens (8) 9.4 ->
+// 8.5, 1600 (8) 11.9 -> 12.5, 2400 (8) 12.7 -> 16.2, 8 of 1000 (64) 9.9 -> 9.6, 16 of 1600 (128) 16.8 -> 14.5, 32 of 2400 (256) 29.3 -> 26.4, of 500 to 4000 (256) 30.2 -> 29.0, 64 of 1 to
+// 128 (512) 25.4 -> 6.2, of 1 to 512 27.5 -> 10.0, of 1000 to 2000 39.0 -> 33.5, of 1024 to 4096 63.9 -> 62.5, 256 of 1000 to 2000 (2048) 142 -> 127; weights in 24 bits, pages of 32: one of
+// 1000 9.9 -> 10.3, 1600 12.8 -> 14.5, 64 of 1000 to 2000 38.5 -> 35.5; x 64: one of 1600 10.6 -> 10.5, 2400 12.0 -> 14.7, 64 of 1000 to 2000 24.0 -> 20.4; x 96: one of 1000 9.4 -> 9.0, 64 of
+// 1000 to 2000 31.5 -> 28.1; x 256: one of 500 13.4 -> 10.9, 1000 13.3 -> 16.3, 64 of 1000 to 2000 75.9 -> 71.5; fp32 x 128: one of 1000 10.9 -> 11.7, 16 of 1600 20.0 -> 18.0, 64 of 1000 to 2000
+// 40.8 -> 37.4, 16 of 1024 to 4096 24.8 -> 32.7.
 bool one_workgroup_a_pair(const AttnArgs& a, int64_t pairs, int64_t cus)
 {
     const int64_t size = (int64_t)a.max_ctx * (a.c.d + 64), line = a.c.dtype == AG_BF16 ? 400000 : 290000;

@@ -10,7 +10,9 @@
 //   iteration t: K(t + 2) and V(t + 1) requested into registers; S(t) = K(t) Q^T, and between its products K(t + 1) and V(t), which are
 //   in registers, converted and written to LDS; P(t) side by side with O += V(t - 1) P(t - 1); barrier.
 // The conversions - 40 vector instructions a wave and tile at NW = 8 and 128 channels, beside 100 of the softmax - so run while the vector units
-// have nothing else; ahead of the products eight prompts of 4096 tokens took 1222 us, so 1134 (970 TFLOP/s; over a bf16 cache 1120).
+// have nothing else; ahead of the products eight prompts of 4096 tokens took 1222 us, so 1134 (970 TFLOP/s).  Over a bf16 cache,
+// whose tiles need no conversion, they take 1026 where these take 1100 (one session of measurements); 8 of 512 38.6 and 45.1, one of 2048 51 and 57, 32 chunks of
+// 128..1024 rows on 2048..8192 tokens 1770 and 1812.
 // Weights are rounded to bf16 for the value product at every shape, where bf16 caches have that for 128 channels on pages of 16 only: an error of up to
 // 2^-8 of a weight, each for itself, beside 2^-4 of a cached value and 2^-8 of the output.  As three terms, 24 bits: eight prompts of 2000 x 64 202 -> 307 us,
 // x 256 776 -> 1229, eight of 4096 x 128 1124 -> 2129 (by attn_split_q8.hip: tiles spill); 64-bit attention over the cached numbers differs from the output by 1.05 to 1.33 times
