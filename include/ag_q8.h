@@ -23,6 +23,7 @@
  *     q, out, k_new, v_new, k_out, v_out, the pools and exps 16-byte aligned (AG_ERR_INVALID_ARG otherwise).
  *   - max_ctx is at most 2^31 - 1025 (AG_ERR_INVALID_ARG beyond it).
  *   - Slots that no token uses may hold anything, NaN included: they are read, but nothing depends on them.  Table entries that no token uses are not followed.
+ *     (ag_debug_validate looks at tables and lengths only: it takes an ag_kv_cache of the same num_pages, page_size, num_kv_heads, head_dim and dtype.)
  *   - fp32 activations keep 24 bits of queries and softmax weights in the products, as three bf16 terms, in every call.  bf16 activations: decode
  *     keeps them too, but with head_dim 128, page_size 16 and up to 16 heads a group, where weights are rounded to bf16 as over a bf16 cache of that
  *     shape; prefill and resume round them at every shape (over bf16 caches at that one only): off by up to 2^-8 of themselves, each for itself, beside

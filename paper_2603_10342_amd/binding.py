@@ -514,8 +514,11 @@ def ag_device_info() -> dict:
     return {"num_cus": cus.value, "num_xcd": xcd.value, "wavefront_size": wave.value, "arch": name.value.decode()}
 
 
-def ag_debug_validate(cache: KVCache, block_tables, prefix_lens, new_lens, cu_new, stream=None):
+def ag_debug_validate(cache, block_tables, prefix_lens, new_lens, cu_new, stream=None):
+    """A KVCache, or a KVCacheQ8: only tables and lengths are looked at, against the cache's pages."""
     c = cache.c_struct()
+    if isinstance(c, ag_kv_cache_q8):
+        c = ag_kv_cache(c.k_pool, c.v_pool, c.num_pages, c.page_size, c.num_kv_heads, c.head_dim, c.dtype)
     _check(lib().ag_debug_validate(C.byref(c), _i32(block_tables), block_tables.shape[1], _i32(prefix_lens),
                                    _i32(new_lens), _i32(cu_new), new_lens.shape[0], _stream(stream)))
 

@@ -293,7 +293,8 @@ bool split_preferred(const AttnArgs& a, hipStream_t st)
     return split < tiles;
 }
 
-// 256 columns a workgroup, bf16 x 128: a tile is brought in for twice the columns, but a launch ends on longer chains.  Where the context is
+// 256 columns a workgroup, bf16 x 128 (at 64 channels eight waves would each bring half a piece a lane, at 256 there are no registers): a tile is
+// brought in for twice the columns, but a launch ends on longer chains.  Where the context is
 // long, and there are workgroups for two a CU, or one and chunks that are alike beside their contexts.  Graph replay, 128 -> 256 columns, us (of the larger a
 // CU): eight prompts of 4096 (16) 1203 -> 1134, 32 chunks of 128..1024 on 2048..8192 (9.5) 1931 -> 1874, of 100..200 on 2000..4000 (2.6) 294 -> 281, two
 // of 1000 on 2000 (1) 101 -> 93; but one prompt of 2048 (1) 58 -> 64, eight of 512 (2) 43 -> 48, 64 of 600 (19) 353 -> 380, 16 of 1500 (12) 383 -> 389, one chunk of 1000

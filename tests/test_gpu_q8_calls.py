@@ -116,3 +116,20 @@ def test_decodes_and_chunks_in_one_batch(few_cus, dtype, d, page):  # noqa: F811
     q, scale = side.draw(int(new.sum()), 8, d), d ** -0.5
     for stream in (None, few_cus):
         check_resume(side, q, resume(side, q, new, 8, scale, stream=stream), new, scale, (d, page))
+
+
+def test_the_checker_of_tables_takes_an_8_bit_cache():
+    side = Side("f32", 96, 64, 2, [130, 64], seed=1)
+    side.append([130, 64])
+    lens, none, cu = i32([130, 64]), i32([0, 0]), i32([0, 0, 0])
+    B.ag_debug_validate(side.cache, side.bt_dev, lens, none, cu)
+    bt = side.bt.copy()
+    bt[1, 1] = 1 << 30                                            # not in use
+    B.ag_debug_validate(side.cache, i32(bt), lens, none, cu)
+    for at, page in (((0, 2), side.cache.num_pages), ((1, 0), -1)):
+        bad = bt.copy()
+        bad[at] = page
+        with pytest.raises(B.AgError, match="outside"):
+            B.ag_debug_validate(side.cache, i32(bad), lens, none, cu)
+    with pytest.raises(B.AgError, match="cu_new"):
+        B.ag_debug_validate(side.cache, side.bt_dev, none, lens, i32([0, 130, 130]))
