@@ -36,6 +36,11 @@ EXPORTS = [
     # ag_q8.h
     "ag_kv_append_q8", "ag_kv_read_q8", "ag_attn_prefill_q8", "ag_attn_resume_q8", "ag_attn_decode_q8_workspace_bytes",
     "ag_attn_decode_q8",
+    # ag_rope.h
+    "ag_rope_turns", "ag_rope_rows", "ag_kv_append_rope",
+    # ag_latent.h
+    "ag_latent_row", "ag_kv_append_latent", "ag_attn_decode_latent_workspace_bytes", "ag_attn_decode_latent",
+    "ag_attn_resume_latent_workspace_bytes", "ag_attn_resume_latent",
     # ag_sched.h
     "ag_ctl_create", "ag_ctl_destroy", "ag_ctl_record_decode", "ag_ctl_tick", "ag_ctl_get", "ag_ctl_classify",
     "ag_partition_level_for", "ag_slots_create", "ag_slots_destroy", "ag_slots_count", "ag_slots_units",
@@ -86,6 +91,14 @@ class ag_kv_cache_q8(C.Structure):
                 ("page_size", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
+class ag_rope(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float)]
+
+
+class ag_latent_cache(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("num_pages", C.c_int32), ("page_size", C.c_int32), ("latent_dim", C.c_int32), ("rope_dim", C.c_int32)]
+
+
 _lib = None
 
 
@@ -122,6 +135,18 @@ def lib():
     l.ag_attn_decode_q8_workspace_bytes.argtypes = [i32, i32, i32, i32]
     l.ag_attn_decode_q8_workspace_bytes.restype = C.c_size_t
     l.ag_attn_decode_q8.argtypes = [c8, vp, vp, i32p, i32, i32p, i32, i32, i32, C.c_float, vp, C.c_size_t, vp]
+    i64, f64, rp, cl = C.c_int64, C.c_double, C.POINTER(ag_rope), C.POINTER(ag_latent_cache)
+    l.ag_rope_turns.argtypes = [C.POINTER(f64), i32, f64, i32, f64, f64, f64, f64]
+    l.ag_rope_rows.argtypes = [rp, i32, vp, i64, i64, vp, i64, i64, i32, i32, i32p, i32p, i32p, i32, i32, i32, vp]
+    l.ag_kv_append_rope.argtypes = [cp, rp, vp, vp, i32, vp, vp, i32p, i32, i32p, i32p, i32p, i32, i32, vp]
+    l.ag_latent_row.argtypes = [i32, i32]
+    l.ag_kv_append_latent.argtypes = [cl, rp, vp, i64, vp, i64, i32p, i32, i32p, i32p, i32p, i32, i32, vp]
+    l.ag_attn_decode_latent_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    l.ag_attn_decode_latent_workspace_bytes.restype = C.c_size_t
+    l.ag_attn_decode_latent.argtypes = [cl, vp, vp, i32p, i32, i32p, i32, i32, i32, C.c_float, vp, C.c_size_t, vp]
+    l.ag_attn_resume_latent_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    l.ag_attn_resume_latent_workspace_bytes.restype = C.c_size_t
+    l.ag_attn_resume_latent.argtypes = [cl, vp, vp, i32p, i32, i32p, i32p, i32p, i32, i32, i32, i32, i32, C.c_float, vp, C.c_size_t, vp]
     l.ag_stream_create_cumask.argtypes = [C.POINTER(vp), u32p, i32]
     l.ag_stream_destroy.argtypes = [vp]
     l.ag_cumask_build.argtypes = [u32p, i32, i32, i32, i32, i32]
@@ -160,7 +185,7 @@ def lib():
     l.ag_pager_page_state.argtypes = [vp, i32]
     l.ag_pager_get_stats.argtypes = [vp, C.POINTER(ag_pager_stats)]
     for name in EXPORTS:
-        if name not in ("ag_attn_decode_workspace_bytes", "ag_decode_step_workspace_bytes", "ag_attn_merged_workspace_bytes", "ag_attn_decode_q8_workspace_bytes", "ag_status_string", "ag_last_error", "ag_version"):
+        if not name.endswith("_workspace_bytes") and name not in ("ag_status_string", "ag_last_error", "ag_version"):
             getattr(l, name).restype = C.c_int
     l.ag_status_string.argtypes = [C.c_int]
     for name in ("ag_status_string", "ag_last_error", "ag_version"):
@@ -171,7 +196,8 @@ def lib():
 
 _native = None
 _CALLS = ("kv_append", "attn_prefill", "attn_resume", "attn_decode", "attn_decode_static", "decode_step", "attn_merged",
-          "kv_append_q8", "kv_read_q8", "attn_prefill_q8", "attn_resume_q8", "attn_decode_q8")
+          "kv_append_q8", "kv_read_q8", "attn_prefill_q8", "attn_resume_q8", "attn_decode_q8",
+          "rope_rows", "kv_append_rope", "kv_append_latent", "attn_decode_latent", "attn_resume_latent")
 
 
 class _NoCalls:
@@ -194,7 +220,7 @@ def _load_calls():
     here = f"torch {torch.__version__} python {sys.version_info[0]}.{sys.version_info[1]}"
     if getattr(m, "built_for", None) != here:                 # it reads torch's and Python's objects directly
         raise ImportError(f"{CALL_PATH} is built for {getattr(m, 'built_for', 'an unknown torch')}, this is {here}")
-    m.setup(KVCache, KVCacheQ8, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+    m.setup(KVCache, KVCacheQ8, Rope, LatentCache, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
             *(C.cast(getattr(l, "ag_" + name), C.c_void_p).value for name in _CALLS))
     return m
 
@@ -481,6 +507,136 @@ def ag_attn_decode_q8(cache: KVCacheQ8, q, out, block_tables, ctx_lens, max_ctx:
     _check(lib().ag_attn_decode_q8(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1],
                                    _i32(ctx_lens), ctx_lens.shape[0], max_ctx, num_q_heads, scale, _ptr(workspace),
                                    workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+AG_ROPE_HALVES, AG_ROPE_PAIRS = 0, 1
+AG_ROPE_PLAIN, AG_ROPE_LINEAR, AG_ROPE_RAMP = 0, 1, 2
+
+
+def ag_rope_turns(rot_dim: int, base: float = 10000.0, scaling: int = AG_ROPE_PLAIN, factor: float = 1.0, trained_len: float = 0.0,
+                  low: float = 0.0, high: float = 0.0) -> torch.Tensor:
+    """Turns a position of every pair, fp64 on the host."""
+    turns = torch.empty(max(rot_dim // 2, 0), dtype=torch.float64)
+    _check(lib().ag_rope_turns(C.cast(turns.data_ptr(), C.POINTER(C.c_double)), rot_dim, base, scaling, factor, trained_len, low, high))
+    return turns
+
+
+class Rope:
+    """A rotation (mirrors ag_rope): `turns` of every pair, fp64 on the GPU (ag_rope_turns() makes some), which channels make a pair, and the magnitude."""
+
+    def __init__(self, turns: torch.Tensor, layout: int = AG_ROPE_HALVES, magnitude: float = 1.0):
+        if turns.dtype != torch.float64 or turns.dim() != 1:
+            raise TypeError("turns are one fp64 number a pair")
+        self.turns, self.rot_dim, self.layout, self.magnitude = turns, 2 * turns.shape[0], layout, float(magnitude)
+
+    def c_struct(self) -> ag_rope:
+        return ag_rope(_ptr(self.turns), self.rot_dim, self.layout, self.magnitude)
+
+
+def _rows(t: torch.Tensor, dims: int):
+    """Device pointer and element strides of rows whose channels are contiguous."""
+    if not t.is_cuda or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] != 1):
+        raise ValueError(f"rows must come from CUDA/ROCm tensors of {dims} dimensions with contiguous channels")
+    return (t.data_ptr(), *t.stride()[:-1])
+
+
+def _rope_dtype(t: torch.Tensor) -> int:
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("rows are float32 or bfloat16")
+    return AG_F32 if t.dtype == torch.float32 else AG_BF16
+
+
+def ag_rope_rows(rope: Rope, x, y, prefix_lens, new_lens, cu_new, total_new: int, transposed: bool = False, stream=None):
+    """x and y are [T][heads][head_dim] of any token and head strides; y may be x."""
+    st = (_native or _calls()).rope_rows(rope, x, y, prefix_lens, new_lens, cu_new, total_new, transposed, stream)
+    if st is not None:
+        return _check(st)
+    if x.shape != y.shape or x.dtype != y.dtype:
+        raise ValueError("x and y are rows of one shape and dtype")
+    r = rope.c_struct()
+    xp, xt, xh = _rows(x, 3)
+    yp, yt, yh = _rows(y, 3)
+    if total_new > x.shape[0]:
+        raise ValueError("total_new exceeds the rows")
+    _check(lib().ag_rope_rows(C.byref(r), _rope_dtype(x), xp, xt, xh, yp, yt, yh, x.shape[1], x.shape[2], _i32(prefix_lens), _i32(new_lens),
+                              _i32(cu_new), new_lens.shape[0], total_new, int(transposed), _stream(stream)))
+
+
+def ag_kv_append_rope(cache: KVCache, rope: Rope, q, q_out, k_new, v_new, block_tables, prefix_lens, new_lens, cu_new, total_new: int, stream=None):
+    """q and q_out are [T][Hq][D], or None both."""
+    st = (_native or _calls()).kv_append_rope(cache, rope, q, q_out, k_new, v_new, block_tables, prefix_lens, new_lens, cu_new, total_new, stream)
+    if st is not None:
+        return _check(st)
+    c, r = cache.c_struct(), rope.c_struct()
+    _check(lib().ag_kv_append_rope(C.byref(c), C.byref(r), _ptr(q), _ptr(q_out), 0 if q is None else q.shape[1], _ptr(k_new), _ptr(v_new),
+                                   _i32(block_tables), block_tables.shape[1], _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0],
+                                   total_new, _stream(stream)))
+
+
+def ag_latent_row(latent_dim: int, rope_dim: int) -> int:
+    return int(lib().ag_latent_row(latent_dim, rope_dim))
+
+
+class LatentCache:
+    """Caller-owned pool of a latent cache plus its geometry (mirrors ag_latent_cache); rows of ag_latent_row() bf16 numbers."""
+
+    def __init__(self, num_pages: int, page_size: int, latent_dim: int, rope_dim: int, device="cuda", fill: Optional[float] = None):
+        row = ag_latent_row(latent_dim, rope_dim)
+        if row == 0:
+            raise ValueError("a latent cache has a latent_dim of 128, 256 or 512 and a rope_dim of 32 or 64")
+        shape = (num_pages, page_size, row)
+        self.pool = torch.empty(shape, dtype=torch.bfloat16, device=device) if fill is None else torch.full(shape, fill, dtype=torch.bfloat16, device=device)
+        self.num_pages, self.page_size, self.latent_dim, self.rope_dim = num_pages, page_size, latent_dim, rope_dim
+
+    def c_struct(self) -> ag_latent_cache:
+        return ag_latent_cache(self.pool.data_ptr(), self.num_pages, self.page_size, self.latent_dim, self.rope_dim)
+
+
+def ag_kv_append_latent(cache: LatentCache, rope: Optional[Rope], latent_new, rope_new, block_tables, prefix_lens, new_lens, cu_new, total_new: int,
+                        stream=None):
+    """latent_new [T][latent_dim] and rope_new [T][rope_dim] of any token strides; rope None: rope_new is rotated already."""
+    st = (_native or _calls()).kv_append_latent(cache, rope, latent_new, rope_new, block_tables, prefix_lens, new_lens, cu_new, total_new, stream)
+    if st is not None:
+        return _check(st)
+    if latent_new.dtype != torch.bfloat16 or rope_new.dtype != torch.bfloat16:
+        raise TypeError("rows of a latent cache are bfloat16")
+    lp, lt = _rows(latent_new, 2)
+    rp, rt = _rows(rope_new, 2)
+    if latent_new.shape[1] != cache.latent_dim or rope_new.shape[1] != cache.rope_dim:
+        raise ValueError("rows have the cache's latent_dim and rope_dim channels")
+    c, r = cache.c_struct(), None if rope is None else rope.c_struct()
+    _check(lib().ag_kv_append_latent(C.byref(c), None if r is None else C.byref(r), lp, lt, rp, rt, _i32(block_tables), block_tables.shape[1],
+                                     _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0], total_new, _stream(stream)))
+
+
+def ag_attn_decode_latent_workspace_bytes(batch: int, num_q_heads: int, latent_dim: int, max_ctx: int) -> int:
+    return int(lib().ag_attn_decode_latent_workspace_bytes(batch, num_q_heads, latent_dim, max_ctx))
+
+
+def ag_attn_decode_latent(cache: LatentCache, q, out, block_tables, ctx_lens, max_ctx: int, num_q_heads: int, scale: float, workspace: torch.Tensor,
+                          stream=None):
+    st = (_native or _calls()).attn_decode_latent(cache, q, out, block_tables, ctx_lens, max_ctx, num_q_heads, scale, workspace, stream)
+    if st is not None:
+        return _check(st)
+    c = cache.c_struct()
+    _check(lib().ag_attn_decode_latent(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1], _i32(ctx_lens), ctx_lens.shape[0],
+                                       max_ctx, num_q_heads, scale, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def ag_attn_resume_latent_workspace_bytes(batch: int, total_new: int, num_q_heads: int, latent_dim: int, max_ctx: int) -> int:
+    return int(lib().ag_attn_resume_latent_workspace_bytes(batch, total_new, num_q_heads, latent_dim, max_ctx))
+
+
+def ag_attn_resume_latent(cache: LatentCache, q, out, block_tables, prefix_lens, new_lens, cu_new, total_new: int, max_new: int, max_ctx: int,
+                          num_q_heads: int, scale: float, workspace: torch.Tensor, stream=None):
+    st = (_native or _calls()).attn_resume_latent(cache, q, out, block_tables, prefix_lens, new_lens, cu_new, total_new, max_new, max_ctx, num_q_heads,
+                                                  scale, workspace, stream)
+    if st is not None:
+        return _check(st)
+    c = cache.c_struct()
+    _check(lib().ag_attn_resume_latent(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1], _i32(prefix_lens), _i32(new_lens),
+                                       _i32(cu_new), new_lens.shape[0], total_new, max_new, max_ctx, num_q_heads, scale, _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def ag_cumask_build(total_cus: int, n_xcd: int, first_cu_per_xcd: int, cus_per_xcd: int) -> list:

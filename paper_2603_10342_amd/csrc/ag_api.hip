@@ -70,7 +70,7 @@ static int log2_exact(int x)
     return s;
 }
 
-static ag_status view_cache(const ag_kv_cache* c, CacheView* v)
+ag_status view_cache(const ag_kv_cache* c, CacheView* v)
 {
     if (!c) { set_error("cache is NULL"); return AG_ERR_INVALID_ARG; }
     if (!c->k_pool || !c->v_pool) { set_error("cache pools are NULL"); return AG_ERR_INVALID_ARG; }

@@ -51,6 +51,8 @@ struct AttnArgs {
 
 void set_error(const char* fmt, ...);
 ag_status hip_check(hipError_t e, const char* what);
+// The checked view of a caller's cache.
+ag_status view_cache(const ag_kv_cache* c, CacheView* v);
 
 // Lets `kernel` be launched on the current device with `bytes` of dynamic LDS, more than the 64 KiB a kernel may use
 // without being told so.  The attribute belongs to a device: `devices` keeps the ones it has been set on.

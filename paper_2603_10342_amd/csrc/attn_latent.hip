@@ -1,0 +1,688 @@
+// Attention over the latent cache (include/ag_latent.h): one row a token is key and value of every query head,
+//     S = scale * Q . row,   O = softmax(S) . row[0 .. L)
+// so that the rows of a tile serve all heads of all the query rows that see it.  Decode reads ctx * (L + R) * 2 bytes for 2 H ctx (2 L + R) operations: 242 a byte at
+// 128 heads, where the matrix units and memory are about equally long; fewer heads are bound by memory, chunks of rows by the matrix units.
+//
+// A workgroup holds 128, 64 or 32 columns - (query row, head) pairs of one session, rows that follow each other - and walks 32-token tiles of its rows:
+//     S^T (32 tokens x 32 columns) = rows . Q^T     O^T (L channels x 32 columns) += rows^T . P^T         on 32x32x16 bf16 MFMA
+// Q^T stays in registers, O^T in fp32 accumulators: of 512 channels and 128 columns together 80 % of a CU's registers, so that one workgroup of four waves is
+// all a CU holds and latency is hidden by order alone: the tile after the next is on its way, and the softmax of a tile runs beside the value product of the one
+// before.  With 64 or 32 columns, waves share columns and divide the channels of O; each takes the scores again, which memory's pace leaves time for.
+//
+// One tile in LDS feeds both products: scores read it along a row (16 bytes a lane), values across rows, by transposing reads.  Tiles come in by direct
+// global-to-LDS loads.
+//
+// Work is dealt in equal shares of key tiles, one a workgroup and CU: units (session, column tile) lie end to end, a share cuts them where it ends, and the
+// pieces' partial (max, sum, O) go through the workspace and are merged in order by a second launch.
+#include <algorithm>
+#include <atomic>
+
+#include "latent_internal.h"
+#include "lds_dma.h"
+
+namespace ag {
+namespace latent {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTokens = 32;             // of a tile
+constexpr int kStages = 4;              // tiles in LDS: the one whose values are taken, the one whose scores are, two on their way
+constexpr int kMostShares = 256;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kRescaleSlack = 8.0f;   // log2 units a column's maximum may exceed m when the ordered path leaves m alone
+constexpr float kWeightSumLimit = 16384.0f;   // a lane's 16 weights of a tile may sum to this much before m is moved
+
+// ---- how a batch is cut ----
+
+// Columns of a tile: whole query rows' heads while they fit (m rows of `heads` columns), otherwise parts of one row's heads (nh tiles a row).
+struct Cut {
+    int cols, heads, m, nh;
+    __host__ __device__ Cut(int cols_, int heads_) : cols(cols_), heads(heads_), m(heads_ < cols_ ? cols_ / heads_ : 1), nh((heads_ + cols_ - 1) / cols_) {}
+};
+
+// Work is counted in tiles of 32 keys for decode.  A chunk's column tile k counts the keys that its last row sees, P + min((k + 1) m, N), so that the
+// sum over the tiles of a session has a closed form; shares are multiples of 32 of that.
+template <bool kDecode> struct Counting { typedef uint32_t Cost; static constexpr int kTile = 1; };
+template <> struct Counting<false> { typedef uint64_t Cost; static constexpr int kTile = kTokens; };
+
+struct Lens { int prefix, n, row0; };   // of a session
+template <bool kDecode>
+__device__ __forceinline__ Lens lens_of(const AttnArgs& a, int s)
+{
+    if constexpr (kDecode) {
+        const int ctx = a.ctx_lens[s];
+        return Lens{ctx - 1, ctx > 0 ? 1 : 0, s};
+    } else {
+        return Lens{a.prefix_lens[s], max(a.new_lens[s], 0), a.cu_new[s]};
+    }
+}
+// of column tiles 0 .. k - 1 of a session (all full), without the factor nh
+__device__ __forceinline__ uint64_t cost_below(const Lens& x, int m, uint64_t k) { return k * (uint64_t)x.prefix + (uint64_t)m * (k * (k + 1) / 2); }
+template <bool kDecode>
+__device__ __forceinline__ typename Counting<kDecode>::Cost session_cost(const Lens& x, const Cut& cut)
+{
+    if (x.n <= 0) return 0;
+    if constexpr (kDecode) return (uint32_t)cut.nh * (uint32_t)((x.prefix + kTokens) / kTokens);
+    const uint64_t k = (x.n - 1) / cut.m;                              // tiles before the last
+    return (uint64_t)cut.nh * (cost_below(x, cut.m, k) + x.prefix + x.n);
+}
+
+template <typename T>
+__device__ __forceinline__ T scan64(T v)                               // inclusive, over the wave
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const T up = __shfl_up(v, d);
+        v += lane >= d ? up : 0;
+    }
+    return v;
+}
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+__device__ __forceinline__ uint64_t from_lane(uint64_t v, int l) { return from_lane((uint32_t)v, l) | (uint64_t)from_lane((uint32_t)(v >> 32), l) << 32; }
+
+// A unit: column tile k of session s, part hh of its heads.
+struct Unit { int s, k, hh; Lens x; };
+
+// Share w of `shares`: [begin, begin + len) of the batch's work, and the unit that begin lies in, `off` into it.  len 0: nothing.
+template <bool kDecode>
+struct Share {
+    typedef typename Counting<kDecode>::Cost Cost;
+    Cost begin, len, off, per, total;
+    Unit u;
+    __device__ __forceinline__ Share(const AttnArgs& a, const Cut& cut, int w, int shares, int least)
+    {
+        const int lane = threadIdx.x & 63;
+        Cost incl = 0;
+        total = 0;
+        for (int base = 0; base < a.batch; base += 64) {
+            incl = scan64(base + lane < a.batch ? session_cost<kDecode>(lens_of<kDecode>(a, base + lane), cut) : (Cost)0);
+            total += from_lane(incl, 63);
+        }
+        constexpr Cost kT = Counting<kDecode>::kTile;
+        per = (total + shares - 1) / shares;
+        per = per < (Cost)least * kT ? (Cost)least * kT : (per + kT - 1) / kT * kT;
+        begin = (Cost)w * per;
+        len = begin < total ? (total - begin < per ? total - begin : per) : 0;
+        off = 0;
+        u = Unit{0, 0, 0, Lens{0, 0, 0}};
+        if (len == 0) return;
+        Cost run = 0;
+        for (int base = 0;; base += 64) {                              // ends: begin < total
+            if (a.batch > 64) incl = scan64(base + lane < a.batch ? session_cost<kDecode>(lens_of<kDecode>(a, base + lane), cut) : (Cost)0);
+            const uint64_t past = __builtin_amdgcn_ballot_w64(run + incl > begin);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                u.s = base + l;
+                run += l ? from_lane(incl, l - 1) : 0;
+                break;
+            }
+            run += from_lane(incl, 63);
+        }
+        u.x = lens_of<kDecode>(a, u.s);
+        Cost y = begin - run;
+        if constexpr (!kDecode) {
+            int lo = 0, hi = (u.x.n - 1) / cut.m;                      // the last tile that starts at or before y
+            while (lo < hi) {
+                const int mid = lo + (hi - lo + 1) / 2;
+                if ((uint64_t)cut.nh * cost_below(u.x, cut.m, mid) <= y) lo = mid;
+                else hi = mid - 1;
+            }
+            u.k = lo;
+            y -= (uint64_t)cut.nh * cost_below(u.x, cut.m, lo);
+        }
+        const Cost c = cost(cut);
+        u.hh = (int)(y / c);
+        off = y - (Cost)u.hh * c;
+    }
+    __device__ __forceinline__ int last_pos(const Cut& cut) const { return u.x.prefix + min((u.k + 1) * cut.m, u.x.n) - 1; }      // that the unit's last row sees
+    __device__ __forceinline__ int tiles(const Cut& cut) const { return last_pos(cut) / kTokens + 1; }
+    __device__ __forceinline__ Cost cost(const Cut& cut) const { return kDecode ? (Cost)tiles(cut) : (Cost)last_pos(cut) + 1; }
+    // the unit after u, from its start
+    __device__ __forceinline__ bool next(const AttnArgs& a, const Cut& cut)
+    {
+        off = 0;
+        if (++u.hh < cut.nh) return true;
+        u.hh = 0;
+        if (++u.k * cut.m < u.x.n) return true;
+        u.k = 0;
+        do {
+            if (++u.s >= a.batch) return false;
+            u.x = lens_of<kDecode>(a, u.s);
+        } while (u.x.n <= 0);
+        return true;
+    }
+};
+
+// ---- the workspace ----
+// Records of the cuts: for share w's start, if it is the first that cuts its unit, the unit's first output row, its columns, and how many pieces it is in
+// (otherwise 0).  Pieces: two places a share, 2 w for a unit that began in an earlier one, 2 w + 1 for the one that it leaves unfinished.
+struct Record { int64_t row; int32_t cols, pieces; };
+__host__ __device__ inline size_t ml_offset() { return kMostShares * sizeof(Record); }
+__host__ __device__ inline size_t o_offset(int places, int cols) { return ml_offset() + (size_t)places * cols * 8; }
+// O of a place: [32 columns][channel / 32][channel / 8 % 4][channel / 4 % 2][column][channel % 4]: a store writes 1 KiB in a run
+__host__ __device__ inline size_t place_floats(int cols, int lat) { return (size_t)cols * lat; }
+
+// ---- the kernel ----
+
+template <int L, int R> struct Row {
+    static constexpr int kRow = row_of(L, R), kBytes = kRow * 2, kBlocks = kRow / 64, kSteps = (L + R) / 16, kTile = kTokens * kBytes;
+};
+// Where a tile's 16-byte pieces stand in LDS: [token / 8][channel / 64][token % 8][8 pieces], piece c of token n at place c ^ turn(n): the tokens of a score operand
+// and the four rows of a transposing read then lie in different banks.
+__device__ __forceinline__ int turn_of(int n) { return (((n & 3) ^ ((n >> 3) & 1)) << 1) | ((n >> 2) & 1); }
+
+__device__ __forceinline__ bf16x4 read_across(unsigned lds_addr)
+{
+    typedef __attribute__((address_space(3))) bf16x4* ptr;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ptr)(uintptr_t)lds_addr);
+}
+__device__ __forceinline__ bf16x8 read_along(unsigned lds_addr)
+{
+    typedef const __attribute__((address_space(3))) bf16x8* ptr;
+    return *(ptr)(uintptr_t)lds_addr;
+}
+__device__ __forceinline__ void barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+constexpr int kAhead = 3;               // operand reads run this many products ahead of their use
+
+// The score products are written in assembly because their accumulators have to be vector registers: the compiler gives all matrix instructions of a
+// kernel accumulation registers, which O^T fills.  What the compiler keeps for its own matrix instructions is kept here by hand: two states between a vector
+// instruction that may have moved an operand and the product; none between products into one accumulator; and nothing of the result is read before
+// score_products_end(), 20 states after the last product (18 are asked for behind the longest there is).  Operands come by the compiler's loads, whose arrival it waits for.
+__device__ __forceinline__ void score_product_first(f32x16& s, const bf16x8& a, const bf16x8& b)
+{
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void score_product(f32x16& s, const bf16x8& a, const bf16x8& b)
+{
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void score_products_end(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
+
+// S^T of a tile: tokens x columns.  k0: the lane's place in the tile.
+template <int L, int R>
+__device__ __forceinline__ f32x16 scores(unsigned k0, const bf16x8 (&qf)[Row<L, R>::kSteps])
+{
+    constexpr int kN = Row<L, R>::kSteps;
+    bf16x8 opnd[kAhead + 1];
+    f32x16 s;
+    const unsigned kb[4] = {k0, k0 ^ 32, k0 ^ 64, k0 ^ 96};
+    auto operand = [&](int i) { return read_along(kb[i & 3] + (i >> 2) * 1024); };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) opnd[i] = operand(i);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        if (i + kAhead < kN) opnd[(i + kAhead) % (kAhead + 1)] = operand(i + kAhead);
+        if (i == 0) score_product_first(s, opnd[0], qf[0]);
+        else score_product(s, opnd[i % (kAhead + 1)], qf[i]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    score_products_end(s);
+    return s;
+}
+
+struct Weights { bf16x8 k[2]; };        // of a tile, as the B operands of the two k-steps of the value product
+
+__device__ __forceinline__ float add_pair(bf16x2 p, float sum)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(p, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, sum, false);
+}
+
+// Weights of a tile under m, and their sum as rounded.
+__device__ __forceinline__ float weigh(const f32x16& s, float sl2, float m, Weights& p)
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bf16x2 w = {(__bf16)__builtin_amdgcn_exp2f(fmaf(s[2 * i], sl2, -m)), (__bf16)__builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], sl2, -m))};
+        p.k[i >> 2][(2 * i) & 7] = w[0];
+        p.k[i >> 2][(2 * i + 1) & 7] = w[1];
+        sum = add_pair(w, sum);
+    }
+    return sum;
+}
+
+// The value product's operand i: k-step i / kCb, channel block i % kCb.  vb: the lane's places for slots 0..7 / 8..15 of a k-step (turn_of() differs by 2) and
+// even / odd blocks (four pieces on).
+template <int L, int R, int kCb>
+__device__ __forceinline__ bf16x8 value_operand(const unsigned (&vb)[2][2], int i)
+{
+    const int kk = i / kCb, cb = i % kCb;
+    const bf16x4 lo = read_across(vb[0][cb & 1] + (2 * kk) * (8 * Row<L, R>::kBytes) + (cb >> 1) * 1024);
+    const bf16x4 hi = read_across(vb[1][cb & 1] + (2 * kk + 1) * (8 * Row<L, R>::kBytes) + (cb >> 1) * 1024);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// A block of O is in accumulation registers here: the compiler would otherwise take all of it into vector registers at once, where it does not fit.
+__device__ __forceinline__ void stays_put(f32x16& o) { asm volatile("" : "+a"(o)); }
+
+// One iteration's vector work and value product: the weights of tile t from its scores (if do_sm) beside O += rows(t-1)^T . P(t-1) (if do_pv).
+// m is a reference, not the running maximum: the common case takes the weights under it and looks afterwards whether they came out large (a lane's 16 sum to
+// 2^14 at most; inf and NaN fail too); only then, and on a unit's first tile, the maximum is found and m moved.
+template <int L, int R, int kCb>
+__device__ __forceinline__ void softmax_and_values(bool do_sm, bool do_pv, unsigned v0, const f32x16& s, float sl2, float& m, float& lsum,
+                                                   const Weights& p_prev, Weights& p_cur, f32x16 (&o)[kCb])
+{
+    constexpr int kN = 2 * kCb;
+    bool redo = false;
+    if (do_pv) {
+        constexpr int kEvery = kN > 8 ? kN / 8 : 1, kPairs = 8 * kEvery / kN, kLinks = kN / kEvery;      // pairs of scores a step, every kEvery products
+        static_assert(kPairs * kLinks == 8, "every pair has its step");
+        const unsigned vb[2][2] = {{v0, v0 ^ 64}, {v0 ^ 32, v0 ^ 96}};
+        bf16x8 opnd[kAhead + 1];
+#pragma unroll
+        for (int i = 0; i < kAhead && i < kN; ++i) opnd[i] = value_operand<L, R, kCb>(vb, i);
+        float sum = 0.f, x0[kPairs], x1[kPairs], q0[kPairs], q1[kPairs];
+        bf16x2 w[kPairs];
+        // a chain (scale, exp, round, sum) is spread over four steps
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+            x0[k] = fmaf(s[2 * k], sl2, -m);
+            x1[k] = fmaf(s[2 * k + 1], sl2, -m);
+            q0[k] = q1[k] = 0.f;
+            w[k] = bf16x2{(__bf16)0.f, (__bf16)0.f};
+        }
+#pragma unroll
+        for (int step = 0; step < kN + 2 * kEvery; ++step) {
+            if (step < kN) {
+                if (step + kAhead < kN) opnd[(step + kAhead) % (kAhead + 1)] = value_operand<L, R, kCb>(vb, step + kAhead);
+                o[step % kCb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opnd[step % (kAhead + 1)], p_prev.k[step / kCb], o[step % kCb], 0, 0, 0);
+            }
+            const int i = step / kEvery;
+#pragma unroll
+            for (int k = 0; k < (step % kEvery == 0 ? kPairs : 0); ++k) {
+                if (i >= 2) sum = add_pair(w[k], sum);
+                if (i >= 1 && i <= kLinks) {
+                    w[k] = bf16x2{(__bf16)q0[k], (__bf16)q1[k]};
+                    const int pair = (i - 1) * kPairs + k;
+                    p_cur.k[pair >> 2][(2 * pair) & 7] = w[k][0];
+                    p_cur.k[pair >> 2][(2 * pair + 1) & 7] = w[k][1];
+                }
+                if (i < kLinks) {
+                    q0[k] = __builtin_amdgcn_exp2f(x0[k]);
+                    q1[k] = __builtin_amdgcn_exp2f(x1[k]);
+                }
+                if (i + 1 < kLinks) {
+                    const int pair = (i + 1) * kPairs + k;
+                    x0[k] = fmaf(s[2 * pair], sl2, -m);
+                    x1[k] = fmaf(s[2 * pair + 1], sl2, -m);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (do_sm) {
+            redo = __builtin_amdgcn_ballot_w64(!(sum <= kWeightSumLimit)) != 0;      // uniform over the wave
+            if (!redo) lsum += sum;
+        }
+    }
+    if (do_sm && (!do_pv || redo)) {
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        mx *= sl2;                                   // scale > 0: maximum and scaling commute
+        if (__builtin_amdgcn_ballot_w64(mx > m + kRescaleSlack) != 0) {
+            mx = fmaxf(mx, __shfl_xor(mx, 32));      // m is shared by the two lanes of a column
+            const float m_new = fmaxf(m, mx);
+            // (a column that has seen no key has m = m_new = -inf: nothing to rescale)
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+            lsum *= alpha;
+#pragma unroll
+            for (int cb = 0; cb < kCb; ++cb) {
+                stays_put(o[cb]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[cb][i] *= alpha;
+                stays_put(o[cb]);
+            }
+            m = m_new;
+        }
+        lsum += weigh(s, sl2, m == -INFINITY ? 0.f : m, p_cur);       // (no key seen yet: weights of zero, not NaN)
+    }
+}
+
+template <int L, int R, int kSplit, bool kDecode>
+__global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
+{
+    typedef Row<L, R> Rw;
+    constexpr int kCols = 128 / kSplit, kCb = L / 32 / kSplit, kRB = Rw::kBytes;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    int* const s_bad = reinterpret_cast<int*>(lds + kStages * Rw::kTile);
+    const unsigned lds0 = lds_address(lds);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ct = wave / kSplit, part = wave % kSplit, n = lane & 31, hi = lane >> 5;
+    const Cut cut(kCols, a.heads);
+    const int shares = gridDim.x;
+    // shares that follow each other on one XCD: they read the same rows
+    const int w = shares % 8 == 0 ? (blockIdx.x % 8) * (shares / 8) + blockIdx.x / 8 : blockIdx.x;
+    Share<kDecode> sh(a, cut, w, shares, least);
+    typedef typename Share<kDecode>::Cost Cost;
+    constexpr Cost kT = Counting<kDecode>::kTile;
+
+    if (tid == 0) {
+        Record rec = {0, 0, 0};
+        if (sh.len && sh.off / kT > 0) {
+            const Cost u0 = sh.begin - sh.off, first = (u0 + kT + sh.per - 1) / sh.per;       // the first share whose start cuts the unit
+            if (first == (Cost)w) {
+                rec.row = ((int64_t)sh.u.x.row0 + (int64_t)sh.u.k * cut.m) * a.heads + (int64_t)sh.u.hh * kCols;
+                rec.cols = a.heads <= kCols ? min(cut.m, sh.u.x.n - sh.u.k * cut.m) * a.heads : min(kCols, a.heads - sh.u.hh * kCols);
+                rec.pieces = (int)((u0 + sh.cost(cut) - 1) / sh.per) - w + 2;
+            }
+        }
+        reinterpret_cast<Record*>(a.ws)[w] = rec;
+        *s_bad = 0;
+    }
+
+    // ---- the lane's places ----
+    // loads: token lane / 8 of the wave's eight, piece lane % 8 of its place
+    const uint32_t piece = (uint32_t)((lane & 7) ^ turn_of(wave * 8 + (lane >> 3))) * 16;
+    const uint32_t load_off = (uint32_t)(lane >> 3) * kRB + piece;
+    // scores: token n of the tile, piece hi of a run of eight; piece 2 j + hi is 32 j further, by exclusive or (runs are 128 bytes, aligned)
+    const unsigned k_lane = lds0 + (n >> 3) * (8 * kRB) + (n & 7) * 128 + (hi ^ turn_of(n)) * 16;
+    // values: sixteen lanes read four tokens (row i / 4, four channels i % 4); tokens 16 kk + 4 hi + row, channels of the part's first block
+    unsigned v_lane;
+    {
+        const int i = lane & 15, row = 4 * hi + (i >> 2), chunk = part * kCb * 4 + ((lane >> 4) & 1) * 2 + ((i >> 1) & 1);
+        v_lane = lds0 + row * 128 + (chunk >> 3) * 1024 + ((chunk & 7) ^ turn_of(row)) * 16 + (i & 1) * 8;
+    }
+
+    const float sl2 = a.scale * kLog2e;
+    const int ps = a.c.ps, shift = a.c.ps_shift;
+    Cost left = sh.len;
+    while (left) {
+        const int tiles = sh.tiles(cut);
+        const Cost rest = sh.cost(cut) - sh.off;
+        const int begin = (int)(sh.off / kT), end = left >= rest ? tiles : (int)((sh.off + left) / kT);
+        if (begin < end) {
+            // ---- the unit's columns ----
+            const Unit& u = sh.u;
+            const int first_row = u.k * cut.m, last = sh.last_pos(cut), qmin = u.x.prefix + first_row;
+            const int cols = a.heads <= kCols ? min(cut.m, u.x.n - first_row) * a.heads : min(kCols, a.heads - u.hh * kCols);
+            const int64_t base_row = ((int64_t)u.x.row0 + first_row) * a.heads + (int64_t)u.hh * kCols;
+            const int col = min(ct * 32 + n, cols - 1);                   // columns beyond the tile repeat the last one
+            const int qpos = a.heads <= kCols ? qmin + col / a.heads : qmin;
+
+            // ---- pages: the ids of 64 at a time, a lane each ----
+            const int32_t* const bt = a.bt + (int64_t)u.s * a.max_pages;
+            int window = -1, ids = 0;
+            auto page_of = [&](int pos) {
+                const int p = pos >> shift;
+                if (p >> 6 != window) {
+                    window = p >> 6;
+                    ids = bt[min(window * 64 + lane, last >> shift)];
+                    AG_WAIT_VMCNT(0);            // here and not at the use, which would wait for the tiles on their way every time
+                }
+                return __builtin_amdgcn_readlane(ids, p & 63);
+            };
+            // tile t into its stage; positions past the last one repeat that
+            auto request = [&](int t) {
+                const int r0 = t * kTokens + wave * 8, room = last - r0, at = min(r0, last);
+                const int page = page_of(at);
+                const unsigned char* src = (const unsigned char*)a.c.pool + ((int64_t)page * ps + (at & (ps - 1))) * kRB;
+                const uint32_t off = room >= 7 ? load_off : (uint32_t)min(lane >> 3, max(room, 0)) * kRB + piece;
+                const unsigned dst = lds0 + (t % kStages) * Rw::kTile + wave * (8 * kRB);
+#pragma unroll
+                for (int b = 0; b < Rw::kBlocks; ++b) load_to_lds_from(src + b * 128, off, dst + b * 1024);
+            };
+            barrier();                           // the unit before has read its last tiles
+            request(begin);
+            if (begin + 1 < end) request(begin + 1);
+
+            bf16x8 qf[Rw::kSteps];
+            {
+                const __bf16* qp = (const __bf16*)a.q + (base_row + col) * (L + R) + hi * 8;
+#pragma unroll
+                for (int i = 0; i < Rw::kSteps; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(qp + i * 16);
+            }
+            float m = -INFINITY, lsum = 0.f;
+            f32x16 o[kCb];
+#pragma unroll
+            for (int cb = 0; cb < kCb; ++cb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[cb][i] = 0.f;
+            AG_WAIT_VMCNT(0);
+
+            Weights pa, pb;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pa.k[0][i] = pa.k[1][i] = pb.k[0][i] = pb.k[1][i] = (__bf16)0.f;
+            auto iter = [&](int t, const Weights& p_prev, Weights& p_cur) {
+                const bool do_sm = t < end, do_pv = t > begin;
+                if (do_sm) {
+                    if (t + 1 < end) AG_WAIT_VMCNT(Rw::kBlocks);
+                    else AG_WAIT_VMCNT(0);
+                }
+                barrier();                       // tile t is there, and every wave has taken the values of tile t - 2
+                if (t + 2 < end) request(t + 2);
+                f32x16 s;
+                if (do_sm) {
+                    s = scores<L, R>(k_lane + (t % kStages) * Rw::kTile, qf);
+                    if (t * kTokens + kTokens - 1 > qmin) {
+                        const int key = t * kTokens + hi * 4;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = key + (i >> 2) * 8 + (i & 3) <= qpos ? s[i] : -INFINITY;
+                    }
+                }
+                // A weight of zero does not hide a NaN.  Rows that only some of the columns see are looked through, once their scores are taken: what is not
+                // finite in them becomes zero for the value product, and goes to the columns that see it afterwards.
+                const int tv = t - 1, seen = qmin + 1 - tv * kTokens;        // tokens below `seen` are seen by all columns
+                bool bad = false;
+                if (!kDecode && cut.m > 1 && do_pv && seen < kTokens) {
+                    const int from = max(seen, 0);
+                    unsigned char* const tile = lds + (tv % kStages) * Rw::kTile;
+                    bool mine = false;
+                    for (int i = tid; i < (kTokens - from) * (L / 8); i += 256) {
+                        const int tok = from + i / (L / 8), c = i % (L / 8);
+                        u32x4* const x = reinterpret_cast<u32x4*>(tile + (tok >> 3) * (8 * kRB) + (c >> 3) * 1024 + (tok & 7) * 128 + ((c & 7) ^ turn_of(tok)) * 16);
+                        u32x4 v = *x;
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t high = ((v[j] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;       // the halves whose exponent is all ones
+                            any |= high;
+                            v[j] &= ~((high << 1) - (high >> 15));
+                        }
+                        if (any) {
+                            *x = v;
+                            mine = true;
+                        }
+                    }
+                    if (mine) *s_bad = 1;
+                    __syncthreads();
+                    bad = *reinterpret_cast<volatile int*>(s_bad) != 0;
+                }
+                softmax_and_values<L, R, kCb>(do_sm, do_pv, v_lane + ((t + kStages - 1) % kStages) * Rw::kTile, s, sl2, m, lsum, p_prev, p_cur, o);
+                if (bad) {
+#pragma unroll 1
+                    for (int at = max(tv * kTokens, qmin + 1); at <= min(tv * kTokens + kTokens - 1, last); ++at) {
+                        const int page = bt[at >> shift];
+                        const uint16_t* const row = (const uint16_t*)a.c.pool + ((int64_t)page * ps + (at & (ps - 1))) * Rw::kRow + part * (kCb * 32) + hi * 4;
+#pragma unroll
+                        for (int cb = 0; cb < kCb; ++cb) {
+                            stays_put(o[cb]);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const bool odd = (row[cb * 32 + (i >> 2) * 8 + (i & 3)] & 0x7F80) == 0x7F80;
+                                o[cb][i] = odd && at <= qpos ? __builtin_nanf("") : o[cb][i];
+                            }
+                            stays_put(o[cb]);
+                        }
+                    }
+                    __syncthreads();
+                    if (tid == 0) *s_bad = 0;
+                    __syncthreads();
+                }
+            };
+#pragma unroll 1
+            for (int t = begin; t <= end; t += 2) {
+                iter(t, pb, pa);
+                if (t + 1 <= end) iter(t + 1, pa, pb);
+            }
+
+            lsum += __shfl_xor(lsum, 32);
+            if (begin == 0 && end == tiles) {
+                if (ct * 32 + n < cols) {
+                    const float inv = 1.0f / lsum;
+                    __bf16* const op = (__bf16*)a.out + (base_row + col) * L + part * (kCb * 32) + hi * 4;
+#pragma unroll
+                    for (int cb = 0; cb < kCb; ++cb) {
+                        stays_put(o[cb]);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            bf16x4 v;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[cb][q * 4 + i] * inv);
+                            *reinterpret_cast<bf16x4*>(op + cb * 32 + q * 8) = v;
+                        }
+                    }
+                }
+            } else {
+                const int place = 2 * w + (begin == 0);
+                unsigned char* const ws = (unsigned char*)a.ws;
+                if (part == 0 && hi == 0)
+                    reinterpret_cast<float2*>(ws + ml_offset())[(int64_t)place * kCols + ct * 32 + n] = make_float2(m, lsum);
+                f32x4* const op = reinterpret_cast<f32x4*>(ws + o_offset(2 * shares, kCols)) + ((int64_t)place * kCols * L + ct * (32 * L)) / 4 + (part * kCb) * 256 + lane;
+#pragma unroll
+                for (int cb = 0; cb < kCb; ++cb) {
+                    stays_put(o[cb]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        f32x4 v;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = o[cb][q * 4 + i];
+                        op[(cb * 4 + q) * 64] = v;
+                    }
+                }
+            }
+        }
+        if (left <= rest) break;
+        left -= rest;
+        if (!sh.next(a, cut)) break;
+    }
+    if constexpr (kDecode) {
+        // sessions without a token: rows of zeros
+        for (int s = blockIdx.x; s < a.batch; s += gridDim.x) {
+            if (a.ctx_lens[s] > 0) continue;
+            u32x4* const op = reinterpret_cast<u32x4*>((__bf16*)a.out + (int64_t)s * a.heads * L);
+            for (int64_t i = tid; i < (int64_t)a.heads * (L / 8); i += 256) op[i] = u32x4{0, 0, 0, 0};
+        }
+    }
+}
+
+// Pieces of the units that shares cut, in order.  blockIdx.x + 1 is the share whose start cuts; a thread takes four channels of a column.
+constexpr int kMergeSlices = 8;
+__global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* ws, __bf16* out, int shares, int cols, int lat)
+{
+    const int w = blockIdx.x + 1;
+    const Record rec = reinterpret_cast<const Record*>(ws)[w];
+    if (rec.pieces == 0) return;
+    const float2* const ml = reinterpret_cast<const float2*>(ws + ml_offset());
+    const f32x4* const o = reinterpret_cast<const f32x4*>(ws + o_offset(2 * shares, cols));
+    const int quads = lat / 4;
+    auto place = [&](int i) { return i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1); };
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < (rec.cols + 7) / 8 * 8 * quads; i += kMergeSlices * 256) {
+        // eight columns side by side, eight quads of each: runs of 128 bytes in, of 64 out
+        const int tile = i / (8 * quads), in = i - tile * 8 * quads, col = tile * 8 + ((in >> 3) & 7), quad = (in >> 6) * 8 + (in & 7);
+        if (col >= rec.cols) continue;
+        float top = -INFINITY;
+        for (int p = 0; p < rec.pieces; ++p) top = fmaxf(top, ml[(int64_t)place(p) * cols + col].x);
+        float l = 0.f;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < rec.pieces; ++p) {
+            const float2 x = ml[(int64_t)place(p) * cols + col];
+            const f32x4 v = o[(int64_t)place(p) * (cols * lat / 4) + (col >> 5) * (8 * lat) + quad * 32 + (col & 31)];
+            const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - top);
+            l += x.y * f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += v[e] * f;
+        }
+        const float inv = 1.0f / l;
+        bf16x4 r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (__bf16)(sum[e] * inv);
+        *reinterpret_cast<bf16x4*>(out + (rec.row + col) * lat + quad * 4) = r;
+    }
+}
+
+// ---- the host's side ----
+
+constexpr int kLeastTiles = 4;          // of a share
+
+int columns(int64_t most) { return most <= 32 ? 32 : most <= 64 ? 64 : 128; }
+
+// Shares of a launch whose units are at most `units` of `tiles` tiles: no more than have kLeastTiles each.
+int shares_of(int64_t units, int64_t tiles, int cus)
+{
+    const int64_t n = (units * tiles + kLeastTiles - 1) / kLeastTiles;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(n, std::min(cus, kMostShares)));
+}
+int64_t units_of(bool decode, int batch, int total, const Cut& cut)
+{
+    return (decode ? (int64_t)batch : (int64_t)total / cut.m + batch) * cut.nh;
+}
+size_t bytes_of(int shares, int cols, int lat) { return o_offset(2 * shares, cols) + (size_t)2 * shares * place_floats(cols, lat) * 4; }
+
+template <int L, int R, int kSplit, bool kDecode>
+ag_status run(const AttnArgs& a, int shares, hipStream_t st)
+{
+    static std::atomic<uint64_t> told{0};
+    constexpr int kLds = kStages * Row<L, R>::kTile + 16;
+    ag_status e = allow_dynamic_lds((const void*)latent_kernel<L, R, kSplit, kDecode>, kLds, told);
+    if (e) return e;
+    prof_before(st);
+    hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, kLeastTiles);
+    if (shares > 1)
+        hipLaunchKernelGGL(latent_merge_kernel, dim3(shares - 1, kMergeSlices), dim3(256), 0, st, (const unsigned char*)a.ws, (__bf16*)a.out, shares, 128 / kSplit, L);
+    prof_after(st);
+    return hip_check(hipGetLastError(), "latent attention launch");
+}
+template <int L, int R>
+ag_status run_columns(const AttnArgs& a, int cols, int shares, hipStream_t st)
+{
+    if (a.ctx_lens) {
+        if (cols == 32) return run<L, R, 4, true>(a, shares, st);
+        return cols == 64 ? run<L, R, 2, true>(a, shares, st) : run<L, R, 1, true>(a, shares, st);
+    }
+    if (cols == 32) return run<L, R, 4, false>(a, shares, st);
+    return cols == 64 ? run<L, R, 2, false>(a, shares, st) : run<L, R, 1, false>(a, shares, st);
+}
+
+}  // namespace
+
+size_t attn_workspace(bool decode, int batch, int total, int heads, int lat, int max_ctx)
+{
+    const int64_t tiles = ((int64_t)max_ctx + kTokens - 1) / kTokens;
+    size_t most = 0;
+    for (int cols : {32, 64, 128}) {
+        if (cols > columns((int64_t)total * heads)) break;             // (no session has more columns than all rows)
+        const Cut cut(cols, heads);
+        const int64_t units = units_of(decode, batch, total, cut);
+        // sums of costs: 32 bits of tiles for decode, 64 of keys otherwise
+        if ((double)units * (double)std::max<int64_t>(tiles, 1) >= (decode ? 2147483648.0 : 1.0e16)) return 0;
+        most = std::max(most, bytes_of(shares_of(units, tiles, kMostShares), cols, lat));
+    }
+    return most;
+}
+
+ag_status launch_attn(const AttnArgs& a, hipStream_t st)
+{
+    const bool decode = a.ctx_lens != nullptr;
+    const int cols = columns(decode ? a.heads : (int64_t)a.max_new * a.heads);
+    const Cut cut(cols, a.heads);
+    const int shares = shares_of(units_of(decode, a.batch, a.total, cut), ((int64_t)a.max_ctx + kTokens - 1) / kTokens, stream_cus(st));
+    if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, shares, st) : run_columns<512, 32>(a, cols, shares, st);
+    if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, shares, st) : run_columns<256, 32>(a, cols, shares, st);
+    return a.c.rd == 64 ? run_columns<128, 64>(a, cols, shares, st) : run_columns<128, 32>(a, cols, shares, st);
+}
+
+}  // namespace latent
+}  // namespace ag

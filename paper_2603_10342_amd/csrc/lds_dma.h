@@ -28,6 +28,11 @@ __device__ __forceinline__ void load_dword_to_lds(const void* src, unsigned lds_
 {
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(lds_addr) : "m0");
 }
+// The 16-byte form from a uniform base and an offset of the lane's own.
+__device__ __forceinline__ void load_to_lds_from(const void* base, uint32_t offset, unsigned lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds_addr) : "m0");
+}
 #pragma clang diagnostic pop
 __device__ __forceinline__ unsigned lds_address(const void* p)
 {

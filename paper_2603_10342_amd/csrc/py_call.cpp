@@ -12,7 +12,9 @@
 #include <type_traits>
 
 #include "ag.h"
+#include "ag_latent.h"
 #include "ag_q8.h"
+#include "ag_rope.h"
 
 namespace {
 
@@ -29,13 +31,21 @@ struct Entries {
     decltype(&ag_attn_prefill_q8) attn_prefill_q8;
     decltype(&ag_attn_resume_q8) attn_resume_q8;
     decltype(&ag_attn_decode_q8) attn_decode_q8;
+    decltype(&ag_rope_rows) rope_rows;
+    decltype(&ag_kv_append_rope) kv_append_rope;
+    decltype(&ag_kv_append_latent) kv_append_latent;
+    decltype(&ag_attn_decode_latent) attn_decode_latent;
+    decltype(&ag_attn_resume_latent) attn_resume_latent;
 };
 Entries entries;
 PyObject* cache_type;           // binding.KVCache
 PyObject* cache_q8_type;        // binding.KVCacheQ8
+PyObject* rope_type;            // binding.Rope
+PyObject* latent_type;          // binding.LatentCache
 PyObject* get_device;           // torch._C._cuda_getDevice
 PyObject* get_raw_stream;       // torch._C._cuda_getCurrentRawStream
-PyObject *n_k_pool, *n_v_pool, *n_exps, *n_num_pages, *n_page_size, *n_num_kv_heads, *n_head_dim, *n_dtype, *n_cuda_stream;
+PyObject *n_k_pool, *n_v_pool, *n_exps, *n_num_pages, *n_page_size, *n_num_kv_heads, *n_head_dim, *n_dtype, *n_cuda_stream, *n_turns, *n_rot_dim, *n_layout,
+    *n_magnitude, *n_pool, *n_latent_dim, *n_rope_dim;
 
 // Reads arguments; `plain` becomes false at the first that is not for this path, and the rest is not looked at.
 struct Reader {
@@ -93,16 +103,53 @@ struct Reader {
         if (const at::Tensor* t = tensor(v)) c.exps = t->data_ptr();
         Py_DECREF(v);
     }
+    // an attribute of o
+    template <class Use>
+    void get_from(PyObject* o, PyObject* name, Use use)
+    {
+        PyObject* v = plain ? PyObject_GetAttr(o, name) : nullptr;
+        if (!v) { PyErr_Clear(); plain = false; return; }
+        use(v);
+        Py_DECREF(v);
+    }
+    bool of_type(PyObject* o, PyObject* type)
+    {
+        if (plain && (PyObject*)Py_TYPE(o) == type) return true;
+        plain = false;
+        return false;
+    }
+    void cache(PyObject* o, ag_latent_cache& c)
+    {
+        if (!of_type(o, latent_type)) return;
+        get_from(o, n_pool, [&](PyObject* v) { if (const at::Tensor* t = tensor(v)) c.pool = t->data_ptr(); });
+        get_from(o, n_num_pages, [&](PyObject* v) { c.num_pages = number(v); });
+        get_from(o, n_page_size, [&](PyObject* v) { c.page_size = number(v); });
+        get_from(o, n_latent_dim, [&](PyObject* v) { c.latent_dim = number(v); });
+        get_from(o, n_rope_dim, [&](PyObject* v) { c.rope_dim = number(v); });
+    }
+    void rope(PyObject* o, ag_rope& r)
+    {
+        if (!of_type(o, rope_type)) return;
+        get_from(o, n_turns, [&](PyObject* v) { r.turns = (const double*)device(v); });
+        get_from(o, n_rot_dim, [&](PyObject* v) { r.rot_dim = number(v); });
+        get_from(o, n_layout, [&](PyObject* v) { r.layout = number(v); });
+        get_from(o, n_magnitude, [&](PyObject* v) { r.magnitude = real(v); });
+    }
+    // rows of `dims` dimensions whose channels are contiguous, bf16 (or fp32)
+    void* rows(PyObject* o, int dims, const at::Tensor** out)
+    {
+        const at::Tensor* t = tensor(o);
+        if (!t) return nullptr;
+        const bool bf16 = t->scalar_type() == at::kBFloat16;
+        if (!t->is_cuda() || t->dim() != dims || t->stride(dims - 1) != 1 || !(bf16 || (dims == 3 && t->scalar_type() == at::kFloat))) { plain = false; return nullptr; }
+        *out = t;
+        return t->data_ptr();
+    }
     template <class Cache>
     void pools(PyObject* o, PyObject* type, Cache& c)
     {
-        if (!plain || (PyObject*)Py_TYPE(o) != type) { plain = false; return; }
-        auto get = [&](PyObject* name, auto use) {
-            PyObject* v = plain ? PyObject_GetAttr(o, name) : nullptr;
-            if (!v) { PyErr_Clear(); plain = false; return; }
-            use(v);
-            Py_DECREF(v);
-        };
+        if (!of_type(o, type)) return;
+        auto get = [&](PyObject* name, auto use) { get_from(o, name, use); };
         get(n_k_pool, [&](PyObject* v) { if (const at::Tensor* t = tensor(v)) c.k_pool = t->data_ptr(); });
         get(n_v_pool, [&](PyObject* v) { if (const at::Tensor* t = tensor(v)) c.v_pool = t->data_ptr(); });
         get(n_num_pages, [&](PyObject* v) { c.num_pages = number(v); });
@@ -191,11 +238,11 @@ PyObject* attn_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
-// resume prefill, and the merged batch, which takes a workspace as well
+// resume prefill; the merged batch and the latent cache's take a workspace as well
 template <class Cache, auto kEntry>
 PyObject* attn_resume(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    constexpr bool kMerged = std::is_same_v<decltype(kEntry), decltype(&Entries::attn_merged)>;
+    constexpr bool kMerged = std::is_same_v<decltype(kEntry), decltype(&Entries::attn_merged)> || std::is_same_v<Cache, ag_latent_cache>;       // (with a workspace)
     return guarded(n, kMerged ? 14 : 13, [&] {
         Reader r;
         Cache c;
@@ -258,24 +305,84 @@ PyObject* decode_step(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
-// setup(KVCache, KVCacheQ8, _cuda_getDevice, _cuda_getCurrentRawStream, addresses of the entry points in the order of Entries)
+PyObject* rope_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 9, [&] {
+        Reader r;
+        ag_rope rope;
+        const at::Tensor *x, *y, *lens;
+        r.rope(a[0], rope);
+        void *xp = r.rows(a[1], 3, &x), *yp = r.rows(a[2], 3, &y);
+        const int32_t *prefix = r.ints(a[3]), *len = r.ints(a[4], &lens), *cu = r.ints(a[5]);
+        const int32_t total = r.number(a[6]), batch = r.plain ? r.size(lens, 0) : 0;
+        if (!PyBool_Check(a[7])) r.plain = false;
+        void* s = r.stream(a[8]);
+        if (r.plain && (x->sizes() != y->sizes() || x->scalar_type() != y->scalar_type() || total > x->size(0))) r.plain = false;
+        const int32_t heads = r.plain ? r.size(x, 1) : 0, d = r.plain ? r.size(x, 2) : 0;
+        return finish(r, [&] {
+            return entries.rope_rows(&rope, x->scalar_type() == at::kFloat ? AG_F32 : AG_BF16, xp, x->stride(0), x->stride(1), yp, y->stride(0), y->stride(1),
+                                     heads, d, prefix, len, cu, batch, total, a[7] == Py_True, s);
+        });
+    });
+}
+
+PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 12, [&] {
+        Reader r;
+        ag_kv_cache c;
+        ag_rope rope;
+        const at::Tensor *q = nullptr, *bt, *lens;
+        r.cache(a[0], c);
+        r.rope(a[1], rope);
+        const bool queries = a[2] != Py_None || a[3] != Py_None;
+        void *qp = queries ? r.device(a[2], &q) : nullptr, *qo = queries ? r.device(a[3]) : nullptr, *k = r.device(a[4]), *v = r.device(a[5]);
+        const int32_t *b = r.ints(a[6], &bt), *prefix = r.ints(a[7]), *len = r.ints(a[8], &lens), *cu = r.ints(a[9]);
+        const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), total = r.number(a[10]), hq = queries ? r.size(q, 1) : 0;
+        void* s = r.stream(a[11]);
+        return finish(r, [&] { return entries.kv_append_rope(&c, &rope, qp, qo, hq, k, v, b, pages, prefix, len, cu, batch, total, s); });
+    });
+}
+
+PyObject* kv_append_latent(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&] {
+        Reader r;
+        ag_latent_cache c;
+        ag_rope rope;
+        const at::Tensor *lat, *rot, *bt, *lens;
+        r.cache(a[0], c);
+        const bool turned = a[1] == Py_None;
+        if (!turned) r.rope(a[1], rope);
+        void *lp = r.rows(a[2], 2, &lat), *rp = r.rows(a[3], 2, &rot);
+        const int32_t *b = r.ints(a[4], &bt), *prefix = r.ints(a[5]), *len = r.ints(a[6], &lens), *cu = r.ints(a[7]);
+        const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), total = r.number(a[8]);
+        void* s = r.stream(a[9]);
+        if (r.plain && (lat->size(1) != c.latent_dim || rot->size(1) != c.rope_dim)) r.plain = false;
+        return finish(r, [&] {
+            return entries.kv_append_latent(&c, turned ? nullptr : &rope, lp, lat->stride(0), rp, rot->stride(0), b, pages, prefix, len, cu, batch, total, s);
+        });
+    });
+}
+
+// setup(KVCache, KVCacheQ8, Rope, LatentCache, _cuda_getDevice, _cuda_getCurrentRawStream, addresses of the entry points in the order of Entries)
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     void** at = reinterpret_cast<void**>(&entries);
     constexpr Py_ssize_t kEntries = sizeof(Entries) / sizeof(void*);
-    if (n != 4 + kEntries) { PyErr_SetString(PyExc_TypeError, "setup: wrong number of arguments"); return nullptr; }
+    constexpr Py_ssize_t kObjects = 6;
+    if (n != kObjects + kEntries) { PyErr_SetString(PyExc_TypeError, "setup: wrong number of arguments"); return nullptr; }
     for (Py_ssize_t i = 0; i < kEntries; ++i) {
-        at[i] = PyLong_AsVoidPtr(a[4 + i]);
+        at[i] = PyLong_AsVoidPtr(a[kObjects + i]);
         if (PyErr_Occurred()) return nullptr;
     }
-    Py_INCREF(a[0]);
-    Py_INCREF(a[1]);
-    Py_INCREF(a[2]);
-    Py_INCREF(a[3]);
+    for (Py_ssize_t i = 0; i < kObjects; ++i) Py_INCREF(a[i]);
     cache_type = a[0];
     cache_q8_type = a[1];
-    get_device = a[2];
-    get_raw_stream = a[3];
+    rope_type = a[2];
+    latent_type = a[3];
+    get_device = a[4];
+    get_raw_stream = a[5];
     Py_RETURN_NONE;
 }
 
@@ -290,7 +397,10 @@ PyMethodDef methods[] = {
     AG_METHOD("kv_append_q8", (kv_rows<ag_kv_cache_q8, &Entries::kv_append_q8>)), AG_METHOD("kv_read_q8", (kv_rows<ag_kv_cache_q8, &Entries::kv_read_q8>)),
     AG_METHOD("attn_prefill_q8", (attn_prefill<ag_kv_cache_q8, &Entries::attn_prefill_q8>)),
     AG_METHOD("attn_resume_q8", (attn_resume<ag_kv_cache_q8, &Entries::attn_resume_q8>)),
-    AG_METHOD("attn_decode_q8", (attn_decode<ag_kv_cache_q8, &Entries::attn_decode_q8>)), {nullptr, nullptr, 0, nullptr}};
+    AG_METHOD("attn_decode_q8", (attn_decode<ag_kv_cache_q8, &Entries::attn_decode_q8>)),
+    AG_METHOD("rope_rows", rope_rows), AG_METHOD("kv_append_rope", kv_append_rope), AG_METHOD("kv_append_latent", kv_append_latent),
+    AG_METHOD("attn_decode_latent", (attn_decode<ag_latent_cache, &Entries::attn_decode_latent>)),
+    AG_METHOD("attn_resume_latent", (attn_resume<ag_latent_cache, &Entries::attn_resume_latent>)), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "agcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -299,7 +409,9 @@ PyMODINIT_FUNC PyInit_agcall()
 {
     struct { PyObject** at; const char* name; } names[] = {
         {&n_k_pool, "k_pool"}, {&n_v_pool, "v_pool"}, {&n_exps, "exps"}, {&n_num_pages, "num_pages"}, {&n_page_size, "page_size"},
-        {&n_num_kv_heads, "num_kv_heads"}, {&n_head_dim, "head_dim"}, {&n_dtype, "dtype"}, {&n_cuda_stream, "cuda_stream"}};
+        {&n_num_kv_heads, "num_kv_heads"}, {&n_head_dim, "head_dim"}, {&n_dtype, "dtype"}, {&n_cuda_stream, "cuda_stream"},
+        {&n_turns, "turns"}, {&n_rot_dim, "rot_dim"}, {&n_layout, "layout"}, {&n_magnitude, "magnitude"}, {&n_pool, "pool"}, {&n_latent_dim, "latent_dim"},
+        {&n_rope_dim, "rope_dim"}};
     for (auto& x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.name))) return nullptr;
     PyObject* m = PyModule_Create(&module);
