@@ -47,9 +47,10 @@ struct Cut {
 };
 
 // Work is counted in tiles of 32 keys for decode.  A chunk's column tile k counts the keys that its last row sees, P + min((k + 1) m, N), so that the
-// sum over the tiles of a session has a closed form; shares are multiples of 32 of that.
-template <bool kDecode> struct Counting { typedef uint32_t Cost; static constexpr int kTile = 1; };
-template <> struct Counting<false> { typedef uint64_t Cost; static constexpr int kTile = kTokens; };
+// sum over the tiles of a session has a closed form; shares are multiples of 32 of that.  A unit costs kLead on top, for its queries, first tile and output.
+constexpr int kLeadTiles = 4;
+template <bool kDecode> struct Counting { typedef uint32_t Cost; static constexpr int kTile = 1, kLead = kLeadTiles; };
+template <> struct Counting<false> { typedef uint64_t Cost; static constexpr int kTile = kTokens, kLead = kLeadTiles * kTokens; };
 
 struct Lens { int prefix, n, row0; };   // of a session
 template <bool kDecode>
@@ -63,14 +64,14 @@ __device__ __forceinline__ Lens lens_of(const AttnArgs& a, int s)
     }
 }
 // of column tiles 0 .. k - 1 of a session (all full), without the factor nh
-__device__ __forceinline__ uint64_t cost_below(const Lens& x, int m, uint64_t k) { return k * (uint64_t)x.prefix + (uint64_t)m * (k * (k + 1) / 2); }
+__device__ __forceinline__ uint64_t cost_below(const Lens& x, int m, uint64_t k) { return k * ((uint64_t)x.prefix + Counting<false>::kLead) + (uint64_t)m * (k * (k + 1) / 2); }
 template <bool kDecode>
 __device__ __forceinline__ typename Counting<kDecode>::Cost session_cost(const Lens& x, const Cut& cut)
 {
     if (x.n <= 0) return 0;
-    if constexpr (kDecode) return (uint32_t)cut.nh * (uint32_t)((x.prefix + kTokens) / kTokens);
+    if constexpr (kDecode) return (uint32_t)cut.nh * (uint32_t)((x.prefix + kTokens) / kTokens + kLeadTiles);
     const uint64_t k = (x.n - 1) / cut.m;                              // tiles before the last
-    return (uint64_t)cut.nh * (cost_below(x, cut.m, k) + x.prefix + x.n);
+    return (uint64_t)cut.nh * (cost_below(x, cut.m, k) + x.prefix + x.n + Counting<false>::kLead);
 }
 
 template <typename T>
@@ -143,7 +144,9 @@ struct Share {
     }
     __device__ __forceinline__ int last_pos(const Cut& cut) const { return u.x.prefix + min((u.k + 1) * cut.m, u.x.n) - 1; }      // that the unit's last row sees
     __device__ __forceinline__ int tiles(const Cut& cut) const { return last_pos(cut) / kTokens + 1; }
-    __device__ __forceinline__ Cost cost(const Cut& cut) const { return kDecode ? (Cost)tiles(cut) : (Cost)last_pos(cut) + 1; }
+    __device__ __forceinline__ Cost cost(const Cut& cut) const { return (kDecode ? (Cost)tiles(cut) : (Cost)last_pos(cut) + 1) + Counting<kDecode>::kLead; }
+    // tiles of the unit that lie before a cut at `y`
+    static __device__ __forceinline__ int tiles_before(Cost y) { return y < Counting<kDecode>::kLead ? 0 : (int)((y - Counting<kDecode>::kLead) / Counting<kDecode>::kTile); }
     // the unit after u, from its start
     __device__ __forceinline__ bool next(const AttnArgs& a, const Cut& cut)
     {
@@ -334,16 +337,17 @@ __device__ __forceinline__ void softmax_and_values(bool do_sm, bool do_pv, unsig
         mx *= sl2;                                   // scale > 0: maximum and scaling commute
         if (__builtin_amdgcn_ballot_w64(mx > m + kRescaleSlack) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 32));      // m is shared by the two lanes of a column
-            const float m_new = fmaxf(m, mx);
-            // (a column that has seen no key has m = m_new = -inf: nothing to rescale)
-            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+            const float m_new = mx > m + kRescaleSlack ? mx : m;         // (a column keeps its own: what others see does not show in its bits)
+            const float alpha = m_new == m ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
             lsum *= alpha;
+            if (do_pv) {
 #pragma unroll
-            for (int cb = 0; cb < kCb; ++cb) {
-                stays_put(o[cb]);
+                for (int cb = 0; cb < kCb; ++cb) {
+                    stays_put(o[cb]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[cb][i] *= alpha;
-                stays_put(o[cb]);
+                    for (int i = 0; i < 16; ++i) o[cb][i] *= alpha;
+                    stays_put(o[cb]);
+                }
             }
             m = m_new;
         }
@@ -367,12 +371,12 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
     const int w = shares % 8 == 0 ? (blockIdx.x % 8) * (shares / 8) + blockIdx.x / 8 : blockIdx.x;
     Share<kDecode> sh(a, cut, w, shares, least);
     typedef typename Share<kDecode>::Cost Cost;
-    constexpr Cost kT = Counting<kDecode>::kTile;
+    constexpr Cost kT = Counting<kDecode>::kTile, kLead = Counting<kDecode>::kLead;
 
     if (tid == 0) {
         Record rec = {0, 0, 0};
-        if (sh.len && sh.off / kT > 0) {
-            const Cost u0 = sh.begin - sh.off, first = (u0 + kT + sh.per - 1) / sh.per;       // the first share whose start cuts the unit
+        if (sh.len && sh.tiles_before(sh.off) > 0) {
+            const Cost u0 = sh.begin - sh.off, first = (u0 + kLead + kT + sh.per - 1) / sh.per;       // the first share whose start cuts the unit
             if (first == (Cost)w) {
                 rec.row = ((int64_t)sh.u.x.row0 + (int64_t)sh.u.k * cut.m) * a.heads + (int64_t)sh.u.hh * kCols;
                 rec.cols = a.heads <= kCols ? min(cut.m, sh.u.x.n - sh.u.k * cut.m) * a.heads : min(kCols, a.heads - sh.u.hh * kCols);
@@ -386,7 +390,6 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
     // ---- the lane's places ----
     // loads: token lane / 8 of the wave's eight, piece lane % 8 of its place
     const uint32_t piece = (uint32_t)((lane & 7) ^ turn_of(wave * 8 + (lane >> 3))) * 16;
-    const uint32_t load_off = (uint32_t)(lane >> 3) * kRB + piece;
     // scores: token n of the tile, piece hi of a run of eight; piece 2 j + hi is 32 j further, by exclusive or (runs are 128 bytes, aligned)
     const unsigned k_lane = lds0 + (n >> 3) * (8 * kRB) + (n & 7) * 128 + (hi ^ turn_of(n)) * 16;
     // values: sixteen lanes read four tokens (row i / 4, four channels i % 4); tokens 16 kk + 4 hi + row, channels of the part's first block
@@ -399,10 +402,12 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
     const float sl2 = a.scale * kLog2e;
     const int ps = a.c.ps, shift = a.c.ps_shift;
     Cost left = sh.len;
+    int done = 0;                        // tiles of this share so far
     while (left) {
         const int tiles = sh.tiles(cut);
         const Cost rest = sh.cost(cut) - sh.off;
-        const int begin = (int)(sh.off / kT), end = left >= rest ? tiles : (int)((sh.off + left) / kT);
+        // the piece of the unit, counted from its far end: a share starts with the first keys of a unit, like the whole units that others take at that time
+        const int from = sh.tiles_before(sh.off), to = left >= rest ? tiles : sh.tiles_before(sh.off + left), begin = tiles - to, end = tiles - from;
         if (begin < end) {
             // ---- the unit's columns ----
             const Unit& u = sh.u;
@@ -424,19 +429,23 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                 }
                 return __builtin_amdgcn_readlane(ids, p & 63);
             };
-            // tile t into its stage; positions past the last one repeat that
-            auto request = [&](int t) {
-                const int r0 = t * kTokens + wave * 8, room = last - r0, at = min(r0, last);
+            // The order of the tiles: a whole unit starts where `done` says and wraps round, so that workgroups that have done as much read the same keys at
+            // the same time, and find them in their XCD's cache (chunks; a decode's keys have one reader)
+            const int count = end - begin, turn = kDecode || from != 0 || to != tiles ? 0 : done % count;
+            auto tile_at = [&](int i) { return begin + (i + turn < count ? i + turn : i + turn - count); };
+            // tile i of the order into its stage; positions past the last one repeat that
+            auto request = [&](int i) {
+                const int r0 = tile_at(i) * kTokens + wave * 8, room = last - r0, at = min(r0, last);
                 const int page = page_of(at);
                 const unsigned char* src = (const unsigned char*)a.c.pool + ((int64_t)page * ps + (at & (ps - 1))) * kRB;
-                const uint32_t off = room >= 7 ? load_off : (uint32_t)min(lane >> 3, max(room, 0)) * kRB + piece;
-                const unsigned dst = lds0 + (t % kStages) * Rw::kTile + wave * (8 * kRB);
+                const uint32_t off = (uint32_t)min(lane >> 3, max(room, 0)) * kRB + piece;
+                const unsigned dst = lds0 + (i % kStages) * Rw::kTile + wave * (8 * kRB);
 #pragma unroll
                 for (int b = 0; b < Rw::kBlocks; ++b) load_to_lds_from(src + b * 128, off, dst + b * 1024);
             };
             barrier();                           // the unit before has read its last tiles
-            request(begin);
-            if (begin + 1 < end) request(begin + 1);
+            request(0);
+            if (1 < count) request(1);
 
             bf16x8 qf[Rw::kSteps];
             {
@@ -455,35 +464,27 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
             Weights pa, pb;
 #pragma unroll
             for (int i = 0; i < 8; ++i) pa.k[0][i] = pa.k[1][i] = pb.k[0][i] = pb.k[1][i] = (__bf16)0.f;
-            auto iter = [&](int t, const Weights& p_prev, Weights& p_cur) {
-                const bool do_sm = t < end, do_pv = t > begin;
+            auto iter = [&](int i, const Weights& p_prev, Weights& p_cur) {
+                const bool do_sm = i < count, do_pv = i > 0;
+                const int t = tile_at(i);
                 if (do_sm) {
-                    if (t + 1 < end) AG_WAIT_VMCNT(Rw::kBlocks);
+                    if (i + 1 < count) AG_WAIT_VMCNT(Rw::kBlocks);
                     else AG_WAIT_VMCNT(0);
                 }
-                barrier();                       // tile t is there, and every wave has taken the values of tile t - 2
-                if (t + 2 < end) request(t + 2);
-                f32x16 s;
-                if (do_sm) {
-                    s = scores<L, R>(k_lane + (t % kStages) * Rw::kTile, qf);
-                    if (t * kTokens + kTokens - 1 > qmin) {
-                        const int key = t * kTokens + hi * 4;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = key + (i >> 2) * 8 + (i & 3) <= qpos ? s[i] : -INFINITY;
-                    }
-                }
-                // A weight of zero does not hide a NaN.  Rows that only some of the columns see are looked through, once their scores are taken: what is not
+                barrier();                       // tile i is there, and every wave has taken the values of tile i - 2
+                if (i + 2 < count) request(i + 2);
+                // A weight of zero does not hide a NaN.  Rows that only some of the columns see are looked through, their scores being taken: what is not
                 // finite in them becomes zero for the value product, and goes to the columns that see it afterwards.
-                const int tv = t - 1, seen = qmin + 1 - tv * kTokens;        // tokens below `seen` are seen by all columns
+                const int tv = do_pv ? tile_at(i - 1) : 0, seen = qmin + 1 - tv * kTokens;        // tokens below `seen` are seen by all columns
                 bool bad = false;
                 if (!kDecode && cut.m > 1 && do_pv && seen < kTokens) {
-                    const int from = max(seen, 0);
-                    unsigned char* const tile = lds + (tv % kStages) * Rw::kTile;
+                    const int unseen = max(seen, 0);
+                    unsigned char* const tile = lds + ((i - 1) % kStages) * Rw::kTile;
                     bool mine = false;
-                    for (int i = tid; i < (kTokens - from) * (L / 8); i += 256) {
-                        const int tok = from + i / (L / 8), c = i % (L / 8);
-                        u32x4* const x = reinterpret_cast<u32x4*>(tile + (tok >> 3) * (8 * kRB) + (c >> 3) * 1024 + (tok & 7) * 128 + ((c & 7) ^ turn_of(tok)) * 16);
-                        u32x4 v = *x;
+                    for (int x = tid; x < (kTokens - unseen) * (L / 8); x += 256) {
+                        const int tok = unseen + x / (L / 8), c = x % (L / 8);
+                        u32x4* const at = reinterpret_cast<u32x4*>(tile + (tok >> 3) * (8 * kRB) + (c >> 3) * 1024 + (tok & 7) * 128 + ((c & 7) ^ turn_of(tok)) * 16);
+                        u32x4 v = *at;
                         uint32_t any = 0;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -492,7 +493,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                             v[j] &= ~((high << 1) - (high >> 15));
                         }
                         if (any) {
-                            *x = v;
+                            *at = v;
                             mine = true;
                         }
                     }
@@ -500,7 +501,16 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                     __syncthreads();
                     bad = *reinterpret_cast<volatile int*>(s_bad) != 0;
                 }
-                softmax_and_values<L, R, kCb>(do_sm, do_pv, v_lane + ((t + kStages - 1) % kStages) * Rw::kTile, s, sl2, m, lsum, p_prev, p_cur, o);
+                f32x16 s;
+                if (do_sm) {
+                    s = scores<L, R>(k_lane + (i % kStages) * Rw::kTile, qf);
+                    if (t * kTokens + kTokens - 1 > qmin) {
+                        const int key = t * kTokens + hi * 4;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[e] = key + (e >> 2) * 8 + (e & 3) <= qpos ? s[e] : -INFINITY;
+                    }
+                }
+                softmax_and_values<L, R, kCb>(do_sm, do_pv, v_lane + ((i + kStages - 1) % kStages) * Rw::kTile, s, sl2, m, lsum, p_prev, p_cur, o);
                 if (bad) {
 #pragma unroll 1
                     for (int at = max(tv * kTokens, qmin + 1); at <= min(tv * kTokens + kTokens - 1, last); ++at) {
@@ -510,9 +520,9 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                         for (int cb = 0; cb < kCb; ++cb) {
                             stays_put(o[cb]);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const bool odd = (row[cb * 32 + (i >> 2) * 8 + (i & 3)] & 0x7F80) == 0x7F80;
-                                o[cb][i] = odd && at <= qpos ? __builtin_nanf("") : o[cb][i];
+                            for (int e = 0; e < 16; ++e) {
+                                const bool odd = (row[cb * 32 + (e >> 2) * 8 + (e & 3)] & 0x7F80) == 0x7F80;
+                                o[cb][e] = odd && at <= qpos ? __builtin_nanf("") : o[cb][e];
                             }
                             stays_put(o[cb]);
                         }
@@ -523,30 +533,40 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                 }
             };
 #pragma unroll 1
-            for (int t = begin; t <= end; t += 2) {
-                iter(t, pb, pa);
-                if (t + 1 <= end) iter(t + 1, pa, pb);
+            for (int i = 0; i <= count; i += 2) {
+                iter(i, pb, pa);
+                if (i + 1 <= count) iter(i + 1, pa, pb);
             }
+            done += count;
 
             lsum += __shfl_xor(lsum, 32);
-            if (begin == 0 && end == tiles) {
-                if (ct * 32 + n < cols) {
-                    const float inv = 1.0f / lsum;
-                    __bf16* const op = (__bf16*)a.out + (base_row + col) * L + part * (kCb * 32) + hi * 4;
+            if (from == 0 && to == tiles) {
+                // rows that are whole in LDS, 16-byte pieces in a place that depends on the row (8-byte stores of the accumulators themselves, 32 rows an
+                // instruction, took 100 us for every unit of the 256 CUs)
+                constexpr int kPieces = kCb * 4, kMask = kPieces < 8 ? kPieces - 1 : 7;      // of a row
+                barrier();                       // the last tiles' values have been taken
+                const float inv = 1.0f / lsum;
+                unsigned char* const mine = lds + wave * (32 * kPieces * 16);
 #pragma unroll
-                    for (int cb = 0; cb < kCb; ++cb) {
-                        stays_put(o[cb]);
+                for (int cb = 0; cb < kCb; ++cb) {
+                    stays_put(o[cb]);
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            bf16x4 v;
+                    for (int q = 0; q < 4; ++q) {
+                        bf16x4 v;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[cb][q * 4 + i] * inv);
-                            *reinterpret_cast<bf16x4*>(op + cb * 32 + q * 8) = v;
-                        }
+                        for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[cb][q * 4 + i] * inv);
+                        *reinterpret_cast<bf16x4*>(mine + (n * kPieces + ((cb * 4 + q) ^ (n & kMask))) * 16 + hi * 8) = v;
                     }
                 }
+                u32x4* const op = reinterpret_cast<u32x4*>((__bf16*)a.out + (base_row + ct * 32) * L + part * (kCb * 32));
+#pragma unroll
+                for (int i = 0; i < kPieces / 2; ++i) {
+                    const int at = i * 64 + lane, row = at / kPieces, c = at % kPieces;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(mine + (row * kPieces + (c ^ (row & kMask))) * 16);
+                    if (ct * 32 + row < cols) __builtin_nontemporal_store(v, op + (int64_t)row * (L / 8) + c);
+                }
             } else {
-                const int place = 2 * w + (begin == 0);
+                const int place = 2 * w + (from == 0);
                 unsigned char* const ws = (unsigned char*)a.ws;
                 if (part == 0 && hi == 0)
                     reinterpret_cast<float2*>(ws + ml_offset())[(int64_t)place * kCols + ct * 32 + n] = make_float2(m, lsum);
@@ -559,7 +579,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                         f32x4 v;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) v[i] = o[cb][q * 4 + i];
-                        op[(cb * 4 + q) * 64] = v;
+                        __builtin_nontemporal_store(v, op + (cb * 4 + q) * 64);
                     }
                 }
             }
@@ -578,44 +598,104 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
     }
 }
 
-// Pieces of the units that shares cut, in order.  blockIdx.x + 1 is the share whose start cuts; a thread takes four channels of a column.
-constexpr int kMergeSlices = 8;
+// Pieces of the units that shares cut, in order.  A workgroup finds those units among the records and takes slices of them, eight columns by 32 kQ channels: a lane has
+// kQ times four channels of a column, a wave every fourth piece.
+template <int kQ>
 __global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* ws, __bf16* out, int shares, int cols, int lat)
 {
-    const int w = blockIdx.x + 1;
-    const Record rec = reinterpret_cast<const Record*>(ws)[w];
-    if (rec.pieces == 0) return;
+    __shared__ int s_cut[kMostShares];
+    __shared__ int s_count[4];
+    __shared__ float s_part[3][64][2 + 4 * kQ];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Record* const recs = reinterpret_cast<const Record*>(ws);
+    {
+        static_assert(kMostShares <= 256, "a thread a record");
+        const bool cut = tid >= 1 && tid < shares && recs[tid < shares ? tid : 0].pieces > 0;
+        const uint64_t those = __builtin_amdgcn_ballot_w64(cut);
+        if (lane == 0) s_count[wave] = __builtin_popcountll(those);
+        __syncthreads();
+        int at = __builtin_popcountll(those & ((1ull << lane) - 1));
+        for (int i = 0; i < wave; ++i) at += s_count[i];
+        if (cut) s_cut[at] = tid;
+        __syncthreads();
+    }
+    const int cuts = s_count[0] + s_count[1] + s_count[2] + s_count[3];
     const float2* const ml = reinterpret_cast<const float2*>(ws + ml_offset());
     const f32x4* const o = reinterpret_cast<const f32x4*>(ws + o_offset(2 * shares, cols));
-    const int quads = lat / 4;
-    auto place = [&](int i) { return i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1); };
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < (rec.cols + 7) / 8 * 8 * quads; i += kMergeSlices * 256) {
-        // eight columns side by side, eight quads of each: runs of 128 bytes in, of 64 out
-        const int tile = i / (8 * quads), in = i - tile * 8 * quads, col = tile * 8 + ((in >> 3) & 7), quad = (in >> 6) * 8 + (in & 7);
-        if (col >= rec.cols) continue;
-        float top = -INFINITY;
-        for (int p = 0; p < rec.pieces; ++p) top = fmaxf(top, ml[(int64_t)place(p) * cols + col].x);
-        float l = 0.f;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < rec.pieces; ++p) {
-            const float2 x = ml[(int64_t)place(p) * cols + col];
-            const f32x4 v = o[(int64_t)place(p) * (cols * lat / 4) + (col >> 5) * (8 * lat) + quad * 32 + (col & 31)];
-            const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - top);
-            l += x.y * f;
+    const int across = lat / (32 * kQ), slices = cols / 8 * across;
+    for (int item = blockIdx.x; item < cuts * slices; item += gridDim.x) {
+        const int w = s_cut[item / slices], slice = item % slices;
+        const Record rec = recs[w];
+        const int col = slice / across * 8 + (lane >> 3), quad0 = slice % across * (8 * kQ) + (lane & 7);
+        const int64_t o0 = (col >> 5) * (8 * lat) + quad0 * 32 + (col & 31);
+        float top = -INFINITY, l = 0.f;
+        f32x4 sum[kQ];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += v[e] * f;
+        for (int q = 0; q < kQ; ++q) sum[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (col < rec.cols) {
+            constexpr int kFlight = 4;           // pieces whose loads are in flight together
+            for (int p0 = wave; p0 < rec.pieces; p0 += 4 * kFlight) {
+                float2 x[kFlight];
+                f32x4 v[kFlight][kQ];
+#pragma unroll
+                for (int j = 0; j < kFlight; ++j) {
+                    const int p = min(p0 + 4 * j, rec.pieces - 1);
+                    const int64_t place = p == 0 ? 2 * (w - 1) + 1 : 2 * (w + p - 1);
+                    x[j] = ml[place * cols + col];
+#pragma unroll
+                    for (int q = 0; q < kQ; ++q) v[j][q] = o[place * (cols * lat / 4) + o0 + q * 256];
+                }
+#pragma unroll
+                for (int j = 0; j < kFlight; ++j) {
+                    if (p0 + 4 * j >= rec.pieces) break;
+                    const float t = fmaxf(top, x[j].x), f0 = top == -INFINITY ? 0.f : exp2f(top - t), f1 = x[j].x == -INFINITY ? 0.f : exp2f(x[j].x - t);
+                    top = t;
+                    l = l * f0 + x[j].y * f1;
+#pragma unroll
+                    for (int q = 0; q < kQ; ++q)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[q][e] = sum[q][e] * f0 + v[j][q][e] * f1;
+                }
+            }
+        }
+        __syncthreads();                         // the slice before has been read
+        if (wave > 0) {
+            float* const x = s_part[wave - 1][lane];
+            x[0] = top;
+            x[1] = l;
+#pragma unroll
+            for (int i = 0; i < 4 * kQ; ++i) x[2 + i] = sum[i >> 2][i & 3];
+        }
+        __syncthreads();
+        if (wave > 0 || col >= rec.cols) continue;
+        float most = top;
+        for (int i = 0; i < 3; ++i) most = fmaxf(most, s_part[i][lane][0]);
+        float f = top == -INFINITY ? 0.f : exp2f(top - most);
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < 4 * kQ; ++i) sum[i >> 2][i & 3] *= f;
+        for (int j = 0; j < 3; ++j) {
+            const float* const x = s_part[j][lane];
+            f = x[0] == -INFINITY ? 0.f : exp2f(x[0] - most);
+            l += x[1] * f;
+#pragma unroll
+            for (int i = 0; i < 4 * kQ; ++i) sum[i >> 2][i & 3] += x[2 + i] * f;
         }
         const float inv = 1.0f / l;
-        bf16x4 r;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = (__bf16)(sum[e] * inv);
-        *reinterpret_cast<bf16x4*>(out + (rec.row + col) * lat + quad * 4) = r;
+        for (int q = 0; q < kQ; ++q) {
+            bf16x4 r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = (__bf16)(sum[q][e] * inv);
+            *reinterpret_cast<bf16x4*>(out + (rec.row + col) * lat + (quad0 + q * 8) * 4) = r;
+        }
     }
 }
 
 // ---- the host's side ----
 
 constexpr int kLeastTiles = 4;          // of a share
+constexpr int kMergeMost = 1024;        // workgroups of a merge
 
 int columns(int64_t most) { return most <= 32 ? 32 : most <= 64 ? 64 : 128; }
 
@@ -632,7 +712,7 @@ int64_t units_of(bool decode, int batch, int total, const Cut& cut)
 size_t bytes_of(int shares, int cols, int lat) { return o_offset(2 * shares, cols) + (size_t)2 * shares * place_floats(cols, lat) * 4; }
 
 template <int L, int R, int kSplit, bool kDecode>
-ag_status run(const AttnArgs& a, int shares, hipStream_t st)
+ag_status run(const AttnArgs& a, int64_t units, int shares, hipStream_t st)
 {
     static std::atomic<uint64_t> told{0};
     constexpr int kLds = kStages * Row<L, R>::kTile + 16;
@@ -640,20 +720,25 @@ ag_status run(const AttnArgs& a, int shares, hipStream_t st)
     if (e) return e;
     prof_before(st);
     hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, kLeastTiles);
-    if (shares > 1)
-        hipLaunchKernelGGL(latent_merge_kernel, dim3(shares - 1, kMergeSlices), dim3(256), 0, st, (const unsigned char*)a.ws, (__bf16*)a.out, shares, 128 / kSplit, L);
+    if (shares > 1) {
+        constexpr int kCols = 128 / kSplit, kSlices = kCols / 8 * (L / 32);
+        const int64_t cuts = std::min<int64_t>(shares - 1, units);
+        // four channels a lane where the cut units have few columns between them, sixteen otherwise
+        if (cuts * kSlices <= kMergeMost) hipLaunchKernelGGL(latent_merge_kernel<1>, dim3(cuts * kSlices), dim3(256), 0, st, (const unsigned char*)a.ws, (__bf16*)a.out, shares, kCols, L);
+        else hipLaunchKernelGGL(latent_merge_kernel<4>, dim3(std::min<int64_t>(cuts * kSlices / 4, kMergeMost)), dim3(256), 0, st, (const unsigned char*)a.ws, (__bf16*)a.out, shares, kCols, L);
+    }
     prof_after(st);
     return hip_check(hipGetLastError(), "latent attention launch");
 }
 template <int L, int R>
-ag_status run_columns(const AttnArgs& a, int cols, int shares, hipStream_t st)
+ag_status run_columns(const AttnArgs& a, int cols, int64_t units, int shares, hipStream_t st)
 {
     if (a.ctx_lens) {
-        if (cols == 32) return run<L, R, 4, true>(a, shares, st);
-        return cols == 64 ? run<L, R, 2, true>(a, shares, st) : run<L, R, 1, true>(a, shares, st);
+        if (cols == 32) return run<L, R, 4, true>(a, units, shares, st);
+        return cols == 64 ? run<L, R, 2, true>(a, units, shares, st) : run<L, R, 1, true>(a, units, shares, st);
     }
-    if (cols == 32) return run<L, R, 4, false>(a, shares, st);
-    return cols == 64 ? run<L, R, 2, false>(a, shares, st) : run<L, R, 1, false>(a, shares, st);
+    if (cols == 32) return run<L, R, 4, false>(a, units, shares, st);
+    return cols == 64 ? run<L, R, 2, false>(a, units, shares, st) : run<L, R, 1, false>(a, units, shares, st);
 }
 
 }  // namespace
@@ -667,7 +752,7 @@ size_t attn_workspace(bool decode, int batch, int total, int heads, int lat, int
         const Cut cut(cols, heads);
         const int64_t units = units_of(decode, batch, total, cut);
         // sums of costs: 32 bits of tiles for decode, 64 of keys otherwise
-        if ((double)units * (double)std::max<int64_t>(tiles, 1) >= (decode ? 2147483648.0 : 1.0e16)) return 0;
+        if ((double)units * (double)(tiles + kLeadTiles) >= (decode ? 2147483648.0 : 1.0e16)) return 0;
         most = std::max(most, bytes_of(shares_of(units, tiles, kMostShares), cols, lat));
     }
     return most;
@@ -678,10 +763,11 @@ ag_status launch_attn(const AttnArgs& a, hipStream_t st)
     const bool decode = a.ctx_lens != nullptr;
     const int cols = columns(decode ? a.heads : (int64_t)a.max_new * a.heads);
     const Cut cut(cols, a.heads);
-    const int shares = shares_of(units_of(decode, a.batch, a.total, cut), ((int64_t)a.max_ctx + kTokens - 1) / kTokens, stream_cus(st));
-    if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, shares, st) : run_columns<512, 32>(a, cols, shares, st);
-    if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, shares, st) : run_columns<256, 32>(a, cols, shares, st);
-    return a.c.rd == 64 ? run_columns<128, 64>(a, cols, shares, st) : run_columns<128, 32>(a, cols, shares, st);
+    const int64_t units = units_of(decode, a.batch, a.total, cut);
+    const int shares = shares_of(units, ((int64_t)a.max_ctx + kTokens - 1) / kTokens, stream_cus(st));
+    if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, units, shares, st) : run_columns<512, 32>(a, cols, units, shares, st);
+    if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, units, shares, st) : run_columns<256, 32>(a, cols, units, shares, st);
+    return a.c.rd == 64 ? run_columns<128, 64>(a, cols, units, shares, st) : run_columns<128, 32>(a, cols, units, shares, st);
 }
 
 }  // namespace latent
