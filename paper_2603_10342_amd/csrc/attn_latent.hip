@@ -16,6 +16,8 @@
 // pieces' partial (max, sum, O) go through the workspace and are merged in order by a second launch.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
+#include <utility>
 
 #include "latent_internal.h"
 #include "lds_dma.h"
@@ -35,8 +37,9 @@ constexpr int kTokens = 32;             // of a tile
 constexpr int kStages = 4;              // tiles in LDS: the one whose values are taken, the one whose scores are, two on their way
 constexpr int kMostShares = 256;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kRescaleSlack = 8.0f;   // log2 units a column's maximum may exceed m when the ordered path leaves m alone
-constexpr float kWeightSumLimit = 16384.0f;   // a lane's 16 weights of a tile may sum to this much before m is moved
+// What a column's reference m may be exceeded by: a lane's 16 weights of a tile sum to at most this.  Weights are floating-point numbers, as exact at 2^40 as at 1.
+constexpr float kMostWeight = 1099511627776.0f;
+constexpr float kLeastSum = 1.0f / kMostWeight;
 
 // ---- how a batch is cut ----
 
@@ -200,10 +203,10 @@ __device__ __forceinline__ void barrier()
 
 constexpr int kAhead = 3;               // operand reads run this many products ahead of their use
 
-// The score products are written in assembly because their accumulators have to be vector registers: the compiler gives all matrix instructions of a
-// kernel accumulation registers, which O^T fills.  What the compiler keeps for its own matrix instructions is kept here by hand: two states between a vector
-// instruction that may have moved an operand and the product; none between products into one accumulator; and nothing of the result is read before
-// score_products_end(), 20 states after the last product (18 are asked for behind the longest there is).  Operands come by the compiler's loads, whose arrival it waits for.
+// The products are written in assembly because the scores' accumulators have to be vector registers and O's accumulation registers: the compiler gives all matrix
+// instructions of a kernel the same kind, and O^T fills that.  What the compiler keeps for its own matrix instructions is kept here by hand: two states between a vector
+// instruction that may have moved an operand and the product; none between products into one accumulator; and nothing of a result is read before
+// products_end(), 20 states after the last product (18 are asked for behind the longest there is).  Operands come by the compiler's loads, whose arrival it waits for.
 __device__ __forceinline__ void score_product_first(f32x16& s, const bf16x8& a, const bf16x8& b)
 {
     asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
@@ -212,29 +215,12 @@ __device__ __forceinline__ void score_product(f32x16& s, const bf16x8& a, const 
 {
     asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }
-__device__ __forceinline__ void score_products_end(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
-
-// S^T of a tile: tokens x columns.  k0: the lane's place in the tile.
-template <int L, int R>
-__device__ __forceinline__ f32x16 scores(unsigned k0, const bf16x8 (&qf)[Row<L, R>::kSteps])
+__device__ __forceinline__ void value_product(f32x16& o, const bf16x8& a, const bf16x8& b)
 {
-    constexpr int kN = Row<L, R>::kSteps;
-    bf16x8 opnd[kAhead + 1];
-    f32x16 s;
-    const unsigned kb[4] = {k0, k0 ^ 32, k0 ^ 64, k0 ^ 96};
-    auto operand = [&](int i) { return read_along(kb[i & 3] + (i >> 2) * 1024); };
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) opnd[i] = operand(i);
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-        if (i + kAhead < kN) opnd[(i + kAhead) % (kAhead + 1)] = operand(i + kAhead);
-        if (i == 0) score_product_first(s, opnd[0], qf[0]);
-        else score_product(s, opnd[i % (kAhead + 1)], qf[i]);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    score_products_end(s);
-    return s;
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(a), "v"(b));
 }
+__device__ __forceinline__ void products_end() { asm volatile("s_nop 15\n\ts_nop 3"); }
+__device__ __forceinline__ void products_end(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
 
 struct Weights { bf16x8 k[2]; };        // of a tile, as the B operands of the two k-steps of the value product
 
@@ -271,87 +257,79 @@ __device__ __forceinline__ bf16x8 value_operand(const unsigned (&vb)[2][2], int 
 // A block of O is in accumulation registers here: the compiler would otherwise take all of it into vector registers at once, where it does not fit.
 __device__ __forceinline__ void stays_put(f32x16& o) { asm volatile("" : "+a"(o)); }
 
-// One iteration's vector work and value product: the weights of tile t from its scores (if do_sm) beside O += rows(t-1)^T . P(t-1) (if do_pv).
-// m is a reference, not the running maximum: the common case takes the weights under it and looks afterwards whether they came out large (a lane's 16 sum to
-// 2^14 at most; inf and NaN fail too); only then, and on a unit's first tile, the maximum is found and m moved.
-template <int L, int R, int kCb>
-__device__ __forceinline__ void softmax_and_values(bool do_sm, bool do_pv, unsigned v0, const f32x16& s, float sl2, float& m, float& lsum,
-                                                   const Weights& p_prev, Weights& p_cur, f32x16 (&o)[kCb])
+// One iteration: the scores of tile t (kScores), then O += rows(t-1)^T . P(t-1) (kValues) beside the weights of tile t under m, which go to p_cur, and their sum to `sum`.
+// The operands of both products are one stream, read kAhead products ahead.  between(j) runs behind score product j, mask(s) once the scores are there; without values
+// the scores are all that comes of it.
+template <int L, int R, int kCb, bool kScores, bool kValues, class Between, class Mask>
+__device__ __forceinline__ void step(unsigned k0, unsigned v0, const bf16x8 (&qf)[Row<L, R>::kSteps], float sl2, float m, float& sum, f32x16& s, const Weights& p_prev,
+                                     Weights& p_cur, f32x16 (&o)[kCb], Between between, Mask mask)
 {
-    constexpr int kN = 2 * kCb;
-    bool redo = false;
-    if (do_pv) {
-        constexpr int kEvery = kN > 8 ? kN / 8 : 1, kPairs = 8 * kEvery / kN, kLinks = kN / kEvery;      // pairs of scores a step, every kEvery products
-        static_assert(kPairs * kLinks == 8, "every pair has its step");
-        const unsigned vb[2][2] = {{v0, v0 ^ 64}, {v0 ^ 32, v0 ^ 96}};
-        bf16x8 opnd[kAhead + 1];
+    constexpr int kNs = kScores ? Row<L, R>::kSteps : 0, kNv = kValues ? 2 * kCb : 0, kN = kNs + kNv;
+    const unsigned kb[4] = {k0, k0 ^ 32, k0 ^ 64, k0 ^ 96}, vb[2][2] = {{v0, v0 ^ 64}, {v0 ^ 32, v0 ^ 96}};
+    bf16x8 opnd[kAhead + 1];
+    auto operand = [&](int j) { return j < kNs ? read_along(kb[j & 3] + (j >> 2) * 1024) : value_operand<L, R, kCb>(vb, j - kNs); };
 #pragma unroll
-        for (int i = 0; i < kAhead && i < kN; ++i) opnd[i] = value_operand<L, R, kCb>(vb, i);
-        float sum = 0.f, x0[kPairs], x1[kPairs], q0[kPairs], q1[kPairs];
-        bf16x2 w[kPairs];
-        // a chain (scale, exp, round, sum) is spread over four steps
+    for (int j = 0; j < kAhead && j < kN; ++j) {
+        opnd[j] = operand(j);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) {
-            x0[k] = fmaf(s[2 * k], sl2, -m);
-            x1[k] = fmaf(s[2 * k + 1], sl2, -m);
-            q0[k] = q1[k] = 0.f;
-            w[k] = bf16x2{(__bf16)0.f, (__bf16)0.f};
-        }
-#pragma unroll
-        for (int step = 0; step < kN + 2 * kEvery; ++step) {
-            if (step < kN) {
-                if (step + kAhead < kN) opnd[(step + kAhead) % (kAhead + 1)] = value_operand<L, R, kCb>(vb, step + kAhead);
-                o[step % kCb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opnd[step % (kAhead + 1)], p_prev.k[step / kCb], o[step % kCb], 0, 0, 0);
+    for (int j = 0; j < kNs; ++j) {
+        if (j + kAhead < kN) opnd[(j + kAhead) % (kAhead + 1)] = operand(j + kAhead);
+        if (j == 0) score_product_first(s, opnd[0], qf[0]);
+        else score_product(s, opnd[j % (kAhead + 1)], qf[j]);
+        between(j);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // The scores' wait: behind the first three value products where there are enough of them, seven states each
+    constexpr int kWait = kScores && kNv >= 16 ? 3 : 0;
+    if constexpr (kScores && kWait == 0) {
+        products_end(s);
+        mask(s);
+    }
+    if constexpr (kValues) {
+        // a pair of scores goes through four links (scale, exp, round, sum), one a step, so that nothing in a step waits for anything else in it
+        constexpr int kLinks = 8 + 2;
+        float x0 = 0.f, x1 = 0.f, q0 = 0.f, q1 = 0.f;
+        bf16x2 w = {(__bf16)0.f, (__bf16)0.f};
+        sum = 0.f;
+        auto scale = [&](int pair) {
+            x0 = fmaf(s[2 * pair], sl2, -m);
+            x1 = fmaf(s[2 * pair + 1], sl2, -m);
+        };
+        auto link = [&](int i) {
+            if (i >= 2) sum = add_pair(w, sum);
+            if (i >= 1 && i <= 8) {
+                w = bf16x2{(__bf16)q0, (__bf16)q1};
+                p_cur.k[(i - 1) >> 2][(2 * (i - 1)) & 7] = w[0];
+                p_cur.k[(i - 1) >> 2][(2 * (i - 1) + 1) & 7] = w[1];
             }
-            const int i = step / kEvery;
+            if (i < 8) {
+                q0 = __builtin_amdgcn_exp2f(x0);
+                q1 = __builtin_amdgcn_exp2f(x1);
+            }
+            if (i + 1 < 8) scale(i + 1);
+        };
+        if constexpr (kScores && kWait == 0) scale(0);
 #pragma unroll
-            for (int k = 0; k < (step % kEvery == 0 ? kPairs : 0); ++k) {
-                if (i >= 2) sum = add_pair(w[k], sum);
-                if (i >= 1 && i <= kLinks) {
-                    w[k] = bf16x2{(__bf16)q0[k], (__bf16)q1[k]};
-                    const int pair = (i - 1) * kPairs + k;
-                    p_cur.k[pair >> 2][(2 * pair) & 7] = w[k][0];
-                    p_cur.k[pair >> 2][(2 * pair + 1) & 7] = w[k][1];
+        for (int j = 0; j < kNv; ++j) {
+            if (kNs + j + kAhead < kN) opnd[(kNs + j + kAhead) % (kAhead + 1)] = operand(kNs + j + kAhead);
+            value_product(o[j % kCb], opnd[(kNs + j) % (kAhead + 1)], p_prev.k[j / kCb]);
+            if constexpr (kScores) {
+                if (j < kWait) asm volatile("s_nop 6");
+                if (j + 1 == kWait) {
+                    asm volatile("" : "+v"(s));      // 21 states and two products after the last score product: the scores are there
+                    mask(s);
+                    scale(0);
                 }
-                if (i < kLinks) {
-                    q0[k] = __builtin_amdgcn_exp2f(x0[k]);
-                    q1[k] = __builtin_amdgcn_exp2f(x1[k]);
-                }
-                if (i + 1 < kLinks) {
-                    const int pair = (i + 1) * kPairs + k;
-                    x0[k] = fmaf(s[2 * pair], sl2, -m);
-                    x1[k] = fmaf(s[2 * pair + 1], sl2, -m);
+                if (j >= kWait) {
+#pragma unroll
+                    for (int i = 0; i < kLinks; ++i)
+                        if (kWait + i * (kNv - kWait) / kLinks == j) link(i);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (do_sm) {
-            redo = __builtin_amdgcn_ballot_w64(!(sum <= kWeightSumLimit)) != 0;      // uniform over the wave
-            if (!redo) lsum += sum;
-        }
-    }
-    if (do_sm && (!do_pv || redo)) {
-        float mx = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-        mx *= sl2;                                   // scale > 0: maximum and scaling commute
-        if (__builtin_amdgcn_ballot_w64(mx > m + kRescaleSlack) != 0) {
-            mx = fmaxf(mx, __shfl_xor(mx, 32));      // m is shared by the two lanes of a column
-            const float m_new = mx > m + kRescaleSlack ? mx : m;         // (a column keeps its own: what others see does not show in its bits)
-            const float alpha = m_new == m ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-            lsum *= alpha;
-            if (do_pv) {
-#pragma unroll
-                for (int cb = 0; cb < kCb; ++cb) {
-                    stays_put(o[cb]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[cb][i] *= alpha;
-                    stays_put(o[cb]);
-                }
-            }
-            m = m_new;
-        }
-        lsum += weigh(s, sl2, m == -INFINITY ? 0.f : m, p_cur);       // (no key seen yet: weights of zero, not NaN)
     }
 }
 
@@ -361,7 +339,8 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
     typedef Row<L, R> Rw;
     constexpr int kCols = 128 / kSplit, kCb = L / 32 / kSplit, kRB = Rw::kBytes;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    int* const s_bad = reinterpret_cast<int*>(lds + kStages * Rw::kTile);
+    int* const s_bad = reinterpret_cast<int*>(lds + kStages * Rw::kTile);         // rows that are not finite; a piece to be done again
+    int* const s_again = s_bad + 1;
     const unsigned lds0 = lds_address(lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ct = wave / kSplit, part = wave % kSplit, n = lane & 31, hi = lane >> 5;
@@ -384,7 +363,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
             }
         }
         reinterpret_cast<Record*>(a.ws)[w] = rec;
-        *s_bad = 0;
+        *s_bad = *s_again = 0;
     }
 
     // ---- the lane's places ----
@@ -431,89 +410,132 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
             };
             // The order of the tiles: a whole unit starts where `done` says and wraps round, so that workgroups that have done as much read the same keys at
             // the same time, and find them in their XCD's cache (chunks; a decode's keys have one reader)
-            const int count = end - begin, turn = kDecode || from != 0 || to != tiles ? 0 : done % count;
-            auto tile_at = [&](int i) { return begin + (i + turn < count ? i + turn : i + turn - count); };
-            // tile i of the order into its stage; positions past the last one repeat that
-            auto request = [&](int i) {
-                const int r0 = tile_at(i) * kTokens + wave * 8, room = last - r0, at = min(r0, last);
-                const int page = page_of(at);
-                const unsigned char* src = (const unsigned char*)a.c.pool + ((int64_t)page * ps + (at & (ps - 1))) * kRB;
-                const uint32_t off = (uint32_t)min(lane >> 3, max(room, 0)) * kRB + piece;
-                const unsigned dst = lds0 + (i % kStages) * Rw::kTile + wave * (8 * kRB);
-#pragma unroll
-                for (int b = 0; b < Rw::kBlocks; ++b) load_to_lds_from(src + b * 128, off, dst + b * 1024);
-            };
-            barrier();                           // the unit before has read its last tiles
-            request(0);
-            if (1 < count) request(1);
+            const int count = end - begin, start = begin + (kDecode || from != 0 || to != tiles || done % count * kTokens > qmin ? 0 : done % count);
+            const int shown = (qmin + 1) / kTokens;      // tiles from here on have keys that some column does not see
+            const bool split = !kDecode && cut.m > 1;    // ... and others do
 
+            // The tiles in hand: values are taken of `before`, scores of `now`; `last_asked` is the latest requested, and left_to_ask are still to be.  Their stages go round
+            // with them.  (Past the end of the order the last tile is read again, into stages that nothing reads: the loop has one shape.)
+            int before = 0, now = 0, after = 0, last_asked = 0, left_to_ask = 0;
+            unsigned st_before = 0, st_now = 0, st_after = 0, st_next = 0;
+            // A request in six short parts, which go behind products one by one: address arithmetic is scalar and has no other wave to hide behind.  A run of the wave's eight
+            // tokens an instruction follows; positions past the last one repeat that.
+            struct { int at, room; int64_t row; const unsigned char* src; uint32_t off; } ask;
+            auto plan = [&](int part) {
+                if (part == 0) {
+                    if (left_to_ask > 0) last_asked = last_asked + 1 == end ? begin : last_asked + 1;
+                    --left_to_ask;
+                } else if (part == 1) {
+                    const int r0 = last_asked * kTokens + wave * 8;
+                    ask.room = last - r0;
+                    ask.at = min(r0, last);
+                } else if (part == 2) {
+                    ask.row = page_of(ask.at);
+                } else if (part == 3) {
+                    ask.row = ask.row * ps + (ask.at & (ps - 1));
+                } else if (part == 4) {
+                    ask.src = (const unsigned char*)a.c.pool + ask.row * kRB;
+                } else {
+                    ask.off = (uint32_t)min(lane >> 3, max(ask.room, 0)) * kRB + piece;
+                }
+            };
+            constexpr int kParts = 6;
+            auto request = [&](int b) { load_to_lds_from(ask.src + b * 128, ask.off, lds0 + st_next + wave * (8 * kRB) + b * 1024); };
+            auto go_round = [&] {
+                before = now;
+                now = after;
+                after = last_asked;
+                const unsigned x = st_before;
+                st_before = st_now;
+                st_now = st_after;
+                st_after = st_next;
+                st_next = x;
+            };
+            auto request_all = [&] {
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) plan(part);
+#pragma unroll
+                for (int b = 0; b < Rw::kBlocks; ++b) request(b);
+                go_round();
+            };
             bf16x8 qf[Rw::kSteps];
             {
                 const __bf16* qp = (const __bf16*)a.q + (base_row + col) * (L + R) + hi * 8;
 #pragma unroll
                 for (int i = 0; i < Rw::kSteps; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(qp + i * 16);
             }
-            float m = -INFINITY, lsum = 0.f;
+            // m is a reference that every weight of the column is taken under, the largest score of its first tile: weights may come out far above one, and only if they
+            // leave what kMostWeight allows for (or nothing came out at all) the piece is done again, under the largest score of all its tiles.  O never has to be rescaled.
+            float m = -INFINITY, lsum;
             f32x16 o[kCb];
-#pragma unroll
-            for (int cb = 0; cb < kCb; ++cb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[cb][i] = 0.f;
-            AG_WAIT_VMCNT(0);
-
+            bool wrong = false;                  // this column's weights
             Weights pa, pb;
+            auto request_first = [&] {
+                AG_WAIT_VMCNT(0);
+                barrier();                       // the last tiles have been read, and no request is on the way
+                st_before = 0, st_now = Rw::kTile, st_after = 2 * Rw::kTile, st_next = 3 * Rw::kTile;
+                left_to_ask = count;
+                last_asked = start == begin ? end - 1 : start - 1;       // (the first plan() steps to `start`)
+                request_all();
+                request_all();
+            };
+            auto largest = [](const f32x16& s) {
+                float x = s[0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) pa.k[0][i] = pa.k[1][i] = pb.k[0][i] = pb.k[1][i] = (__bf16)0.f;
-            auto iter = [&](int i, const Weights& p_prev, Weights& p_cur) {
-                const bool do_sm = i < count, do_pv = i > 0;
-                const int t = tile_at(i);
-                if (do_sm) {
-                    if (i + 1 < count) AG_WAIT_VMCNT(Rw::kBlocks);
-                    else AG_WAIT_VMCNT(0);
-                }
-                barrier();                       // tile i is there, and every wave has taken the values of tile i - 2
-                if (i + 2 < count) request(i + 2);
+                for (int e = 1; e < 16; ++e) x = fmaxf(x, s[e]);
+                return x;
+            };
+            // Scores of the tile `now`, values of the one before
+            auto iter = [&](auto scores, auto values, float& sum, f32x16& s) {
+                AG_WAIT_VMCNT(Rw::kBlocks);
+                barrier();                       // `now` is there, and every wave has taken the values of the tile two before
                 // A weight of zero does not hide a NaN.  Rows that only some of the columns see are looked through, their scores being taken: what is not
-                // finite in them becomes zero for the value product, and goes to the columns that see it afterwards.
-                const int tv = do_pv ? tile_at(i - 1) : 0, seen = qmin + 1 - tv * kTokens;        // tokens below `seen` are seen by all columns
+                                // finite in them becomes zero for the value product, and goes to the columns that see it afterwards.
+                                constexpr bool kValues = decltype(values)::value;
                 bool bad = false;
-                if (!kDecode && cut.m > 1 && do_pv && seen < kTokens) {
+                if (kValues && split && before >= shown) {
+                    const int tv = before, seen = qmin + 1 - tv * kTokens;         // tokens below `seen` are seen by all columns
                     const int unseen = max(seen, 0);
-                    unsigned char* const tile = lds + ((i - 1) % kStages) * Rw::kTile;
-                    bool mine = false;
-                    for (int x = tid; x < (kTokens - unseen) * (L / 8); x += 256) {
-                        const int tok = unseen + x / (L / 8), c = x % (L / 8);
-                        u32x4* const at = reinterpret_cast<u32x4*>(tile + (tok >> 3) * (8 * kRB) + (c >> 3) * 1024 + (tok & 7) * 128 + ((c & 7) ^ turn_of(tok)) * 16);
-                        u32x4 v = *at;
-                        uint32_t any = 0;
+                                    unsigned char* const tile = lds + st_before;
+                                    bool mine = false;
+                                    for (int x = tid; x < (kTokens - unseen) * (L / 8); x += 256) {
+                                        const int tok = unseen + x / (L / 8), c = x % (L / 8);
+                                        u32x4* const at = reinterpret_cast<u32x4*>(tile + (tok >> 3) * (8 * kRB) + (c >> 3) * 1024 + (tok & 7) * 128 + ((c & 7) ^ turn_of(tok)) * 16);
+                                        u32x4 v = *at;
+                                        uint32_t any = 0;
+                #pragma unroll
+                                        for (int j = 0; j < 4; ++j) {
+                                            const uint32_t high = ((v[j] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;       // the halves whose exponent is all ones
+                                            any |= high;
+                                            v[j] &= ~((high << 1) - (high >> 15));
+                                        }
+                                        if (any) {
+                                            *at = v;
+                                            mine = true;
+                                        }
+                                    }
+                                    if (mine) *s_bad = 1;
+                                    __syncthreads();
+                                    bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
+                                }
+                auto between = [&](int j) {
+                    if (j < kParts) plan(j);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t high = ((v[j] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;       // the halves whose exponent is all ones
-                            any |= high;
-                            v[j] &= ~((high << 1) - (high >> 15));
-                        }
-                        if (any) {
-                            *at = v;
-                            mine = true;
-                        }
-                    }
-                    if (mine) *s_bad = 1;
-                    __syncthreads();
-                    bad = *reinterpret_cast<volatile int*>(s_bad) != 0;
-                }
-                f32x16 s;
-                if (do_sm) {
-                    s = scores<L, R>(k_lane + (i % kStages) * Rw::kTile, qf);
-                    if (t * kTokens + kTokens - 1 > qmin) {
-                        const int key = t * kTokens + hi * 4;
+                    for (int b = 0; b < Rw::kBlocks; ++b)
+                        if (j == kParts + b * (Rw::kSteps - kParts) / Rw::kBlocks) request(b);
+                };
+                auto mask = [&](f32x16& s) {
+                    if (now < shown) return;
+                    const int key = now * kTokens + hi * 4;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) s[e] = key + (e >> 2) * 8 + (e & 3) <= qpos ? s[e] : -INFINITY;
-                    }
-                }
-                softmax_and_values<L, R, kCb>(do_sm, do_pv, v_lane + ((i + kStages - 1) % kStages) * Rw::kTile, s, sl2, m, lsum, p_prev, p_cur, o);
+                    for (int e = 0; e < 16; ++e) s[e] = key + (e >> 2) * 8 + (e & 3) <= qpos ? s[e] : -INFINITY;
+                };
+                const unsigned k0 = k_lane + st_now, v0 = v_lane + st_before;
+                step<L, R, kCb, decltype(scores)::value, kValues>(k0, v0, qf, sl2, m, sum, s, pa, pb, o, between, mask);
                 if (bad) {
+                    products_end();
 #pragma unroll 1
-                    for (int at = max(tv * kTokens, qmin + 1); at <= min(tv * kTokens + kTokens - 1, last); ++at) {
+                    for (int at = max(before * kTokens, qmin + 1); at <= min(before * kTokens + kTokens - 1, last); ++at) {
                         const int page = bt[at >> shift];
                         const uint16_t* const row = (const uint16_t*)a.c.pool + ((int64_t)page * ps + (at & (ps - 1))) * Rw::kRow + part * (kCb * 32) + hi * 4;
 #pragma unroll
@@ -531,15 +553,60 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                     if (tid == 0) *s_bad = 0;
                     __syncthreads();
                 }
+                go_round();
             };
+            constexpr std::true_type yes{};
+            constexpr std::false_type no{};
+            for (int attempt = 0;; ++attempt) {
+                f32x16 s;
+                float sum;
+                if (attempt > 0) {
+                    request_first();
+                    float most = -INFINITY;
 #pragma unroll 1
-            for (int i = 0; i <= count; i += 2) {
-                iter(i, pb, pa);
-                if (i + 1 <= count) iter(i + 1, pa, pb);
+                    for (int i = 0; i < count; ++i) {
+                        iter(yes, no, sum, s);
+                        most = fmaxf(most, largest(s));
+                    }
+                    most = fmaxf(most, __shfl_xor(most, 32)) * sl2;               // (scale > 0: maximum and scaling commute)
+                    if (wrong) m = most == -INFINITY ? 0.f : most;
+                }
+                request_first();
+                iter(yes, no, sum, s);
+                if (attempt == 0) {
+                    m = largest(s);
+                    m = fmaxf(m, __shfl_xor(m, 32)) * sl2;                         // the two lanes of a column share it
+                    if (m == -INFINITY) m = 0.f;                                   // (no key seen yet: weights of zero)
+                }
+                lsum = weigh(s, sl2, m, pa);
+                wrong = !(lsum <= kMostWeight);
+#pragma unroll
+                for (int cb = 0; cb < kCb; ++cb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[cb][i] = 0.f;
+#pragma unroll 1
+                for (int i = 1; i < count; ++i) {
+                    iter(yes, yes, sum, s);
+                    pa = pb;
+                    lsum += sum;
+                    wrong |= !(sum <= kMostWeight);
+                }
+                iter(no, yes, sum, s);
+                done += count;
+                products_end();
+                lsum += __shfl_xor(lsum, 32);
+                // (a column that sees no key of the piece has a sum of zero, and that is right)
+                wrong |= lsum < kLeastSum && begin * kTokens <= qpos;
+                wrong |= __shfl_xor((int)wrong, 32) != 0;
+                if (attempt > 0) break;
+                if (__builtin_amdgcn_ballot_w64(wrong) != 0 && lane == 0) *s_again = 1;
+                __syncthreads();
+                if (__builtin_amdgcn_readfirstlane(*s_again) == 0) break;
+                __syncthreads();
+                if (tid == 0) *s_again = 0;
             }
-            done += count;
+            if (lsum == 0.f) m = -INFINITY;
 
-            lsum += __shfl_xor(lsum, 32);
             if (from == 0 && to == tiles) {
                 // rows that are whole in LDS, 16-byte pieces in a place that depends on the row (8-byte stores of the accumulators themselves, 32 rows an
                 // instruction, took 100 us for every unit of the 256 CUs)
@@ -606,7 +673,7 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* 
     __shared__ int s_cut[kMostShares];
     __shared__ int s_count[4];
     __shared__ float s_part[3][64][2 + 4 * kQ];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Record* const recs = reinterpret_cast<const Record*>(ws);
     {
         static_assert(kMostShares <= 256, "a thread a record");
@@ -639,7 +706,8 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* 
                 f32x4 v[kFlight][kQ];
 #pragma unroll
                 for (int j = 0; j < kFlight; ++j) {
-                    const int p = min(p0 + 4 * j, rec.pieces - 1);
+                    const int p = p0 + 4 * j;
+                    if (p >= rec.pieces) break;
                     const int64_t place = p == 0 ? 2 * (w - 1) + 1 : 2 * (w + p - 1);
                     x[j] = ml[place * cols + col];
 #pragma unroll
