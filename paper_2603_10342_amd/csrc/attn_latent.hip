@@ -46,14 +46,15 @@ constexpr float kLeastSum = 1.0f / kMostWeight;
 // Columns of a tile: whole query rows' heads while they fit (m rows of `heads` columns), otherwise parts of one row's heads (nh tiles a row).
 struct Cut {
     int cols, heads, m, nh;
-    __host__ __device__ Cut(int cols_, int heads_) : cols(cols_), heads(heads_), m(heads_ < cols_ ? cols_ / heads_ : 1), nh((heads_ + cols_ - 1) / cols_) {}
+    int lead;                   // what a unit costs beside its tiles, in tiles: its queries, its first tile, its output
+    __host__ __device__ Cut(int cols_, int heads_, int lead_)
+        : cols(cols_), heads(heads_), m(heads_ < cols_ ? cols_ / heads_ : 1), nh((heads_ + cols_ - 1) / cols_), lead(lead_) {}
 };
 
 // Work is counted in tiles of 32 keys for decode.  A chunk's column tile k counts the keys that its last row sees, P + min((k + 1) m, N), so that the
-// sum over the tiles of a session has a closed form; shares are multiples of 32 of that.  A unit costs kLead on top, for its queries, first tile and output.
-constexpr int kLeadTiles = 4;
-template <bool kDecode> struct Counting { typedef uint32_t Cost; static constexpr int kTile = 1, kLead = kLeadTiles; };
-template <> struct Counting<false> { typedef uint64_t Cost; static constexpr int kTile = kTokens, kLead = kLeadTiles * kTokens; };
+// sum over the tiles of a session has a closed form; shares are multiples of 32 of that.  A unit costs `lead` tiles on top.
+template <bool kDecode> struct Counting { typedef uint32_t Cost; static constexpr int kTile = 1; };
+template <> struct Counting<false> { typedef uint64_t Cost; static constexpr int kTile = kTokens; };
 
 struct Lens { int prefix, n, row0; };   // of a session
 template <bool kDecode>
@@ -67,14 +68,17 @@ __device__ __forceinline__ Lens lens_of(const AttnArgs& a, int s)
     }
 }
 // of column tiles 0 .. k - 1 of a session (all full), without the factor nh
-__device__ __forceinline__ uint64_t cost_below(const Lens& x, int m, uint64_t k) { return k * ((uint64_t)x.prefix + Counting<false>::kLead) + (uint64_t)m * (k * (k + 1) / 2); }
+__device__ __forceinline__ uint64_t cost_below(const Lens& x, const Cut& cut, uint64_t k)
+{
+    return k * ((uint64_t)x.prefix + (uint64_t)cut.lead * kTokens) + (uint64_t)cut.m * (k * (k + 1) / 2);
+}
 template <bool kDecode>
 __device__ __forceinline__ typename Counting<kDecode>::Cost session_cost(const Lens& x, const Cut& cut)
 {
     if (x.n <= 0) return 0;
-    if constexpr (kDecode) return (uint32_t)cut.nh * (uint32_t)((x.prefix + kTokens) / kTokens + kLeadTiles);
+    if constexpr (kDecode) return (uint32_t)cut.nh * (uint32_t)((x.prefix + kTokens) / kTokens + cut.lead);
     const uint64_t k = (x.n - 1) / cut.m;                              // tiles before the last
-    return (uint64_t)cut.nh * (cost_below(x, cut.m, k) + x.prefix + x.n + Counting<false>::kLead);
+    return (uint64_t)cut.nh * (cost_below(x, cut, k) + x.prefix + x.n + (uint64_t)cut.lead * kTokens);
 }
 
 template <typename T>
@@ -135,11 +139,11 @@ struct Share {
             int lo = 0, hi = (u.x.n - 1) / cut.m;                      // the last tile that starts at or before y
             while (lo < hi) {
                 const int mid = lo + (hi - lo + 1) / 2;
-                if ((uint64_t)cut.nh * cost_below(u.x, cut.m, mid) <= y) lo = mid;
+                if ((uint64_t)cut.nh * cost_below(u.x, cut, mid) <= y) lo = mid;
                 else hi = mid - 1;
             }
             u.k = lo;
-            y -= (uint64_t)cut.nh * cost_below(u.x, cut.m, lo);
+            y -= (uint64_t)cut.nh * cost_below(u.x, cut, lo);
         }
         const Cost c = cost(cut);
         u.hh = (int)(y / c);
@@ -147,9 +151,9 @@ struct Share {
     }
     __device__ __forceinline__ int last_pos(const Cut& cut) const { return u.x.prefix + min((u.k + 1) * cut.m, u.x.n) - 1; }      // that the unit's last row sees
     __device__ __forceinline__ int tiles(const Cut& cut) const { return last_pos(cut) / kTokens + 1; }
-    __device__ __forceinline__ Cost cost(const Cut& cut) const { return (kDecode ? (Cost)tiles(cut) : (Cost)last_pos(cut) + 1) + Counting<kDecode>::kLead; }
+    __device__ __forceinline__ Cost cost(const Cut& cut) const { return (kDecode ? (Cost)tiles(cut) : (Cost)last_pos(cut) + 1) + (Cost)cut.lead * Counting<kDecode>::kTile; }
     // tiles of the unit that lie before a cut at `y`
-    static __device__ __forceinline__ int tiles_before(Cost y) { return y < Counting<kDecode>::kLead ? 0 : (int)((y - Counting<kDecode>::kLead) / Counting<kDecode>::kTile); }
+    static __device__ __forceinline__ int tiles_before(const Cut& cut, Cost y) { return max((int)(y / Counting<kDecode>::kTile) - cut.lead, 0); }
     // the unit after u, from its start
     __device__ __forceinline__ bool next(const AttnArgs& a, const Cut& cut)
     {
@@ -334,7 +338,7 @@ __device__ __forceinline__ void step(unsigned k0, unsigned v0, const bf16x8 (&qf
 }
 
 template <int L, int R, int kSplit, bool kDecode>
-__global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
+__global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, int lead)
 {
     typedef Row<L, R> Rw;
     constexpr int kCols = 128 / kSplit, kCb = L / 32 / kSplit, kRB = Rw::kBytes;
@@ -344,18 +348,18 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
     const unsigned lds0 = lds_address(lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ct = wave / kSplit, part = wave % kSplit, n = lane & 31, hi = lane >> 5;
-    const Cut cut(kCols, a.heads);
+    const Cut cut(kCols, a.heads, lead);
     const int shares = gridDim.x;
     // shares that follow each other on one XCD: they read the same rows
     const int w = shares % 8 == 0 ? (blockIdx.x % 8) * (shares / 8) + blockIdx.x / 8 : blockIdx.x;
     Share<kDecode> sh(a, cut, w, shares, least);
     typedef typename Share<kDecode>::Cost Cost;
-    constexpr Cost kT = Counting<kDecode>::kTile, kLead = Counting<kDecode>::kLead;
+    constexpr Cost kT = Counting<kDecode>::kTile;
 
     if (tid == 0) {
         Record rec = {0, 0, 0};
-        if (sh.len && sh.tiles_before(sh.off) > 0) {
-            const Cost u0 = sh.begin - sh.off, first = (u0 + kLead + kT + sh.per - 1) / sh.per;       // the first share whose start cuts the unit
+        if (sh.len && sh.tiles_before(cut, sh.off) > 0) {
+            const Cost u0 = sh.begin - sh.off, first = (u0 + (cut.lead + 1) * kT + sh.per - 1) / sh.per;       // the first share whose start cuts the unit
             if (first == (Cost)w) {
                 rec.row = ((int64_t)sh.u.x.row0 + (int64_t)sh.u.k * cut.m) * a.heads + (int64_t)sh.u.hh * kCols;
                 rec.cols = a.heads <= kCols ? min(cut.m, sh.u.x.n - sh.u.k * cut.m) * a.heads : min(kCols, a.heads - sh.u.hh * kCols);
@@ -386,7 +390,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
         const int tiles = sh.tiles(cut);
         const Cost rest = sh.cost(cut) - sh.off;
         // the piece of the unit, counted from its far end: a share starts with the first keys of a unit, like the whole units that others take at that time
-        const int from = sh.tiles_before(sh.off), to = left >= rest ? tiles : sh.tiles_before(sh.off + left), begin = tiles - to, end = tiles - from;
+        const int from = sh.tiles_before(cut, sh.off), to = left >= rest ? tiles : sh.tiles_before(cut, sh.off + left), begin = tiles - to, end = tiles - from;
         if (begin < end) {
             // ---- the unit's columns ----
             const Unit& u = sh.u;
@@ -458,18 +462,6 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                 for (int b = 0; b < Rw::kBlocks; ++b) request(b);
                 go_round();
             };
-            bf16x8 qf[Rw::kSteps];
-            {
-                const __bf16* qp = (const __bf16*)a.q + (base_row + col) * (L + R) + hi * 8;
-#pragma unroll
-                for (int i = 0; i < Rw::kSteps; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(qp + i * 16);
-            }
-            // m is a reference that every weight of the column is taken under, the largest score of its first tile: weights may come out far above one, and only if they
-            // leave what kMostWeight allows for (or nothing came out at all) the piece is done again, under the largest score of all its tiles.  O never has to be rescaled.
-            float m = -INFINITY, lsum;
-            f32x16 o[kCb];
-            bool wrong = false;                  // this column's weights
-            Weights pa, pb;
             auto request_first = [&] {
                 AG_WAIT_VMCNT(0);
                 barrier();                       // the last tiles have been read, and no request is on the way
@@ -479,6 +471,42 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                 request_all();
                 request_all();
             };
+            // ---- the queries, as B operands: column n, channels i * 16 + hi * 8 .. + 7 ----
+            bf16x8 qf[Rw::kSteps];
+            request_first();
+            const __bf16* const q0 = (const __bf16*)a.q + base_row * (L + R);
+            if constexpr (kSplit == 1) {
+                const __bf16* qp = q0 + (int64_t)col * (L + R) + hi * 8;
+#pragma unroll
+                for (int i = 0; i < Rw::kSteps; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(qp + i * 16);
+                AG_WAIT_VMCNT(0);
+            } else {
+                // By way of the stages that the first tiles do not take: waves that share columns read them once, in whole lines (16 bytes a lane out of 32 rows are 64
+                // requests an instruction).  Where a row ends inside a run of 128 bytes, lanes past its end repeat its last half.
+                static_assert(kSplit == 4 || kSplit == 2, "a stage for 32 columns, and two are free");
+#pragma unroll
+                for (int t = 0; t < 4 / kSplit; ++t) {
+                    const unsigned dst = lds0 + (t + 1) * Rw::kTile + wave * (8 * kRB);
+                    const int row = min(t * 32 + wave * 8 + (lane >> 3), cols - 1);
+#pragma unroll
+                    for (int b = 0; b < Rw::kBlocks; ++b) {
+                        const uint32_t in = (b + 1) * 64 <= L + R ? piece : piece & 63;
+                        load_to_lds_from(reinterpret_cast<const unsigned char*>(q0) + b * 128, (uint32_t)row * ((L + R) * 2) + in, dst + b * 1024);
+                    }
+                }
+                AG_WAIT_VMCNT(0);
+                barrier();
+                const unsigned k0 = k_lane + (ct + 1) * Rw::kTile, kb[4] = {k0, k0 ^ 32, k0 ^ 64, k0 ^ 96};
+#pragma unroll
+                for (int i = 0; i < Rw::kSteps; ++i) qf[i] = read_along(kb[i & 3] + (i >> 2) * 1024);
+                __builtin_amdgcn_s_waitcnt(0xC07F);         // lgkmcnt(0): they are read before the next barrier lets a request into their stages
+            }
+            // m is a reference that every weight of the column is taken under, the largest score of its first tile: weights may come out far above one, and only if they
+            // leave what kMostWeight allows for (or nothing came out at all) the piece is done again, under the largest score of all its tiles.  O never has to be rescaled.
+            float m = -INFINITY, lsum;
+            f32x16 o[kCb];
+            bool wrong = false;                  // this column's weights
+            Weights pa, pb;
             auto largest = [](const f32x16& s) {
                 float x = s[0];
 #pragma unroll
@@ -571,7 +599,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                     most = fmaxf(most, __shfl_xor(most, 32)) * sl2;               // (scale > 0: maximum and scaling commute)
                     if (wrong) m = most == -INFINITY ? 0.f : most;
                 }
-                request_first();
+                if (attempt > 0) request_first();
                 iter(yes, no, sum, s);
                 if (attempt == 0) {
                     m = largest(s);
@@ -646,7 +674,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least)
                         f32x4 v;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) v[i] = o[cb][q * 4 + i];
-                        __builtin_nontemporal_store(v, op + (cb * 4 + q) * 64);
+                        op[(cb * 4 + q) * 64] = v;
                     }
                 }
             }
@@ -762,17 +790,23 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* 
 
 // ---- the host's side ----
 
-constexpr int kLeastTiles = 4;          // of a share
+// Tiles of a share at least: what a piece writes and a merge reads back, the columns' O in fp32, is worth a few.  Decode, us, 2 / 4 / 8 tiles: one session of 1000 tokens,
+// 32 heads 13.3 / 15.1 / 18.9; two of 10500 together, 128 heads 38.2 / 35.1 / 32.0.
+constexpr int least_tiles(int cols) { return cols == 32 ? 2 : cols == 64 ? 4 : 8; }
 constexpr int kMergeMost = 1024;        // workgroups of a merge
 
 int columns(int64_t most) { return most <= 32 ? 32 : most <= 64 ? 64 : 128; }
 
-// Shares of a launch whose units are at most `units` of `tiles` tiles: no more than have kLeastTiles each.
-int shares_of(int64_t units, int64_t tiles, int cus)
+// Shares of a launch whose units are at most `units` of `tiles` tiles.
+int shares_of(int64_t units, int64_t tiles, int cols, int cus)
 {
-    const int64_t n = (units * tiles + kLeastTiles - 1) / kLeastTiles;
+    const int64_t n = (units * tiles + least_tiles(cols) - 1) / least_tiles(cols);
     return (int)std::max<int64_t>(1, std::min<int64_t>(n, std::min(cus, kMostShares)));
 }
+// A unit's lead, measured in whole prompts of 500 to 700 rows at 128 heads, where a share has up to fifty: 4, 8, 12 tiles 356, 287, 287 us; where shares are smaller than
+// that, less, so that none is left with a lead alone.
+constexpr int kMostLead = 8;
+int lead_of(int64_t units, int64_t tiles, int shares) { return (int)std::min<int64_t>(kMostLead, units * tiles / shares / 2); }
 int64_t units_of(bool decode, int batch, int total, const Cut& cut)
 {
     return (decode ? (int64_t)batch : (int64_t)total / cut.m + batch) * cut.nh;
@@ -780,14 +814,14 @@ int64_t units_of(bool decode, int batch, int total, const Cut& cut)
 size_t bytes_of(int shares, int cols, int lat) { return o_offset(2 * shares, cols) + (size_t)2 * shares * place_floats(cols, lat) * 4; }
 
 template <int L, int R, int kSplit, bool kDecode>
-ag_status run(const AttnArgs& a, int64_t units, int shares, hipStream_t st)
+ag_status run(const AttnArgs& a, int64_t units, int shares, int lead, hipStream_t st)
 {
     static std::atomic<uint64_t> told{0};
     constexpr int kLds = kStages * Row<L, R>::kTile + 16;
     ag_status e = allow_dynamic_lds((const void*)latent_kernel<L, R, kSplit, kDecode>, kLds, told);
     if (e) return e;
     prof_before(st);
-    hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, kLeastTiles);
+    hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, least_tiles(128 / kSplit), lead);
     if (shares > 1) {
         constexpr int kCols = 128 / kSplit, kSlices = kCols / 8 * (L / 32);
         const int64_t cuts = std::min<int64_t>(shares - 1, units);
@@ -799,14 +833,14 @@ ag_status run(const AttnArgs& a, int64_t units, int shares, hipStream_t st)
     return hip_check(hipGetLastError(), "latent attention launch");
 }
 template <int L, int R>
-ag_status run_columns(const AttnArgs& a, int cols, int64_t units, int shares, hipStream_t st)
+ag_status run_columns(const AttnArgs& a, int cols, int64_t units, int shares, int lead, hipStream_t st)
 {
     if (a.ctx_lens) {
-        if (cols == 32) return run<L, R, 4, true>(a, units, shares, st);
-        return cols == 64 ? run<L, R, 2, true>(a, units, shares, st) : run<L, R, 1, true>(a, units, shares, st);
+        if (cols == 32) return run<L, R, 4, true>(a, units, shares, lead, st);
+        return cols == 64 ? run<L, R, 2, true>(a, units, shares, lead, st) : run<L, R, 1, true>(a, units, shares, lead, st);
     }
-    if (cols == 32) return run<L, R, 4, false>(a, units, shares, st);
-    return cols == 64 ? run<L, R, 2, false>(a, units, shares, st) : run<L, R, 1, false>(a, units, shares, st);
+    if (cols == 32) return run<L, R, 4, false>(a, units, shares, lead, st);
+    return cols == 64 ? run<L, R, 2, false>(a, units, shares, lead, st) : run<L, R, 1, false>(a, units, shares, lead, st);
 }
 
 }  // namespace
@@ -817,11 +851,11 @@ size_t attn_workspace(bool decode, int batch, int total, int heads, int lat, int
     size_t most = 0;
     for (int cols : {32, 64, 128}) {
         if (cols > columns((int64_t)total * heads)) break;             // (no session has more columns than all rows)
-        const Cut cut(cols, heads);
+        const Cut cut(cols, heads, 0);
         const int64_t units = units_of(decode, batch, total, cut);
         // sums of costs: 32 bits of tiles for decode, 64 of keys otherwise
-        if ((double)units * (double)(tiles + kLeadTiles) >= (decode ? 2147483648.0 : 1.0e16)) return 0;
-        most = std::max(most, bytes_of(shares_of(units, tiles, kMostShares), cols, lat));
+        if ((double)units * (double)(tiles + kMostLead) >= (decode ? 2147483648.0 : 1.0e16)) return 0;
+        most = std::max(most, bytes_of(shares_of(units, tiles, cols, kMostShares), cols, lat));
     }
     return most;
 }
@@ -830,12 +864,13 @@ ag_status launch_attn(const AttnArgs& a, hipStream_t st)
 {
     const bool decode = a.ctx_lens != nullptr;
     const int cols = columns(decode ? a.heads : (int64_t)a.max_new * a.heads);
-    const Cut cut(cols, a.heads);
+    const Cut cut(cols, a.heads, 0);
     const int64_t units = units_of(decode, a.batch, a.total, cut);
-    const int shares = shares_of(units, ((int64_t)a.max_ctx + kTokens - 1) / kTokens, stream_cus(st));
-    if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, units, shares, st) : run_columns<512, 32>(a, cols, units, shares, st);
-    if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, units, shares, st) : run_columns<256, 32>(a, cols, units, shares, st);
-    return a.c.rd == 64 ? run_columns<128, 64>(a, cols, units, shares, st) : run_columns<128, 32>(a, cols, units, shares, st);
+    const int64_t tiles = ((int64_t)a.max_ctx + kTokens - 1) / kTokens;
+    const int shares = shares_of(units, tiles, cols, stream_cus(st)), lead = lead_of(units, tiles, shares);
+    if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, units, shares, lead, st) : run_columns<512, 32>(a, cols, units, shares, lead, st);
+    if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, units, shares, lead, st) : run_columns<256, 32>(a, cols, units, shares, lead, st);
+    return a.c.rd == 64 ? run_columns<128, 64>(a, cols, units, shares, lead, st) : run_columns<128, 32>(a, cols, units, shares, lead, st);
 }
 
 }  // namespace latent
