@@ -205,7 +205,7 @@ __device__ __forceinline__ void barrier()
     asm volatile("" ::: "memory");
 }
 
-constexpr int kAhead = 3;               // operand reads run this many products ahead of their use
+constexpr int kAhead = 4;               // operand reads run this many products ahead of their use
 
 // The products are written in assembly because the scores' accumulators have to be vector registers and O's accumulation registers: the compiler gives all matrix
 // instructions of a kernel the same kind, and O^T fills that.  What the compiler keeps for its own matrix instructions is kept here by hand: two states between a vector
@@ -213,15 +213,15 @@ constexpr int kAhead = 3;               // operand reads run this many products 
 // products_end(), 20 states after the last product (18 are asked for behind the longest there is).  Operands come by the compiler's loads, whose arrival it waits for.
 __device__ __forceinline__ void score_product_first(f32x16& s, const bf16x8& a, const bf16x8& b)
 {
-    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void score_product(f32x16& s, const bf16x8& a, const bf16x8& b)
 {
-    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void value_product(f32x16& o, const bf16x8& a, const bf16x8& b)
 {
-    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(a), "v"(b));
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void products_end() { asm volatile("s_nop 15\n\ts_nop 3"); }
 __device__ __forceinline__ void products_end(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
