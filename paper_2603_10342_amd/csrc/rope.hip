@@ -73,9 +73,11 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RowsArgs x)
 
 // One workgroup per touched 16-token group of a session and KV head: its keys and values, and the group's query heads.  Keys and values go
 // through LDS, from rows that are read whole to runs of slots that are written whole.
+// kStream: what is written is more than the last cache holds, and marked so that it does not go through the nearer ones (8 x 4096 tokens, 32 and 8 heads x 128, 403 MB
+// written: 186 -> 172 us of 805 MB; a step's tokens are read next, and cost 5.0 -> 5.2 us so).
 constexpr int kGroup = 16;
 
-template <typename A, bool kPairs>
+template <typename A, bool kPairs, bool kStream>
 __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs x)
 {
     constexpr int kAtOnce = 2;
@@ -144,7 +146,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs x)
             int t, u;
             const int64_t row = q_row(i, t, u);
             turn_unit<kPairs>(us, u, s_cs + t * x.r.half, rq[j]);
-            store_unit<kPairs>(us, (A*)x.q_out + row, u, rq[j]);
+            store_unit<kPairs, kStream>(us, (A*)x.q_out + row, u, rq[j]);
         }
         i0 += 256 * kAtOnce;
         load_q(i0);
@@ -155,7 +157,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs x)
     A *const kpage = (A*)x.c.k + block, *const vpage = (A*)x.c.v + block;
     for (int i = tid; i < nv; i += 256) {                              // keys: neighbouring lanes, neighbouring slots
         const int c = i / n_tok, t = i - c * n_tok;
-        *reinterpret_cast<Eight<A>*>(kpage + ((int64_t)c * ps + slot0 + t) * 8) = *reinterpret_cast<const Eight<A>*>(s_k + t * pitch + c * 8);
+        store_eight<kStream>(kpage + ((int64_t)c * ps + slot0 + t) * 8, *reinterpret_cast<const Eight<A>*>(s_k + t * pitch + c * 8));
     }
     if (n_tok == kGroup) {                                             // values of a whole group: chunks of eight slots
         for (int i = tid; i < 2 * d; i += 256) {
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs x)
                 v.e[e] = s_v[(half * 4 + e) * pitch + ch];
                 v.e[4 + e] = s_v[(8 + half * 4 + e) * pitch + ch];
             }
-            *reinterpret_cast<Eight<A>*>(vpage + ((int64_t)((slot0 >> 3) + half) * d + ch) * 8) = __builtin_bit_cast(Eight<A>, v);
+            store_eight<kStream>(vpage + ((int64_t)((slot0 >> 3) + half) * d + ch) * 8, __builtin_bit_cast(Eight<A>, v));
         }
     } else {                                                           // the other slots stay as they are
         for (int i = tid; i < n_tok * d; i += 256) {
@@ -186,6 +188,14 @@ ag_status rows_typed(const RowsArgs& a, hipStream_t st)
     return hip_check(hipGetLastError(), "rope launch");
 }
 
+template <typename A, bool kPairs>
+void append_typed(const AppendArgs& a, dim3 grid, size_t lds, hipStream_t st)
+{
+    const int64_t written = (int64_t)a.total * (2 * a.c.hkv + a.hq) * a.c.d * (int64_t)sizeof(A);
+    if (written > 256ll << 20) hipLaunchKernelGGL((append_rope_kernel<A, kPairs, true>), grid, dim3(256), lds, st, a);
+    else hipLaunchKernelGGL((append_rope_kernel<A, kPairs, false>), grid, dim3(256), lds, st, a);
+}
+
 }  // namespace
 
 ag_status launch_rows(const RowsArgs& a, hipStream_t st)
@@ -202,13 +212,8 @@ ag_status launch_append(const AppendArgs& a, hipStream_t st)
     const size_t el = a.c.dtype == AG_BF16 ? 2 : 4;
     const size_t lds = 2 * kGroup * (a.c.d * el + 16) + kGroup * a.r.half * sizeof(f32x2);
     const bool pairs = a.layout == AG_ROPE_PAIRS;
-    if (a.c.dtype == AG_BF16) {
-        if (pairs) hipLaunchKernelGGL((append_rope_kernel<__bf16, true>), grid, dim3(256), lds, st, a);
-        else hipLaunchKernelGGL((append_rope_kernel<__bf16, false>), grid, dim3(256), lds, st, a);
-    } else {
-        if (pairs) hipLaunchKernelGGL((append_rope_kernel<float, true>), grid, dim3(256), lds, st, a);
-        else hipLaunchKernelGGL((append_rope_kernel<float, false>), grid, dim3(256), lds, st, a);
-    }
+    if (a.c.dtype == AG_BF16) pairs ? append_typed<__bf16, true>(a, grid, lds, st) : append_typed<__bf16, false>(a, grid, lds, st);
+    else pairs ? append_typed<float, true>(a, grid, lds, st) : append_typed<float, false>(a, grid, lds, st);
     return hip_check(hipGetLastError(), "append launch");
 }
 

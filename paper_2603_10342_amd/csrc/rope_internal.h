@@ -113,12 +113,23 @@ __device__ __forceinline__ void turn_unit(const Units& us, int u, const f32x2* c
     narrow(a, r.lo);
     narrow(b, r.hi);
 }
-template <bool kPairs, typename A>
+// kStream: with the streaming hint
+template <bool kStream = false, typename A>
+__device__ __forceinline__ void store_eight(A* dst, const Eight<A>& r)
+{
+    if constexpr (kStream) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(A) / 2; ++i) __builtin_nontemporal_store(r.w[i], reinterpret_cast<u32x4*>(dst) + i);
+    } else {
+        *reinterpret_cast<Eight<A>*>(dst) = r;
+    }
+}
+template <bool kPairs, bool kStream = false, typename A>
 __device__ __forceinline__ void store_unit(const Units& us, A* row, int u, const Unit<A>& r)
 {
     const int lo = us.lo<kPairs>(u), hi = us.hi<kPairs>(u);
-    *reinterpret_cast<Eight<A>*>(row + lo) = r.lo;
-    if (hi < us.d) *reinterpret_cast<Eight<A>*>(row + hi) = r.hi;
+    store_eight<kStream>(row + lo, r.lo);
+    if (hi < us.d) store_eight<kStream>(row + hi, r.hi);
 }
 
 struct RowsArgs {
