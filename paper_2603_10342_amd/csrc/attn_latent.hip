@@ -47,8 +47,9 @@ constexpr float kLeastSum = 1.0f / kMostWeight;
 struct Cut {
     int cols, heads, m, nh;
     int lead;                   // what a unit costs beside its tiles, in tiles: its queries, its first tile, its output
-    __host__ __device__ Cut(int cols_, int heads_, int lead_)
-        : cols(cols_), heads(heads_), m(heads_ < cols_ ? cols_ / heads_ : 1), nh((heads_ + cols_ - 1) / cols_), lead(lead_) {}
+    int whole;                  // a unit of so many tiles or fewer is not cut
+    __host__ __device__ Cut(int cols_, int heads_, int lead_ = 0, int whole_ = 0)
+        : cols(cols_), heads(heads_), m(heads_ < cols_ ? cols_ / heads_ : 1), nh((heads_ + cols_ - 1) / cols_), lead(lead_), whole(whole_) {}
 };
 
 // Work is counted in tiles of 32 keys for decode.  A chunk's column tile k counts the keys that its last row sees, P + min((k + 1) m, N), so that the
@@ -108,14 +109,21 @@ struct Share {
     {
         const int lane = threadIdx.x & 63;
         Cost incl = 0;
+        int sessions = 0;
         total = 0;
         for (int base = 0; base < a.batch; base += 64) {
-            incl = scan64(base + lane < a.batch ? session_cost<kDecode>(lens_of<kDecode>(a, base + lane), cut) : (Cost)0);
+            const Cost c = base + lane < a.batch ? session_cost<kDecode>(lens_of<kDecode>(a, base + lane), cut) : (Cost)0;
+            sessions += __builtin_popcountll(__builtin_amdgcn_ballot_w64(c > 0));
+            incl = scan64(c);
             total += from_lane(incl, 63);
         }
+        // not less than `least` tiles, but for units that are smaller themselves (as far as the number of sessions tells)
         constexpr Cost kT = Counting<kDecode>::kTile;
+        Cost floor = total / (Cost)max(sessions * cut.nh, 1);
+        floor = floor < (Cost)least * kT ? floor : (Cost)least * kT;
         per = (total + shares - 1) / shares;
-        per = per < (Cost)least * kT ? (Cost)least * kT : (per + kT - 1) / kT * kT;
+        per = ((per < floor ? floor : per) + kT - 1) / kT * kT;
+        per = per > 0 ? per : kT;
         begin = (Cost)w * per;
         len = begin < total ? (total - begin < per ? total - begin : per) : 0;
         off = 0;
@@ -153,7 +161,13 @@ struct Share {
     __device__ __forceinline__ int tiles(const Cut& cut) const { return last_pos(cut) / kTokens + 1; }
     __device__ __forceinline__ Cost cost(const Cut& cut) const { return (kDecode ? (Cost)tiles(cut) : (Cost)last_pos(cut) + 1) + (Cost)cut.lead * Counting<kDecode>::kTile; }
     // tiles of the unit that lie before a cut at `y`
-    static __device__ __forceinline__ int tiles_before(const Cut& cut, Cost y) { return max((int)(y / Counting<kDecode>::kTile) - cut.lead, 0); }
+    __device__ __forceinline__ int tiles_before(const Cut& cut, Cost y) const
+    {
+        if (whole(cut)) return 2 * y > cost(cut) ? tiles(cut) : 0;
+        return max((int)(y / Counting<kDecode>::kTile) - cut.lead, 0);
+    }
+    // A unit of a few tiles goes to the share that has more of it: its pieces would cost more than they save
+    __device__ __forceinline__ bool whole(const Cut& cut) const { return tiles(cut) <= cut.whole; }
     // the unit after u, from its start
     __device__ __forceinline__ bool next(const AttnArgs& a, const Cut& cut)
     {
@@ -338,7 +352,7 @@ __device__ __forceinline__ void step(unsigned k0, unsigned v0, const bf16x8 (&qf
 }
 
 template <int L, int R, int kSplit, bool kDecode>
-__global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, int lead)
+__global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, int lead, int uncut)
 {
     typedef Row<L, R> Rw;
     constexpr int kCols = 128 / kSplit, kCb = L / 32 / kSplit, kRB = Rw::kBytes;
@@ -348,7 +362,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
     const unsigned lds0 = lds_address(lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ct = wave / kSplit, part = wave % kSplit, n = lane & 31, hi = lane >> 5;
-    const Cut cut(kCols, a.heads, lead);
+    const Cut cut(kCols, a.heads, lead, uncut);
     const int shares = gridDim.x;
     // shares that follow each other on one XCD: they read the same rows
     const int w = shares % 8 == 0 ? (blockIdx.x % 8) * (shares / 8) + blockIdx.x / 8 : blockIdx.x;
@@ -358,7 +372,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
 
     if (tid == 0) {
         Record rec = {0, 0, 0};
-        if (sh.len && sh.tiles_before(cut, sh.off) > 0) {
+        if (sh.len && sh.off && !sh.whole(cut) && sh.tiles_before(cut, sh.off) > 0) {
             const Cost u0 = sh.begin - sh.off, first = (u0 + (cut.lead + 1) * kT + sh.per - 1) / sh.per;       // the first share whose start cuts the unit
             if (first == (Cost)w) {
                 rec.row = ((int64_t)sh.u.x.row0 + (int64_t)sh.u.k * cut.m) * a.heads + (int64_t)sh.u.hh * kCols;
@@ -793,14 +807,15 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* 
 // Tiles of a share at least: what a piece writes and a merge reads back, the columns' O in fp32, is worth a few.  Decode, us, 2 / 4 / 8 tiles: one session of 1000 tokens,
 // 32 heads 13.3 / 15.1 / 18.9; two of 10500 together, 128 heads 38.2 / 35.1 / 32.0.
 constexpr int least_tiles(int cols) { return cols == 32 ? 2 : cols == 64 ? 4 : 8; }
+constexpr int uncut_tiles(int least) { return 2 * least; }         // a unit of so many tiles or fewer is not cut
 constexpr int kMergeMost = 1024;        // workgroups of a merge
 
 int columns(int64_t most) { return most <= 32 ? 32 : most <= 64 ? 64 : 128; }
 
-// Shares of a launch whose units are at most `units` of `tiles` tiles.
+// Shares of a launch whose units are at most `units` of `tiles` tiles: one for each at least, as far as there are CUs.
 int shares_of(int64_t units, int64_t tiles, int cols, int cus)
 {
-    const int64_t n = (units * tiles + least_tiles(cols) - 1) / least_tiles(cols);
+    const int64_t n = std::max<int64_t>(units, (units * tiles + least_tiles(cols) - 1) / least_tiles(cols));
     return (int)std::max<int64_t>(1, std::min<int64_t>(n, std::min(cus, kMostShares)));
 }
 // A unit's lead, measured in whole prompts of 500 to 700 rows at 128 heads, where a share has up to fifty: 4, 8, 12 tiles 356, 287, 287 us; where shares are smaller than
@@ -821,8 +836,8 @@ ag_status run(const AttnArgs& a, int64_t units, int shares, int lead, hipStream_
     ag_status e = allow_dynamic_lds((const void*)latent_kernel<L, R, kSplit, kDecode>, kLds, told);
     if (e) return e;
     prof_before(st);
-    hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, least_tiles(128 / kSplit), lead);
-    if (shares > 1) {
+    hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, least_tiles(128 / kSplit), lead, uncut_tiles(least_tiles(128 / kSplit)));
+    if (shares > 1 && (a.max_ctx - 1) / kTokens >= uncut_tiles(least_tiles(128 / kSplit))) {
         constexpr int kCols = 128 / kSplit, kSlices = kCols / 8 * (L / 32);
         const int64_t cuts = std::min<int64_t>(shares - 1, units);
         // four channels a lane where the cut units have few columns between them, sixteen otherwise
@@ -851,7 +866,7 @@ size_t attn_workspace(bool decode, int batch, int total, int heads, int lat, int
     size_t most = 0;
     for (int cols : {32, 64, 128}) {
         if (cols > columns((int64_t)total * heads)) break;             // (no session has more columns than all rows)
-        const Cut cut(cols, heads, 0);
+        const Cut cut(cols, heads);
         const int64_t units = units_of(decode, batch, total, cut);
         // sums of costs: 32 bits of tiles for decode, 64 of keys otherwise
         if ((double)units * (double)(tiles + kMostLead) >= (decode ? 2147483648.0 : 1.0e16)) return 0;
@@ -864,7 +879,7 @@ ag_status launch_attn(const AttnArgs& a, hipStream_t st)
 {
     const bool decode = a.ctx_lens != nullptr;
     const int cols = columns(decode ? a.heads : (int64_t)a.max_new * a.heads);
-    const Cut cut(cols, a.heads, 0);
+    const Cut cut(cols, a.heads);
     const int64_t units = units_of(decode, a.batch, a.total, cut);
     const int64_t tiles = ((int64_t)a.max_ctx + kTokens - 1) / kTokens;
     const int shares = shares_of(units, tiles, cols, stream_cus(st)), lead = lead_of(units, tiles, shares);
