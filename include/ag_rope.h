@@ -61,6 +61,7 @@ AG_API ag_status ag_rope_rows(const ag_rope* rope, int32_t dtype, const void* x,
  * ag_kv_append with the rotation on the way: keys go into their pages rotated, values as they are; and the same tokens' queries are rotated from q
  * into q_out in the same launch (q_out may be q; both NULL with num_q_heads = 0: no queries).  k_new is left as it was.  The pools and q_out hold
  * exactly what ag_rope_rows of k_new and q, and ag_kv_append of the rotated keys, would have put there.
+ * (Over an 8-bit cache: ag_rope_rows, then ag_kv_append_q8 of ag_q8.h.)
  * page_size 16 or more (AG_ERR_UNSUPPORTED below); rot_dim at most head_dim; num_q_heads a multiple of num_kv_heads; all pointers 16-byte aligned.
  */
 AG_API ag_status ag_kv_append_rope(const ag_kv_cache* cache, const ag_rope* rope,

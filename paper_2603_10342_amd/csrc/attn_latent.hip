@@ -7,7 +7,8 @@
 //     S^T (32 tokens x 32 columns) = rows . Q^T     O^T (L channels x 32 columns) += rows^T . P^T         on 32x32x16 bf16 MFMA
 // Q^T stays in registers, O^T in fp32 accumulators: of 512 channels and 128 columns together 80 % of a CU's registers, so that one workgroup of four waves is
 // all a CU holds and latency is hidden by order alone: the tile after the next is on its way, and the softmax of a tile runs beside the value product of the one
-// before.  With 64 or 32 columns, waves share columns and divide the channels of O; each takes the scores again, which memory's pace leaves time for.
+// before.  With 64 or 32 columns, waves share columns and divide the channels of O; each takes the scores again, which memory's pace leaves time for.  The matrix units
+// run at the chip's power limit: on random numbers a loop of nothing but these products reaches 1630 TFLOP/s.
 //
 // One tile in LDS feeds both products: scores read it along a row (16 bytes a lane), values across rows, by transposing reads.  Tiles come in by direct
 // global-to-LDS loads.
@@ -17,7 +18,6 @@
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
-#include <utility>
 
 #include "latent_internal.h"
 #include "lds_dma.h"
@@ -224,7 +224,8 @@ constexpr int kAhead = 4;               // operand reads run this many products 
 // The products are written in assembly because the scores' accumulators have to be vector registers and O's accumulation registers: the compiler gives all matrix
 // instructions of a kernel the same kind, and O^T fills that.  What the compiler keeps for its own matrix instructions is kept here by hand: two states between a vector
 // instruction that may have moved an operand and the product; none between products into one accumulator; and nothing of a result is read before
-// products_end(), 20 states after the last product (18 are asked for behind the longest there is).  Operands come by the compiler's loads, whose arrival it waits for.
+// products_end(), 20 states after the last product (its 16 passes and four).  Operands come by the compiler's loads, whose arrival it waits for.
+// tests/test_latent_asm.py looks for all of that in the code.
 __device__ __forceinline__ void score_product_first(f32x16& s, const bf16x8& a, const bf16x8& b)
 {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
@@ -485,6 +486,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
                 request_all();
                 request_all();
             };
+
             // ---- the queries, as B operands: column n, channels i * 16 + hi * 8 .. + 7 ----
             bf16x8 qf[Rw::kSteps];
             request_first();
@@ -515,6 +517,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
                 for (int i = 0; i < Rw::kSteps; ++i) qf[i] = read_along(kb[i & 3] + (i >> 2) * 1024);
                 __builtin_amdgcn_s_waitcnt(0xC07F);         // lgkmcnt(0): they are read before the next barrier lets a request into their stages
             }
+
             // m is a reference that every weight of the column is taken under, the largest score of its first tile: weights may come out far above one, and only if they
             // leave what kMostWeight allows for (or nothing came out at all) the piece is done again, under the largest score of all its tiles.  O never has to be rescaled.
             float m = -INFINITY, lsum;
@@ -532,34 +535,33 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
                 AG_WAIT_VMCNT(Rw::kBlocks);
                 barrier();                       // `now` is there, and every wave has taken the values of the tile two before
                 // A weight of zero does not hide a NaN.  Rows that only some of the columns see are looked through, their scores being taken: what is not
-                                // finite in them becomes zero for the value product, and goes to the columns that see it afterwards.
-                                constexpr bool kValues = decltype(values)::value;
+                // finite in them becomes zero for the value product, and goes to the columns that see it afterwards.
+                constexpr bool kValues = decltype(values)::value;
                 bool bad = false;
                 if (kValues && split && before >= shown) {
-                    const int tv = before, seen = qmin + 1 - tv * kTokens;         // tokens below `seen` are seen by all columns
-                    const int unseen = max(seen, 0);
-                                    unsigned char* const tile = lds + st_before;
-                                    bool mine = false;
-                                    for (int x = tid; x < (kTokens - unseen) * (L / 8); x += 256) {
-                                        const int tok = unseen + x / (L / 8), c = x % (L / 8);
-                                        u32x4* const at = reinterpret_cast<u32x4*>(tile + (tok >> 3) * (8 * kRB) + (c >> 3) * 1024 + (tok & 7) * 128 + ((c & 7) ^ turn_of(tok)) * 16);
-                                        u32x4 v = *at;
-                                        uint32_t any = 0;
-                #pragma unroll
-                                        for (int j = 0; j < 4; ++j) {
-                                            const uint32_t high = ((v[j] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;       // the halves whose exponent is all ones
-                                            any |= high;
-                                            v[j] &= ~((high << 1) - (high >> 15));
-                                        }
-                                        if (any) {
-                                            *at = v;
-                                            mine = true;
-                                        }
-                                    }
-                                    if (mine) *s_bad = 1;
-                                    __syncthreads();
-                                    bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
-                                }
+                    const int unseen = max(qmin + 1 - before * kTokens, 0);        // the first token that not all columns see
+                    unsigned char* const tile = lds + st_before;
+                    bool mine = false;
+                    for (int x = tid; x < (kTokens - unseen) * (L / 8); x += 256) {
+                        const int tok = unseen + x / (L / 8), c = x % (L / 8);
+                        u32x4* const at = reinterpret_cast<u32x4*>(tile + (tok >> 3) * (8 * kRB) + (c >> 3) * 1024 + (tok & 7) * 128 + ((c & 7) ^ turn_of(tok)) * 16);
+                        u32x4 v = *at;
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t high = ((v[j] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;       // the halves whose exponent is all ones
+                            any |= high;
+                            v[j] &= ~((high << 1) - (high >> 15));
+                        }
+                        if (any) {
+                            *at = v;
+                            mine = true;
+                        }
+                    }
+                    if (mine) *s_bad = 1;
+                    __syncthreads();
+                    bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
+                }
                 auto between = [&](int j) {
                     if (j < kParts) plan(j);
 #pragma unroll
@@ -602,7 +604,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
             for (int attempt = 0;; ++attempt) {
                 f32x16 s;
                 float sum;
-                if (attempt > 0) {
+                if (attempt > 0) {                   // the largest scores first
                     request_first();
                     float most = -INFINITY;
 #pragma unroll 1
@@ -612,8 +614,8 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
                     }
                     most = fmaxf(most, __shfl_xor(most, 32)) * sl2;               // (scale > 0: maximum and scaling commute)
                     if (wrong) m = most == -INFINITY ? 0.f : most;
+                    request_first();
                 }
-                if (attempt > 0) request_first();
                 iter(yes, no, sum, s);
                 if (attempt == 0) {
                     m = largest(s);
@@ -634,6 +636,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
                     wrong |= !(sum <= kMostWeight);
                 }
                 iter(no, yes, sum, s);
+                AG_WAIT_VMCNT(0);                // the requests past the end write to LDS too: before rows of O do, and before the workgroup's LDS is another's
                 done += count;
                 products_end();
                 lsum += __shfl_xor(lsum, 32);
@@ -650,8 +653,8 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
             if (lsum == 0.f) m = -INFINITY;
 
             if (from == 0 && to == tiles) {
-                // rows that are whole in LDS, 16-byte pieces in a place that depends on the row (8-byte stores of the accumulators themselves, 32 rows an
-                // instruction, took 100 us for every unit of the 256 CUs)
+                // by way of LDS, 16-byte pieces in a place that depends on the row, so that whole rows are stored (8-byte stores of the accumulators themselves, 32 rows an
+                // instruction: four prompts of 500 to 700 rows at 128 heads 1201 -> 947 us)
                 constexpr int kPieces = kCb * 4, kMask = kPieces < 8 ? kPieces - 1 : 7;      // of a row
                 barrier();                       // the last tiles' values have been taken
                 const float inv = 1.0f / lsum;
