@@ -1,7 +1,8 @@
 // Append to the latent cache (include/ag_latent.h): latent channels copied, rotary ones rotated on the way, a contiguous row of the pool a token.
 //
 // Bound by HBM, 2 T (L + R) 2 bytes, or for a decode step's few rows by three dependent memory round trips: lengths, page, store.  A wave takes kTok consecutive
-// tokens: their rows are requested before their sessions are looked up.  A lane holds 16 bytes of the latent part and one rotary pair.
+// tokens: their rows are requested before their sessions are looked up, and its lanes are dealt to all their 16-byte pieces, then to all their rotary pairs, so that
+// narrow rows fill a wave too (195000 rows of 128 + 64 channels, a token's row at a time 87 us).
 #include "find_session.h"
 #include "latent_internal.h"
 
@@ -12,57 +13,92 @@ namespace {
 using rope::f32x2;
 using rope::u32x4;
 
-template <int kTok>
+// kPieces: 16-byte pieces of a row's latent part; kPairs: its rotary pairs
+template <int kTok, int kPieces, int kPairs>
 __global__ __launch_bounds__(256) void append_latent_kernel(AppendArgs x)
 {
+    constexpr int kCopies = (kTok * kPieces + 63) / 64, kTurns = (kTok * kPairs + 63) / 64, kRow = row_of(kPieces * 8, kPairs * 2);
     const int lane = threadIdx.x & 63, t0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kTok;
     if (t0 >= x.total) return;
-    const int row = row_of(x.c.lat, x.c.rd), half = x.c.rd / 2;
-    const int ca = x.pairs ? 2 * lane : lane, cb = x.pairs ? 2 * lane + 1 : lane + half;          // the lane's pair
-    u32x4 lat[kTok];
-    __bf16 a[kTok], b[kTok];
+    const int most = min(kTok, x.total - t0);                          // tokens of this wave
+    u32x4 lat[kCopies];
+    __bf16 a[kTurns], b[kTurns];
+    auto first = [&](int pair) { return x.pairs ? 2 * pair : pair; };
+    auto second = [&](int pair) { return x.pairs ? 2 * pair + 1 : pair + kPairs; };
 #pragma unroll
-    for (int j = 0; j < kTok; ++j) {
-        const int64_t t = min(t0 + j, x.total - 1);
-        if (lane * 8 < x.c.lat) lat[j] = *reinterpret_cast<const u32x4*>((const __bf16*)x.lat + t * x.lat_stride + lane * 8);
-        if (lane < half) {
-            a[j] = ((const __bf16*)x.rot)[t * x.rot_stride + ca];
-            b[j] = ((const __bf16*)x.rot)[t * x.rot_stride + cb];
+    for (int i = 0; i < kCopies; ++i) {
+        const int at = i * 64 + lane, tok = at / kPieces;
+        if (tok < most) lat[i] = *reinterpret_cast<const u32x4*>((const __bf16*)x.lat + (int64_t)(t0 + tok) * x.lat_stride + at % kPieces * 8);
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int at = i * 64 + lane, tok = at / kPairs, pair = at % kPairs;
+        if (tok < most) {
+            const __bf16* const row = (const __bf16*)x.rot + (int64_t)(t0 + tok) * x.rot_stride;
+            a[i] = row[first(pair)];
+            b[i] = row[second(pair)];
         }
     }
+    int pos[kTok];                                                     // uniform, like the rows
+    int64_t row[kTok];
     Session f = {0, 0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < kTok; ++j) {
         const int t = t0 + j;
-        if (t >= x.total) break;
-        if (j == 0 || t >= f.row0 + f.new_len) f = find_session(x.new_lens, x.prefix_lens, x.cu_new, x.batch, t, [](int, int cu) { return cu; });
-        if (t - f.row0 >= f.new_len) break;                            // behind the last session: nobody's, like all that follow
-        const int pos = f.prefix + (t - f.row0);
-        const int64_t page = x.bt[(int64_t)f.s * x.max_pages + (pos >> x.c.ps_shift)];
-        __bf16* const dst = (__bf16*)x.c.pool + (page * x.c.ps + (pos & (x.c.ps - 1))) * row;
-        if (lane * 8 < x.c.lat) *reinterpret_cast<u32x4*>(dst + lane * 8) = lat[j];
-        if (lane < half) {
-            __bf16 ra = a[j], rb = b[j];
-            if (x.r.turns) {
-                float u = (float)ra, v = (float)rb;
-                rope::turn(u, v, rope::cos_sin(pos, x.r, lane));
-                ra = (__bf16)u;
-                rb = (__bf16)v;
+        pos[j] = -1;
+        row[j] = 0;
+        if (j < most) {
+            if (j == 0 || t >= f.row0 + f.new_len) f = find_session(x.new_lens, x.prefix_lens, x.cu_new, x.batch, t, [](int, int cu) { return cu; });
+            if (t - f.row0 < f.new_len) {                              // (otherwise behind the last session: nobody's)
+                pos[j] = f.prefix + (t - f.row0);
+                row[j] = (int64_t)x.bt[(int64_t)f.s * x.max_pages + (pos[j] >> x.c.ps_shift)] * x.c.ps + (pos[j] & (x.c.ps - 1));
             }
-            dst[x.c.lat + ca] = ra;
-            dst[x.c.lat + cb] = rb;
         }
     }
+    auto pick = [&](const auto& of, int tok) {
+        auto r = of[0];
+#pragma unroll
+        for (int j = 1; j < kTok; ++j) r = tok == j ? of[j] : r;
+        return r;
+    };
+    __bf16* const pool = (__bf16*)x.c.pool;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+        const int at = i * 64 + lane, tok = at / kPieces;
+        if (tok < most && pick(pos, tok) >= 0) *reinterpret_cast<u32x4*>(pool + pick(row, tok) * kRow + at % kPieces * 8) = lat[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int at = i * 64 + lane, tok = at / kPairs, pair = at % kPairs, p = pick(pos, tok);
+        if (tok >= most || p < 0) continue;
+        if (x.r.turns) {
+            float u = (float)a[i], v = (float)b[i];
+            rope::turn(u, v, rope::cos_sin(p, x.r, pair));
+            a[i] = (__bf16)u;
+            b[i] = (__bf16)v;
+        }
+        __bf16* const dst = pool + pick(row, tok) * kRow + kPieces * 8;
+        dst[first(pair)] = a[i];
+        dst[second(pair)] = b[i];
+    }
 }
+
+template <int kPieces, int kPairs>
+ag_status run(const AppendArgs& a, hipStream_t st)
+{
+    // One token a wave while the chip holds them all at once
+    if (a.total <= 4096) hipLaunchKernelGGL((append_latent_kernel<1, kPieces, kPairs>), dim3((a.total + 3) / 4), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((append_latent_kernel<4, kPieces, kPairs>), dim3((a.total + 15) / 16), dim3(256), 0, st, a);
+    return hip_check(hipGetLastError(), "append launch");
+}
+template <int kPieces>
+ag_status run(const AppendArgs& a, hipStream_t st) { return a.c.rd == 64 ? run<kPieces, 32>(a, st) : run<kPieces, 16>(a, st); }
 
 }  // namespace
 
 ag_status launch_append(const AppendArgs& a, hipStream_t st)
 {
-    // One token a wave while the chip holds them all at once
-    if (a.total <= 4096) hipLaunchKernelGGL(append_latent_kernel<1>, dim3((a.total + 3) / 4), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(append_latent_kernel<4>, dim3((a.total + 15) / 16), dim3(256), 0, st, a);
-    return hip_check(hipGetLastError(), "append launch");
+    return a.c.lat == 512 ? run<64>(a, st) : a.c.lat == 256 ? run<32>(a, st) : run<16>(a, st);
 }
 
 }  // namespace latent
