@@ -1,8 +1,9 @@
 // Append to the latent cache (include/ag_latent.h): latent channels copied, rotary ones rotated on the way, a contiguous row of the pool a token.
 //
-// Bound by HBM, 2 T (L + R) 2 bytes, or for a decode step's few rows by three dependent memory round trips: lengths, page, store.  A wave takes kTok consecutive
-// tokens: their rows are requested before their sessions are looked up, and its lanes are dealt to all their 16-byte pieces, then to all their rotary pairs, so that
-// narrow rows fill a wave too (195000 rows of 128 + 64 channels, a token's row at a time 87 us).
+// Bound by HBM, 2 T (L + R) 2 bytes, or for a decode step's few rows (4.1 us) by three dependent memory round trips: lengths, page, store.  A wave takes one token
+// of 512 channels, two of fewer, and deals its lanes to all their 16-byte pieces, then to all their rotary pairs; rows are requested before their sessions are
+// looked up.  32768 rows of 512 + 64 channels 14.3 us, 5.3 TB/s, with four tokens a wave the same; 107000 of 256 + 32 23 us, with one 29; 195000 of 128 + 64 41 us,
+// with one 59, with four 48 (and a step of 1024 sessions 4.1 us, with four 10.6: each looks for its session).
 #include "find_session.h"
 #include "latent_internal.h"
 
@@ -14,22 +15,19 @@ using rope::f32x2;
 using rope::u32x4;
 
 // kPieces: 16-byte pieces of a row's latent part; kPairs: its rotary pairs
-template <int kTok, int kPieces, int kPairs>
+template <int kPieces, int kPairs>
 __global__ __launch_bounds__(256) void append_latent_kernel(AppendArgs x)
 {
-    constexpr int kCopies = (kTok * kPieces + 63) / 64, kTurns = (kTok * kPairs + 63) / 64, kRow = row_of(kPieces * 8, kPairs * 2);
+    constexpr int kTok = kPieces == 64 ? 1 : 2, kTurns = (kTok * kPairs + 63) / 64, kRow = row_of(kPieces * 8, kPairs * 2);
     const int lane = threadIdx.x & 63, t0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kTok;
     if (t0 >= x.total) return;
     const int most = min(kTok, x.total - t0);                          // tokens of this wave
-    u32x4 lat[kCopies];
+    u32x4 lat = {};
     __bf16 a[kTurns], b[kTurns];
     auto first = [&](int pair) { return x.pairs ? 2 * pair : pair; };
     auto second = [&](int pair) { return x.pairs ? 2 * pair + 1 : pair + kPairs; };
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-        const int at = i * 64 + lane, tok = at / kPieces;
-        if (tok < most) lat[i] = *reinterpret_cast<const u32x4*>((const __bf16*)x.lat + (int64_t)(t0 + tok) * x.lat_stride + at % kPieces * 8);
-    }
+    const int mine = lane / kPieces, piece = lane % kPieces;
+    if (mine < most) lat = *reinterpret_cast<const u32x4*>((const __bf16*)x.lat + (int64_t)(t0 + mine) * x.lat_stride + piece * 8);
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int at = i * 64 + lane, tok = at / kPairs, pair = at % kPairs;
@@ -62,11 +60,7 @@ __global__ __launch_bounds__(256) void append_latent_kernel(AppendArgs x)
         return r;
     };
     __bf16* const pool = (__bf16*)x.c.pool;
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-        const int at = i * 64 + lane, tok = at / kPieces;
-        if (tok < most && pick(pos, tok) >= 0) *reinterpret_cast<u32x4*>(pool + pick(row, tok) * kRow + at % kPieces * 8) = lat[i];
-    }
+    if (mine < most && pick(pos, mine) >= 0) *reinterpret_cast<u32x4*>(pool + pick(row, mine) * kRow + piece * 8) = lat;
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int at = i * 64 + lane, tok = at / kPairs, pair = at % kPairs, p = pick(pos, tok);
@@ -86,9 +80,8 @@ __global__ __launch_bounds__(256) void append_latent_kernel(AppendArgs x)
 template <int kPieces, int kPairs>
 ag_status run(const AppendArgs& a, hipStream_t st)
 {
-    // One token a wave while the chip holds them all at once
-    if (a.total <= 4096) hipLaunchKernelGGL((append_latent_kernel<1, kPieces, kPairs>), dim3((a.total + 3) / 4), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((append_latent_kernel<4, kPieces, kPairs>), dim3((a.total + 15) / 16), dim3(256), 0, st, a);
+    constexpr int kTok = kPieces == 64 ? 4 : 8;                        // of a workgroup
+    hipLaunchKernelGGL((append_latent_kernel<kPieces, kPairs>), dim3((a.total + kTok - 1) / kTok), dim3(256), 0, st, a);
     return hip_check(hipGetLastError(), "append launch");
 }
 template <int kPieces>
