@@ -827,7 +827,7 @@ int columns(int64_t most) { return most <= 32 ? 32 : most <= 64 ? 64 : 128; }
 int shares_of(int64_t units, int64_t tiles, int cols, int cus)
 {
     const int64_t n = std::max<int64_t>(units, (units * tiles + least_tiles(cols) - 1) / least_tiles(cols));
-    return (int)std::max<int64_t>(1, std::min<int64_t>(n, std::min(cus, kMostShares)));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(n, cus));
 }
 // A unit's lead, measured in whole prompts of 500 to 700 rows at 128 heads, where a share has up to fifty: 4, 8, 12 tiles 356, 287, 287 us; where shares are smaller than
 // that, less, so that none is left with a lead alone.
@@ -890,11 +890,18 @@ size_t attn_workspace(bool decode, int batch, int total, int heads, int lat, int
 ag_status launch_attn(const AttnArgs& a, hipStream_t st)
 {
     const bool decode = a.ctx_lens != nullptr;
-    const int cols = columns(decode ? a.heads : (int64_t)a.max_new * a.heads);
-    const Cut cut(cols, a.heads);
-    const int64_t units = units_of(decode, a.batch, a.total, cut);
     const int64_t tiles = ((int64_t)a.max_ctx + kTokens - 1) / kTokens;
-    const int shares = shares_of(units, tiles, cols, stream_cus(st)), lead = lead_of(units, tiles, shares);
+    const int cus = std::min(stream_cus(st), kMostShares);
+    int cols = columns(decode ? a.heads : (int64_t)a.max_new * a.heads), shares;
+    int64_t units;
+    // ... and fewer, down to 32, while CUs would go without a share: more units read the same rows, and more waves share a column's work.  Decode at 128 heads, us, in
+    // 128 / 64 / 32 columns: two sessions of 5000 tokens 33.4 / 27.9 / 25.1 (45, 178, 256 shares); 256 of 128, a share each, 32.7 / 39.0 / 53.7.
+    for (;; cols /= 2) {
+        units = units_of(decode, a.batch, a.total, Cut(cols, a.heads));
+        shares = shares_of(units, tiles, cols, cus);
+        if (cols == 32 || shares >= cus) break;
+    }
+    const int lead = lead_of(units, tiles, shares);
     if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, units, shares, lead, st) : run_columns<512, 32>(a, cols, units, shares, lead, st);
     if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, units, shares, lead, st) : run_columns<256, 32>(a, cols, units, shares, lead, st);
     return a.c.rd == 64 ? run_columns<128, 64>(a, cols, units, shares, lead, st) : run_columns<128, 32>(a, cols, units, shares, lead, st);
