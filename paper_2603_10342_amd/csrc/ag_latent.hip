@@ -95,7 +95,7 @@ ag_status ag_kv_append_latent(const ag_latent_cache* cache, const ag_rope* rope,
         if (s < 0 || s > most || s % 8) { set_error("strides must be multiples of 8 elements and not negative"); return AG_ERR_INVALID_ARG; }
     if (!latent::aligned(latent_new) || !latent::aligned(rope_new)) { set_error("latent_new and rope_new must be 16-byte aligned"); return AG_ERR_INVALID_ARG; }
     if (total_new == 0) return AG_OK;
-    if ((total_new + 15ll) / 16 > 0xFFFFFFFFll / 256) { set_error("total_new=%d: too many rows for one launch", total_new); return AG_ERR_INVALID_ARG; }
+    if ((total_new + 3ll) / 4 > 0xFFFFFFFFll / 256) { set_error("total_new=%d: too many rows for one launch", total_new); return AG_ERR_INVALID_ARG; }
     a.r = rope ? rope::spec_of(*rope) : rope::Spec{nullptr, a.c.rd / 2, 1.0f, false};
     a.pairs = rope && rope->layout == AG_ROPE_PAIRS;
     a.lat = latent_new; a.lat_stride = latent_stride; a.rot = rope_new; a.rot_stride = rope_stride;

@@ -72,3 +72,14 @@ def test_appends(tmp):
     assert step[0][0] == "append_rope_kernel<__bf16,false,false>" and prompt[0][0] == "append_rope_kernel<__bf16,false,true>" and f32[0][0] == "append_rope_kernel<float,true,false>"
     got = logs(tmp, *(dict(call="append", batch=8, new=n, lat=lat, rd=rd) for lat, rd, n in ((512, 64, 100), (256, 32, 100), (128, 64, 101))))
     assert got == [[["append_latent_kernel<64,32>", "200"]], [["append_latent_kernel<32,16>", "100"]], [["append_latent_kernel<16,32>", "101"]]]
+
+
+MOST = 0xFFFFFFFF // 256                       # workgroups of 256 threads that a launch holds
+
+
+@pytest.mark.parametrize("call,most", [(dict(call="rows", heads=32), 4 * MOST), (dict(call="append"), 4 * MOST), (dict(call="append", lat=128, rd=32), 4 * MOST),
+                                       (dict(call="append_rope", heads=32), 16 * (MOST - 2) + 15)])
+def test_what_one_launch_holds(tmp, call, most):
+    at, past = logs(tmp, *(dict(batch=1, max_ctx=16, total=n, **call) for n in (most, most + 1)))
+    assert len(at) == 1 and int(at[0][1]) <= MOST, at
+    assert past[0][0] == "refused" and past[0][1] == "-1", past
