@@ -604,6 +604,8 @@ def ag_kv_append_latent(cache: LatentCache, rope: Optional[Rope], latent_new, ro
     rp, rt = _rows(rope_new, 2)
     if latent_new.shape[1] != cache.latent_dim or rope_new.shape[1] != cache.rope_dim:
         raise ValueError("rows have the cache's latent_dim and rope_dim channels")
+    if total_new > min(latent_new.shape[0], rope_new.shape[0]):
+        raise ValueError("total_new exceeds the rows")
     c, r = cache.c_struct(), None if rope is None else rope.c_struct()
     _check(lib().ag_kv_append_latent(C.byref(c), None if r is None else C.byref(r), lp, lt, rp, rt, _i32(block_tables), block_tables.shape[1],
                                      _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0], total_new, _stream(stream)))

@@ -358,7 +358,7 @@ PyObject* kv_append_latent(PyObject*, PyObject* const* a, Py_ssize_t n)
         const int32_t *b = r.ints(a[4], &bt), *prefix = r.ints(a[5]), *len = r.ints(a[6], &lens), *cu = r.ints(a[7]);
         const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), total = r.number(a[8]);
         void* s = r.stream(a[9]);
-        if (r.plain && (lat->size(1) != c.latent_dim || rot->size(1) != c.rope_dim)) r.plain = false;
+        if (r.plain && (lat->size(1) != c.latent_dim || rot->size(1) != c.rope_dim || total > lat->size(0) || total > rot->size(0))) r.plain = false;
         return finish(r, [&] {
             return entries.kv_append_latent(&c, turned ? nullptr : &rope, lp, lat->stride(0), rp, rot->stride(0), b, pages, prefix, len, cu, batch, total, s);
         });

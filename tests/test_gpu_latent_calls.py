@@ -207,6 +207,23 @@ def test_both_ways_into_the_library(monkeypatch):
     assert all(same_bits(x, y) for x, y in zip(a, run()))
 
 
+def test_what_python_refuses_before_the_library(monkeypatch):
+    rope, _ = make_rope(64, "pairs")
+    cache = B.LatentCache(2, 16, 512, 64, DEV, fill=2.0)
+    x, bt, lens = torch.zeros(4, 576, dtype=torch.bfloat16, device=DEV), i32([[0, 1]]), (i32([0]), i32([4]), i32([0, 4]))
+    for _ in range(2):
+        for rows, what, error in ((x, 5, ValueError), (x.float(), 4, TypeError), (x.t().contiguous().t(), 4, ValueError), (x[:, 8:], 4, ValueError), (x.cpu(), 4, ValueError)):
+            with pytest.raises(error):
+                B.ag_kv_append_latent(cache, rope, rows[:, :512], rows[:, 512:], bt, *lens, what)
+        q = x.view(4, 1, 576)[..., 512:]
+        for rows, what, error in ((q, 5, ValueError), (q.half(), 4, TypeError), (q[:, 0], 4, ValueError)):
+            with pytest.raises(error):
+                B.ag_rope_rows(rope, rows, rows, *lens, what)
+        torch.cuda.synchronize()
+        assert bool((cache.pool == 2).all()) and bool((x == 0).all())
+        monkeypatch.setattr(B, "_native", B._NoCalls())
+
+
 # ---- batches drawn at random ----
 
 @pytest.mark.parametrize("seed", range(24))
