@@ -112,18 +112,19 @@ struct Share {
     __device__ __forceinline__ Share(const AttnArgs& a, const Cut& cut, int w, int shares, int least)
     {
         const int lane = threadIdx.x & 63;
-        Cost incl = 0;
-        int sessions = 0;
+        Cost incl = 0, units = 0;
         total = 0;
         for (int base = 0; base < a.batch; base += 64) {
-            const Cost c = base + lane < a.batch ? session_cost<kDecode>(lens_of<kDecode>(a, base + lane), cut) : (Cost)0;
-            sessions += __builtin_popcountll(__builtin_amdgcn_ballot_w64(c > 0));
-            incl = scan64(c);
+            const Lens x = base + lane < a.batch ? lens_of<kDecode>(a, base + lane) : Lens{0, 0, 0};
+            incl = scan64(session_cost<kDecode>(x, cut));
             total += from_lane(incl, 63);
+            if constexpr (kDecode) units += __builtin_popcountll(__builtin_amdgcn_ballot_w64(x.n > 0));
+            else units += from_lane(scan64((uint32_t)((x.n + cut.m - 1) / cut.m)), 63);
         }
-        // not less than `least` tiles, but for units that are smaller themselves (as far as the number of sessions tells)
+        // not less than `least` tiles, but for units that are smaller themselves (four prompts of 200 to 300 rows, 32 heads: 27.5 us, as long as only sessions were counted 38)
         constexpr Cost kT = Counting<kDecode>::kTile;
-        Cost floor = total / (Cost)max(sessions * cut.nh, 1);
+        units *= cut.nh;
+        Cost floor = total / (units > 0 ? units : 1);
         floor = floor < (Cost)least * kT ? floor : (Cost)least * kT;
         per = (total + shares - 1) / shares;
         per = ((per < floor ? floor : per) + kT - 1) / kT * kT;
@@ -831,8 +832,14 @@ int shares_of(int64_t units, int64_t tiles, int cols, int cus)
 }
 // A unit's lead, measured in whole prompts of 500 to 700 rows at 128 heads, where a share has up to fifty: 4, 8, 12 tiles 356, 287, 287 us; where shares are smaller than
 // that, less, so that none is left with a lead alone.
-constexpr int kMostLead = 8;
-int lead_of(int64_t units, int64_t tiles, int shares) { return (int)std::min<int64_t>(kMostLead, units * tiles / shares / 2); }
+// Where no unit is cut and a share need have one at most, a lead beside which their tiles do not count, so that none has two (20 rows behind 30 tokens, 32 heads: 10.4 us,
+// by their tiles 14.9).
+constexpr int kMostLead = 8, kOnlyLead = 1024;
+int lead_of(int64_t units, int64_t tiles, int shares, int cols)
+{
+    if (units <= shares && tiles <= uncut_tiles(least_tiles(cols))) return kOnlyLead;
+    return (int)std::min<int64_t>(kMostLead, units * tiles / shares / 2);
+}
 int64_t units_of(bool decode, int batch, int total, const Cut& cut)
 {
     return (decode ? (int64_t)batch : (int64_t)total / cut.m + batch) * cut.nh;
@@ -901,7 +908,7 @@ ag_status launch_attn(const AttnArgs& a, hipStream_t st)
         shares = shares_of(units, tiles, cols, cus);
         if (cols == 32 || shares >= cus) break;
     }
-    const int lead = lead_of(units, tiles, shares);
+    const int lead = lead_of(units, tiles, shares, cols);
     if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, units, shares, lead, st) : run_columns<512, 32>(a, cols, units, shares, lead, st);
     if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, units, shares, lead, st) : run_columns<256, 32>(a, cols, units, shares, lead, st);
     return a.c.rd == 64 ? run_columns<128, 64>(a, cols, units, shares, lead, st) : run_columns<128, 32>(a, cols, units, shares, lead, st);
