@@ -815,9 +815,15 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* 
 // Tiles of a share at least: what a piece writes and a merge reads back, the columns' O in fp32, is worth a few.  Decode, us, 2 / 4 / 8 tiles: one session of 1000 tokens,
 // 32 heads 13.3 / 15.1 / 18.9; two of 10500 together, 128 heads 38.2 / 35.1 / 32.0.
 constexpr int least_tiles(int cols) { return cols == 32 ? 2 : cols == 64 ? 4 : 8; }
-// A unit of so many tiles or fewer is not cut.  Decode, 128 heads, us, at 0 / 2 / 4 times `least`: 128 sessions of 100 to 300 tokens 56.7 / 45.8 / 47.6; 256 of 512
-// 58.4 / 55.5 / 55.4.
-constexpr int uncut_tiles(int least) { return 2 * least; }
+// A unit of so many tiles or fewer is not cut: two shares' least ones (four prompts of 500 to 700 rows, 128 heads: 281 us, with every unit cut 291).
+// Contexts of 512 tokens and less stay whole altogether where there are units for an eighth of the CUs, and nothing is merged: decode, us, cut / whole, 128 sessions of 100 to
+// 300 tokens, 128 heads 36 / 24; 64 of 200 to 400, 64 heads 26 / 20; 16 of 100 to 500, 128 heads 23 / 21; 60 rows behind 300, 100 heads 36 / 22; but 4 sessions of 200 to 400,
+// 32 heads 12 / 18.
+constexpr int kWholeTiles = 16;
+int uncut_tiles(int64_t units, int64_t tiles, int cols, int cus)
+{
+    return tiles <= kWholeTiles && 8 * units >= cus ? kWholeTiles : 2 * least_tiles(cols);
+}
 constexpr int kMergeMost = 1024;        // workgroups of a merge
 
 // As few columns as hold a session's: decode of 256 sessions of 1024 tokens, us, in 32 / 64 / 128 columns: 32 heads 66 / 73 / 93; 64 heads - / 77 / 91.
@@ -835,9 +841,9 @@ int shares_of(int64_t units, int64_t tiles, int cols, int cus)
 // Where no unit is cut and a share need have one at most, a lead beside which their tiles do not count, so that none has two (20 rows behind 30 tokens, 32 heads: 10.4 us,
 // by their tiles 14.9).
 constexpr int kMostLead = 8, kOnlyLead = 1024;
-int lead_of(int64_t units, int64_t tiles, int shares, int cols)
+int lead_of(int64_t units, int64_t tiles, int shares, int uncut)
 {
-    if (units <= shares && tiles <= uncut_tiles(least_tiles(cols))) return kOnlyLead;
+    if (units <= shares && tiles <= uncut) return kOnlyLead;
     return (int)std::min<int64_t>(kMostLead, units * tiles / shares / 2);
 }
 int64_t units_of(bool decode, int batch, int total, const Cut& cut)
@@ -847,15 +853,15 @@ int64_t units_of(bool decode, int batch, int total, const Cut& cut)
 size_t bytes_of(int shares, int cols, int lat) { return o_offset(2 * shares, cols) + (size_t)2 * shares * place_floats(cols, lat) * 4; }
 
 template <int L, int R, int kSplit, bool kDecode>
-ag_status run(const AttnArgs& a, int64_t units, int shares, int lead, hipStream_t st)
+ag_status run(const AttnArgs& a, int64_t units, int shares, int lead, int uncut, hipStream_t st)
 {
     static std::atomic<uint64_t> told{0};
     constexpr int kLds = kStages * Row<L, R>::kTile + 16;
     ag_status e = allow_dynamic_lds((const void*)latent_kernel<L, R, kSplit, kDecode>, kLds, told);
     if (e) return e;
     prof_before(st);
-    hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, least_tiles(128 / kSplit), lead, uncut_tiles(least_tiles(128 / kSplit)));
-    if (shares > 1 && (a.max_ctx - 1) / kTokens >= uncut_tiles(least_tiles(128 / kSplit))) {
+    hipLaunchKernelGGL((latent_kernel<L, R, kSplit, kDecode>), dim3(shares), dim3(256), kLds, st, a, least_tiles(128 / kSplit), lead, uncut);
+    if (shares > 1 && (a.max_ctx - 1) / kTokens >= uncut) {
         constexpr int kCols = 128 / kSplit, kSlices = kCols / 8 * (L / 32);
         const int64_t cuts = std::min<int64_t>(shares - 1, units);
         // four channels a lane where the cut units have few columns between them, sixteen otherwise: decode, us, both ways, four sessions of 16 heads 35.8 and 42.2, 64 of
@@ -867,14 +873,14 @@ ag_status run(const AttnArgs& a, int64_t units, int shares, int lead, hipStream_
     return hip_check(hipGetLastError(), "latent attention launch");
 }
 template <int L, int R>
-ag_status run_columns(const AttnArgs& a, int cols, int64_t units, int shares, int lead, hipStream_t st)
+ag_status run_columns(const AttnArgs& a, int cols, int64_t units, int shares, int lead, int uncut, hipStream_t st)
 {
     if (a.ctx_lens) {
-        if (cols == 32) return run<L, R, 4, true>(a, units, shares, lead, st);
-        return cols == 64 ? run<L, R, 2, true>(a, units, shares, lead, st) : run<L, R, 1, true>(a, units, shares, lead, st);
+        if (cols == 32) return run<L, R, 4, true>(a, units, shares, lead, uncut, st);
+        return cols == 64 ? run<L, R, 2, true>(a, units, shares, lead, uncut, st) : run<L, R, 1, true>(a, units, shares, lead, uncut, st);
     }
-    if (cols == 32) return run<L, R, 4, false>(a, units, shares, lead, st);
-    return cols == 64 ? run<L, R, 2, false>(a, units, shares, lead, st) : run<L, R, 1, false>(a, units, shares, lead, st);
+    if (cols == 32) return run<L, R, 4, false>(a, units, shares, lead, uncut, st);
+    return cols == 64 ? run<L, R, 2, false>(a, units, shares, lead, uncut, st) : run<L, R, 1, false>(a, units, shares, lead, uncut, st);
 }
 
 }  // namespace
@@ -908,10 +914,10 @@ ag_status launch_attn(const AttnArgs& a, hipStream_t st)
         shares = shares_of(units, tiles, cols, cus);
         if (cols == 32 || shares >= cus) break;
     }
-    const int lead = lead_of(units, tiles, shares, cols);
-    if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, units, shares, lead, st) : run_columns<512, 32>(a, cols, units, shares, lead, st);
-    if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, units, shares, lead, st) : run_columns<256, 32>(a, cols, units, shares, lead, st);
-    return a.c.rd == 64 ? run_columns<128, 64>(a, cols, units, shares, lead, st) : run_columns<128, 32>(a, cols, units, shares, lead, st);
+    const int uncut = uncut_tiles(units, tiles, cols, cus), lead = lead_of(units, tiles, shares, uncut);
+    if (a.c.lat == 512) return a.c.rd == 64 ? run_columns<512, 64>(a, cols, units, shares, lead, uncut, st) : run_columns<512, 32>(a, cols, units, shares, lead, uncut, st);
+    if (a.c.lat == 256) return a.c.rd == 64 ? run_columns<256, 64>(a, cols, units, shares, lead, uncut, st) : run_columns<256, 32>(a, cols, units, shares, lead, uncut, st);
+    return a.c.rd == 64 ? run_columns<128, 64>(a, cols, units, shares, lead, uncut, st) : run_columns<128, 32>(a, cols, units, shares, lead, uncut, st);
 }
 
 }  // namespace latent

@@ -53,6 +53,14 @@ def test_merges(tmp):
     assert small[1][0] == "latent_merge_kernel<1>" and wide[1][0] == "latent_merge_kernel<4>"
 
 
+def test_short_contexts_stay_whole(tmp):
+    """... and launch no merge, where there are units for an eighth of the CUs."""
+    whole = [dict(batch=128, max_ctx=300), dict(batch=64, max_ctx=512, heads=32), dict(batch=16, max_ctx=500), dict(call="resume", batch=1, prefix=300, new=60, heads=100)]
+    cut = [dict(batch=4, max_ctx=400, heads=32), dict(batch=64, max_ctx=513, heads=32), dict(call="resume", batch=2, prefix=400, new=8, heads=16)]
+    got = logs(tmp, *({"call": "decode", **b} for b in whole + cut))
+    assert [len(l) for l in got] == [1] * len(whole) + [2] * len(cut), got
+
+
 @pytest.mark.parametrize("heads", G.HEADS)
 def test_the_gpu_tests_of_whole_columns_reach_them(tmp, heads):
     decode, resume = logs(tmp, dict(call="decode", batch=len(G.CTX), max_ctx=G.LOOSE, heads=heads),
