@@ -1,0 +1,28 @@
+"""What gfx950 asks of direct global-to-LDS loads, and the compiler does not see to inside an asm statement (csrc/lds_dma.h): a state between a scalar write of M0 and the
+load that takes its LDS address from there.  Looked for in the machine code of the built library, along every path."""
+import pytest
+
+from device_code import OBJDUMP, code_objects, functions
+
+pytestmark = pytest.mark.skipif(OBJDUMP is None, reason="needs llvm-objdump")
+
+
+@pytest.fixture(scope="module")
+def direct(tmp_path_factory):
+    """Functions with direct loads, and where those are."""
+    path, found = str(tmp_path_factory.mktemp("code") / "image.o"), []
+    for image in code_objects():
+        for f in functions(image, path):
+            loads = [i for i, c in enumerate(f.code) if c.startswith("global_load_lds") or (c.startswith("buffer_load") and c.endswith(" lds"))]
+            if loads:
+                found.append((f, loads))
+    assert len(found) >= 12 + 4 and sum(len(loads) for _, loads in found) > 1000
+    return found
+
+
+def test_a_state_between_m0_and_the_load(direct):
+    wrong = []
+    for f, loads in direct:
+        for i in loads:
+            wrong += [(f.name, f.code[j], f.code[i]) for j in f.near(i, 1, forward=False) if f.operands(j) and f.operands(j)[0] == "m0"]
+    assert not wrong, (len(wrong), wrong[:2])
