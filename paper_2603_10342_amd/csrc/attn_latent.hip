@@ -228,9 +228,9 @@ constexpr int kAhead = 4;               // operand reads run this many products 
 
 // The products are written in assembly because the scores' accumulators have to be vector registers and O's accumulation registers: the compiler gives all matrix
 // instructions of a kernel the same kind, and O^T fills that.  What the compiler keeps for its own matrix instructions is kept here by hand: two states between a vector
-// instruction that may have moved an operand and the product; none between products into one accumulator; and nothing of a result is read before
+// instruction that may have moved an operand or an accumulator and the product; none between products into one accumulator; and nothing of a result is read before
 // products_end(), 20 states after the last product (its 16 passes and four).  Operands come by the compiler's loads, whose arrival it waits for.
-// tests/test_latent_asm.py looks for all of that in the code.
+// tests/test_latent_asm.py and tests/test_latent_paths.py look for all of that in the code.
 __device__ __forceinline__ void score_product_first(f32x16& s, const bf16x8& a, const bf16x8& b)
 {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
@@ -242,6 +242,11 @@ __device__ __forceinline__ void score_product(f32x16& s, const bf16x8& a, const 
 __device__ __forceinline__ void value_product(f32x16& o, const bf16x8& a, const bf16x8& b)
 {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(a), "v"(b));
+}
+// ... where the compiler may just have moved the accumulator, as it does behind the loop
+__device__ __forceinline__ void value_product_moved(f32x16& o, const bf16x8& a, const bf16x8& b)
+{
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void products_end() { asm volatile("s_nop 15\n\ts_nop 3"); }
 __device__ __forceinline__ void products_end(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
@@ -338,7 +343,8 @@ __device__ __forceinline__ void step(unsigned k0, unsigned v0, const bf16x8 (&qf
 #pragma unroll
         for (int j = 0; j < kNv; ++j) {
             if (kNs + j + kAhead < kN) opnd[(kNs + j + kAhead) % (kAhead + 1)] = operand(kNs + j + kAhead);
-            value_product(o[j % kCb], opnd[(kNs + j) % (kAhead + 1)], p_prev.k[j / kCb]);
+            if (!kScores && j < kCb) value_product_moved(o[j], opnd[j % (kAhead + 1)], p_prev.k[0]);
+            else value_product(o[j % kCb], opnd[(kNs + j) % (kAhead + 1)], p_prev.k[j / kCb]);
             if constexpr (kScores) {
                 if (j < kWait) asm volatile("s_nop 6");
                 if (j + 1 == kWait) {
