@@ -615,13 +615,33 @@ def ag_attn_decode_latent_workspace_bytes(batch: int, num_q_heads: int, latent_d
     return int(lib().ag_attn_decode_latent_workspace_bytes(batch, num_q_heads, latent_dim, max_ctx))
 
 
+def _whole_rows(t: torch.Tensor, dtype: torch.dtype, rows: int, numbers: int, what: str):
+    """Device pointer of `rows` rows of so many numbers each, or more rows."""
+    p = _ptr(t)
+    if t is None:                                                      # (the library says so)
+        return p
+    if t.dtype != dtype:
+        raise TypeError(f"{what} is {str(dtype)[6:]}")
+    if t.dim() < 2 or t.shape[0] < rows or t.numel() != t.shape[0] * numbers:
+        raise ValueError(f"{what} has {rows} rows or more of {numbers} numbers each")
+    return p
+
+
+def _latent_rows(cache: LatentCache, q, out, rows: int, heads: int):
+    """Device pointers of the queries, latent_dim + rope_dim channels a head, and of the outputs, latent_dim."""
+    return (_whole_rows(q, torch.bfloat16, rows, heads * (cache.latent_dim + cache.rope_dim), "q"),
+            _whole_rows(out, torch.bfloat16, rows, heads * cache.latent_dim, "out"))
+
+
 def ag_attn_decode_latent(cache: LatentCache, q, out, block_tables, ctx_lens, max_ctx: int, num_q_heads: int, scale: float, workspace: torch.Tensor,
                           stream=None):
+    """q [B][num_q_heads][latent_dim + rope_dim] and out [B][num_q_heads][latent_dim], bfloat16."""
     st = (_native or _calls()).attn_decode_latent(cache, q, out, block_tables, ctx_lens, max_ctx, num_q_heads, scale, workspace, stream)
     if st is not None:
         return _check(st)
     c = cache.c_struct()
-    _check(lib().ag_attn_decode_latent(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1], _i32(ctx_lens), ctx_lens.shape[0],
+    qp, op = _latent_rows(cache, q, out, ctx_lens.shape[0], num_q_heads)
+    _check(lib().ag_attn_decode_latent(C.byref(c), qp, op, _i32(block_tables), block_tables.shape[1], _i32(ctx_lens), ctx_lens.shape[0],
                                        max_ctx, num_q_heads, scale, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
@@ -631,12 +651,14 @@ def ag_attn_resume_latent_workspace_bytes(batch: int, total_new: int, num_q_head
 
 def ag_attn_resume_latent(cache: LatentCache, q, out, block_tables, prefix_lens, new_lens, cu_new, total_new: int, max_new: int, max_ctx: int,
                           num_q_heads: int, scale: float, workspace: torch.Tensor, stream=None):
+    """q [T][num_q_heads][latent_dim + rope_dim] and out [T][num_q_heads][latent_dim], bfloat16, of total_new rows or more."""
     st = (_native or _calls()).attn_resume_latent(cache, q, out, block_tables, prefix_lens, new_lens, cu_new, total_new, max_new, max_ctx, num_q_heads,
                                                   scale, workspace, stream)
     if st is not None:
         return _check(st)
     c = cache.c_struct()
-    _check(lib().ag_attn_resume_latent(C.byref(c), _ptr(q), _ptr(out), _i32(block_tables), block_tables.shape[1], _i32(prefix_lens), _i32(new_lens),
+    qp, op = _latent_rows(cache, q, out, total_new, num_q_heads)
+    _check(lib().ag_attn_resume_latent(C.byref(c), qp, op, _i32(block_tables), block_tables.shape[1], _i32(prefix_lens), _i32(new_lens),
                                        _i32(cu_new), new_lens.shape[0], total_new, max_new, max_ctx, num_q_heads, scale, _ptr(workspace),
                                        workspace.numel() * workspace.element_size(), _stream(stream)))
 

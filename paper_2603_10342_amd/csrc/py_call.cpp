@@ -145,6 +145,20 @@ struct Reader {
         *out = t;
         return t->data_ptr();
     }
+    // `rows` rows or more of so many numbers each
+    void whole_rows(const at::Tensor* t, at::ScalarType type, int32_t rows, int64_t numbers)
+    {
+        if (plain && (t->scalar_type() != type || t->dim() < 2 || t->size(0) < rows || t->numel() != t->size(0) * numbers)) plain = false;
+    }
+    // queries and outputs of attention over a latent cache have two widths
+    template <class Cache>
+    void attention_rows(const Cache& c, const at::Tensor* q, const at::Tensor* out, int32_t rows, int32_t heads)
+    {
+        if constexpr (std::is_same_v<Cache, ag_latent_cache>) {
+            whole_rows(q, at::kBFloat16, rows, (int64_t)heads * (c.latent_dim + c.rope_dim));
+            whole_rows(out, at::kBFloat16, rows, (int64_t)heads * c.latent_dim);
+        }
+    }
     template <class Cache>
     void pools(PyObject* o, PyObject* type, Cache& c)
     {
@@ -246,12 +260,13 @@ PyObject* attn_resume(PyObject*, PyObject* const* a, Py_ssize_t n)
     return guarded(n, kMerged ? 14 : 13, [&] {
         Reader r;
         Cache c;
-        const at::Tensor *bt, *lens, *ws = nullptr;
+        const at::Tensor *q_rows = nullptr, *out_rows = nullptr, *bt, *lens, *ws = nullptr;
         r.cache(a[0], c);
-        void *q = r.device(a[1]), *out = r.device(a[2]);
+        void *q = r.device(a[1], &q_rows), *out = r.device(a[2], &out_rows);
         const int32_t *b = r.ints(a[3], &bt), *prefix = r.ints(a[4]), *len = r.ints(a[5], &lens), *cu = r.ints(a[6]);
         const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), total = r.number(a[7]), max_new = r.number(a[8]),
                       max_ctx = r.number(a[9]), hq = r.number(a[10]);
+        r.attention_rows(c, q_rows, out_rows, total, hq);
         const float scale = r.real(a[11]);
         void* w = kMerged ? r.device(a[12], &ws) : nullptr;
         const size_t bytes = ws && r.plain ? (size_t)ws->numel() * ws->element_size() : 0;
@@ -271,11 +286,12 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n)
     return guarded(n, kStatic ? 9 : 10, [&] {
         Reader r;
         Cache c;
-        const at::Tensor *bt, *lens, *ws = nullptr;
+        const at::Tensor *q_rows = nullptr, *out_rows = nullptr, *bt, *lens, *ws = nullptr;
         r.cache(a[0], c);
-        void *q = r.device(a[1]), *out = r.device(a[2]);
+        void *q = r.device(a[1], &q_rows), *out = r.device(a[2], &out_rows);
         const int32_t *b = r.ints(a[3], &bt), *ctx = r.ints(a[4], &lens);
         const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), max_ctx = r.number(a[5]), hq = r.number(a[6]);
+        r.attention_rows(c, q_rows, out_rows, batch, hq);
         const float scale = r.real(a[7]);
         void* w = kStatic ? nullptr : r.device(a[8], &ws);
         const size_t bytes = ws && r.plain ? (size_t)ws->numel() * ws->element_size() : 0;
