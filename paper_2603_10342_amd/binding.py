@@ -562,14 +562,28 @@ def ag_rope_rows(rope: Rope, x, y, prefix_lens, new_lens, cu_new, total_new: int
                               _i32(cu_new), new_lens.shape[0], total_new, int(transposed), _stream(stream)))
 
 
+def _whole_rows(t: torch.Tensor, dtype: torch.dtype, rows: int, numbers: int, what: str):
+    """Device pointer of `rows` rows of so many numbers each, or more rows."""
+    p = _ptr(t)
+    if t is None:                                                      # (the library says so)
+        return p
+    if t.dtype != dtype:
+        raise TypeError(f"{what} is {str(dtype)[6:]}")
+    if t.dim() < 2 or t.shape[0] < rows or t.numel() != t.shape[0] * numbers:
+        raise ValueError(f"{what} has {rows} rows or more of {numbers} numbers each")
+    return p
+
+
 def ag_kv_append_rope(cache: KVCache, rope: Rope, q, q_out, k_new, v_new, block_tables, prefix_lens, new_lens, cu_new, total_new: int, stream=None):
-    """q and q_out are [T][Hq][D], or None both."""
+    """q and q_out are [T][Hq][D], or None both; k_new and v_new [T][Hkv][D]; all of the cache's dtype, and of total_new rows or more."""
     st = (_native or _calls()).kv_append_rope(cache, rope, q, q_out, k_new, v_new, block_tables, prefix_lens, new_lens, cu_new, total_new, stream)
     if st is not None:
         return _check(st)
-    c, r = cache.c_struct(), rope.c_struct()
-    _check(lib().ag_kv_append_rope(C.byref(c), C.byref(r), _ptr(q), _ptr(q_out), 0 if q is None else q.shape[1], _ptr(k_new), _ptr(v_new),
-                                   _i32(block_tables), block_tables.shape[1], _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0],
+    c, r, dtype = cache.c_struct(), rope.c_struct(), torch_dtype(cache.dtype)
+    hq = 0 if q is None else q.shape[1]
+    qp, qo = (_whole_rows(t, dtype, total_new, hq * cache.head_dim, what) for t, what in ((q, "q"), (q_out, "q_out")))
+    kp, vp = (_whole_rows(t, dtype, total_new, cache.num_kv_heads * cache.head_dim, what) for t, what in ((k_new, "k_new"), (v_new, "v_new")))
+    _check(lib().ag_kv_append_rope(C.byref(c), C.byref(r), qp, qo, hq, kp, vp, _i32(block_tables), block_tables.shape[1], _i32(prefix_lens), _i32(new_lens), _i32(cu_new), new_lens.shape[0],
                                    total_new, _stream(stream)))
 
 
@@ -613,18 +627,6 @@ def ag_kv_append_latent(cache: LatentCache, rope: Optional[Rope], latent_new, ro
 
 def ag_attn_decode_latent_workspace_bytes(batch: int, num_q_heads: int, latent_dim: int, max_ctx: int) -> int:
     return int(lib().ag_attn_decode_latent_workspace_bytes(batch, num_q_heads, latent_dim, max_ctx))
-
-
-def _whole_rows(t: torch.Tensor, dtype: torch.dtype, rows: int, numbers: int, what: str):
-    """Device pointer of `rows` rows of so many numbers each, or more rows."""
-    p = _ptr(t)
-    if t is None:                                                      # (the library says so)
-        return p
-    if t.dtype != dtype:
-        raise TypeError(f"{what} is {str(dtype)[6:]}")
-    if t.dim() < 2 or t.shape[0] < rows or t.numel() != t.shape[0] * numbers:
-        raise ValueError(f"{what} has {rows} rows or more of {numbers} numbers each")
-    return p
 
 
 def _latent_rows(cache: LatentCache, q, out, rows: int, heads: int):

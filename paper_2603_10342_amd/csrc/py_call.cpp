@@ -348,13 +348,17 @@ PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
         Reader r;
         ag_kv_cache c;
         ag_rope rope;
-        const at::Tensor *q = nullptr, *bt, *lens;
+        const at::Tensor *q = nullptr, *q_rows = nullptr, *k_rows, *v_rows, *bt, *lens;
         r.cache(a[0], c);
         r.rope(a[1], rope);
         const bool queries = a[2] != Py_None || a[3] != Py_None;
-        void *qp = queries ? r.device(a[2], &q) : nullptr, *qo = queries ? r.device(a[3]) : nullptr, *k = r.device(a[4]), *v = r.device(a[5]);
+        void *qp = queries ? r.device(a[2], &q) : nullptr, *qo = queries ? r.device(a[3], &q_rows) : nullptr, *k = r.device(a[4], &k_rows), *v = r.device(a[5], &v_rows);
         const int32_t *b = r.ints(a[6], &bt), *prefix = r.ints(a[7]), *len = r.ints(a[8], &lens), *cu = r.ints(a[9]);
         const int32_t pages = r.size(bt, 1), batch = r.size(lens, 0), total = r.number(a[10]), hq = queries ? r.size(q, 1) : 0;
+        const at::ScalarType type = r.plain && c.dtype == AG_F32 ? at::kFloat : at::kBFloat16;
+        for (const at::Tensor* t : {q, q_rows})
+            if (queries) r.whole_rows(t, type, total, (int64_t)hq * c.head_dim);
+        for (const at::Tensor* t : {k_rows, v_rows}) r.whole_rows(t, type, total, (int64_t)c.num_kv_heads * c.head_dim);
         void* s = r.stream(a[11]);
         return finish(r, [&] { return entries.kv_append_rope(&c, &rope, qp, qo, hq, k, v, b, pages, prefix, len, cu, batch, total, s); });
     });
