@@ -16,6 +16,8 @@
  *     number of heads; all pointers 16-byte aligned (AG_ERR_INVALID_ARG otherwise).
  *   - max_ctx is at most 2^31 - 1025 (AG_ERR_INVALID_ARG beyond it).
  *   - Scores and the softmax's sums are fp32; softmax weights are rounded to bf16 for the value product, and summed as rounded.
+ *   - Latent channels up to 2^60 in magnitude: a softmax weight stands at up to 2^40 (under the largest score of the first keys that a workgroup meets, not of all),
+ *     so that fp32 sums of larger ones may come out infinite where the result is not.
  *   - Slots that no token uses may hold anything, NaN included.  Table entries that no token uses are not followed.
  *   - What is not finite in a row reaches the query rows that see its token, and no other.
  *   - Results are reproducible: partial results are merged in a fixed order, same inputs give the same bits (under

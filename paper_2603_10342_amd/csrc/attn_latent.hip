@@ -42,6 +42,7 @@ constexpr int kStages = 4;              // tiles in LDS: the one whose values ar
 constexpr int kMostShares = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 // What a column's reference m may be exceeded by: a lane's 16 weights of a tile sum to at most this.  Weights are floating-point numbers, as exact at 2^40 as at 1.
+// O is then below 2^41 x a context's tiles (2^26) x a channel: fp32 holds it for channels up to 2^60, which is the range that the header gives.
 constexpr float kMostWeight = 1099511627776.0f;
 constexpr float kLeastSum = 1.0f / kMostWeight;
 
