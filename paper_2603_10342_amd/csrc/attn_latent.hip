@@ -845,9 +845,11 @@ int shares_of(int64_t units, int64_t tiles, int cols, int cus)
 }
 // A unit's lead, measured in whole prompts of 500 to 700 rows at 128 heads, where a share has up to fifty: 4, 8, 12 tiles 356, 287, 287 us; where shares are smaller than
 // that, less, so that none is left with a lead alone.
-// Where no unit is cut and a share need have one at most, a lead beside which their tiles do not count, so that none has two (20 rows behind 30 tokens, 32 heads: 10.4 us,
-// by their tiles 14.9).
-constexpr int kMostLead = 8, kOnlyLead = 1024;
+// Where no unit is cut and a share need have one at most, a lead beside which their tiles do not count, so that none has two: what units of 1 to 16 tiles
+// differ by adds up to 128 x 7.5 tiles at most, and has to stay below half a unit; where units are fewer than shares, a share is shorter than a unit by a 256th
+// of one, which has to be more than their tiles (20 rows behind 30 tokens, 32 heads: 10.4 us, by their tiles 14.9; 256 sessions of 2, 4, .. 512 tokens, 128 heads: 50.8, with a lead of
+// 1024 tiles 55.5).
+constexpr int kMostLead = 8, kOnlyLead = 8192;
 int lead_of(int64_t units, int64_t tiles, int shares, int uncut)
 {
     if (units <= shares && tiles <= uncut) return kOnlyLead;
