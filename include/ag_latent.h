@@ -21,7 +21,7 @@
  *   - Slots that no token uses may hold anything, NaN included.  Table entries that no token uses are not followed.
  *   - What is not finite in a row reaches the query rows that see its token, and no other.
  *   - Results are reproducible: partial results are merged in a fixed order, same inputs give the same bits (under
- *     the same max_new and max_ctx, on streams of as many CUs: these decide how a batch is cut).
+ *     the same total_new, max_new and max_ctx, on streams of as many CUs: these decide how a batch is cut).
  */
 #ifndef AG_LATENT_H
 #define AG_LATENT_H

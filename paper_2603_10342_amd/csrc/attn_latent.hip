@@ -16,9 +16,10 @@
 // Work is dealt in equal shares of key tiles, one a workgroup and CU: units (session, column tile) lie end to end, a share cuts them where it ends, and the
 // pieces' partial (max, sum, O) go through the workspace and are merged in order by a second launch.
 //
-// Measured, L + R = 512 + 64.  Eight chunks of 32 to 256 rows onto 2048 to 8192 tokens, 128 heads: 1460 us, 1.28 PFLOP/s, 78 % of the products' own rate.  A decode step of 64
-// sessions of 1024 to 4096 tokens, 128 heads: 87 us, of which 17 are the merge of 82 MB (its 214 MB alone would take 39).  Four sessions of 20000 to 32768, 16 heads: 35 us,
-// 3.6 TB/s.  One of 1000, 32 heads: 13 us, all of it latency.
+// Measured, L + R = 512 + 64, from card to card.  Eight chunks of 32 to 256 rows onto 2048 to 8192 tokens, 128 heads: 1440 to 1490 us, 1.25 to 1.29 PFLOP/s, 78 % of the
+// products' own rate.  A decode step of 64 sessions of 1024 to 4096 tokens, 128 heads: 80 to 93 us, of which 17 are the merge of 82 MB (its 214 MB alone would take 43 at a
+// copy's rate).  Four sessions of 20000 to 32768, 16 heads: 35 to 42 us, 3.0 to 3.6 TB/s.  One of 1000, 32 heads: 13 us, all of it latency.  128 + 64 channels, with
+// the rules below as they were measured at 512 + 64: 560, 33, 20 and 9.8 us (at a product's or a copy's rate 401, 14, 8.5 and a launch).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -532,6 +533,7 @@ __global__ __launch_bounds__(256, 1) void latent_kernel(AttnArgs a, int least, i
 
             // m is a reference that every weight of the column is taken under, the largest score of its first tile: weights may come out far above one, and only if they
             // leave what kMostWeight allows for (or nothing came out at all) the piece is done again, under the largest score of all its tiles.  O never has to be rescaled.
+            // (Two passes more: scores that rise by 30 nats in a context's last quarter, 64 sessions' decode 81 -> 131 us, eight chunks 1442 -> 3520; by 20 nats no slower.)
             float m = -INFINITY, lsum;
             f32x16 o[kCb];
             bool wrong = false;                  // this column's weights
@@ -823,9 +825,16 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(const unsigned char* 
 // 32 heads 13.3 / 15.1 / 18.9; two of 10500 together, 128 heads 38.2 / 35.1 / 32.0.
 constexpr int least_tiles(int cols) { return cols == 32 ? 2 : cols == 64 ? 4 : 8; }
 // A unit of so many tiles or fewer is not cut: two shares' least ones (four prompts of 500 to 700 rows, 128 heads: 281 us, with every unit cut 291).
-// Contexts of 512 tokens and less stay whole altogether where there are units for an eighth of the CUs, and nothing is merged: decode, us, cut / whole, 128 sessions of 100 to
-// 300 tokens, 128 heads 36 / 24; 64 of 200 to 400, 64 heads 26 / 20; 16 of 100 to 500, 128 heads 23 / 21; 60 rows behind 300, 100 heads 36 / 22; but 4 sessions of 200 to 400,
-// 32 heads 12 / 18.
+// Contexts of 512 tokens and less stay whole altogether where there are units for an eighth of the CUs, and nothing is merged: decode, us, cut / whole,
+//                                                100 to 300 tokens    300 to 512    512
+//     16 units (16 sessions, 16 heads)                 14.7 / 15.3     14.4 / 21.7    17.2 / 22.1
+//     32 units (32 sessions, 16 heads)                 16.3 / 16.1     17.6 / 22.1    20.8 / 22.4
+//     32 units (32 sessions, 32 heads)                 16.8 / 16.3     21.0 / 22.1    23.3 / 22.7
+//     32 units ( 8 sessions, 128 heads)                16.0 / 15.6     20.8 / 22.0    22.1 / 22.4
+//     48 units (48 sessions, 32 heads)                 19.6 / 16.3     23.6 / 22.5    24.8 / 23.0
+//     64 units (16 sessions, 128 heads)                19.7 / 15.6     23.3 / 22.4    24.4 / 22.3
+//     128 units (128 sessions, 128 heads)              35.7 / 23.1     40.8 / 40.8    42.2 / 42.2
+// and of chunks, whose pieces have more columns: 100 rows behind 300, 128 heads 41.9 / 24.2; 8 sessions' 4 rows behind 200 to 400, 128 heads 29.3 / 20.1.
 constexpr int kWholeTiles = 16;
 int uncut_tiles(int64_t units, int64_t tiles, int cols, int cus)
 {
