@@ -78,6 +78,10 @@ ag_status ag_rope_rows(const ag_rope* rope, int32_t dtype, const void* x, int64_
         if (s < 0 || s > most || s % eight) { set_error("strides must be multiples of 16 bytes and not negative"); return AG_ERR_INVALID_ARG; }
     if (!rope::aligned(x) || !rope::aligned(y)) { set_error("x and y must be 16-byte aligned"); return AG_ERR_INVALID_ARG; }
     if (x == y && (x_token_stride != y_token_stride || x_head_stride != y_head_stride)) { set_error("rows that are rotated where they stand have one pair of strides"); return AG_ERR_INVALID_ARG; }
+    if ((total_new > 1 && y_token_stride < head_dim) || (num_heads > 1 && y_head_stride < head_dim)) {
+        set_error("rows of y overlap each other: strides %lld and %lld of %d channels", (long long)y_token_stride, (long long)y_head_stride, head_dim);
+        return AG_ERR_INVALID_ARG;
+    }
     if (total_new == 0) return AG_OK;
     if ((total_new + 3ll) / 4 > rope::kMostWorkgroups) { set_error("total_new=%d: too many rows for one launch", total_new); return AG_ERR_INVALID_ARG; }
     return rope::launch_rows(rope::RowsArgs{rope::spec_of(*rope, transposed != 0), rope->layout, dtype, x, x_token_stride, x_head_stride, y, y_token_stride,
