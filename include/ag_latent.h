@@ -48,7 +48,7 @@ AG_API int32_t ag_latent_row(int32_t latent_dim, int32_t rope_dim);
  * Append: new token i of session s (row cu_new[s] + i of latent_new and rope_new) is written to logical position prefix_lens[s] + i, its rotary part
  * rotated by that position on the way (rope: rot_dim = rope_dim; NULL copies rows that are rotated already).  latent_new is [T][latent_dim] and rope_new
  * [T][rope_dim], with token strides of their own in elements (multiples of 8): both may be slices of one projection's rows.
- * total_new >= cu_new[batch] sizes the launch.
+ * total_new >= cu_new[batch] sizes the launch, and both have so many rows: those behind the last session's may be read.
  */
 AG_API ag_status ag_kv_append_latent(const ag_latent_cache* cache, const ag_rope* rope, const void* latent_new, int64_t latent_stride,
                               const void* rope_new, int64_t rope_stride,

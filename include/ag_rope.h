@@ -50,7 +50,8 @@ AG_API ag_status ag_rope_turns(double* turns, int32_t rot_dim, double base, int3
  * [T][heads][head_dim] with strides of their own in elements, channels contiguous: a slice of a wider row is rotated where it stands.
  * y may be x (same pointer, same strides); otherwise they may not overlap.  Rows of y may not overlap each other: its strides are head_dim or more where there are
  * more rows or heads than one (AG_ERR_INVALID_ARG otherwise); those of x may, and may be 0, where y is not x.  transposed != 0 applies the transposed matrix, sin with the other sign: the
- * rotation's gradient (m and all), and with m = 1 its inverse.  Rows behind the last session's are left as they were.
+ * rotation's gradient (m and all), and with m = 1 its inverse.  total_new >= cu_new[batch] sizes the launch, and x has so many rows: those behind the last
+ * session's may be read; y's are left as they were.
  * head_dim a multiple of 8 and at least rot_dim; pointers 16-byte aligned and strides multiples of 16 bytes (AG_ERR_INVALID_ARG otherwise).
  */
 AG_API ag_status ag_rope_rows(const ag_rope* rope, int32_t dtype, const void* x, int64_t x_token_stride, int64_t x_head_stride, void* y,
